@@ -263,7 +263,10 @@ def prepare(case, seed):
         for p in [p for row in table for p in row if p >= 0]:
             ref[p] += 1
         s["table"], s["ref"] = ints(table), ints(ref)
-        s["free"], s["n_free"] = ints(pages[at:] + [0] * at), ints([n - at])
+        s["free"] = ints(pages[at:] + [0] * at)
+        # the pool's state: the number of free pages, then words that are zero between calls (the library's)
+        s["state"] = ints([n - at] + [0] * (3 + (n + 31) // 32))
+        s["n_free"] = s["state"][:1]
         s["cache"] = _cache(c, gen, (n, hk, pr))
         s["src"] = ints([b for b in range(B) for _ in range(per)])
         s["dst"] = ints(list(range(B, B + B * per)))
@@ -286,7 +289,10 @@ def prepare(case, seed):
                 ref[p] += 1
             table.append(row + [-1] * (P - most[b]))
         s["table"], s["ref"] = ints(table), ints(ref)
-        s["free"], s["n_free"] = ints(pages[at:] + [0] * at), ints([n - at])
+        s["free"] = ints(pages[at:] + [0] * at)
+        # the pool's state: the number of free pages, then words that are zero between calls (the library's)
+        s["state"] = ints([n - at] + [0] * (3 + (n + 31) // 32))
+        s["n_free"] = s["state"][:1]
         s["rows"], s["first"], s["end"] = ints([x + c["tokens"] for x in ctx]), ints(ctx), ints([cap] * B)
     if own:  # the descriptors and the workspace that a program keeps beside its cache
         import paper_2608_08081_b200 as iq
@@ -299,7 +305,7 @@ def prepare(case, seed):
             s["shape"] = iq.Shape(n_seqs, c["heads"], hk, d, cap, c["bits"])
             s["handle"] = iq.Cache(k["k_codes"], k["k_scales"], k["v_codes"], k["v_scales"], s["table"], pr)
         if "ref" in s:
-            s["pool"] = iq.PagePool(s["table"], s["ref"], s["free"], s["n_free"], pr)
+            s["pool"] = iq.PagePool(s["table"], s["ref"], s["free"], s["state"], pr)
         if c["kind"] == "tree":
             lv, th = _levels(c["bits"], c["grid"])
             s["codebook"] = iq.Codebook(tuple(lv), tuple(th))
@@ -427,10 +433,11 @@ def _plain_keep(s):
     w[blocks[0], :, blocks[1]] = _pack(codes, bits)
 
 
-def _plain_reserve(s, rows):
+def _plain_reserve(s, first, end):
     table, ref, free, n_free = s["table"], s["ref"], s["free"], s["n_free"]
     pr = s["case"]["page_rows"]
-    want = (torch.arange(table.shape[1], device="cuda") * pr < rows[:, None]) & (table < 0)
+    start = torch.arange(table.shape[1], device="cuda") * pr
+    want = (start + pr > first[:, None]) & (start < end[:, None]) & (table < 0)
     k = want.flatten().cumsum(0).view_as(want) - 1
     got = want & (k < n_free)
     page = free.gather(0, (n_free - 1 - k).clamp(min=0).flatten()).view_as(table)
@@ -506,9 +513,9 @@ def run(state):
             _plain_fork(s)
         return dict(s["cache"], **pool)
     if own:
-        s["iq"].iq_reserve_pages(s["pool"], s["rows"], status_dev=s["status"])
+        s["iq"].iq_reserve_pages(s["pool"], s["first"], s["rows"], status_dev=s["status"])
     else:
-        _plain_reserve(s, s["rows"])
+        _plain_reserve(s, s["first"], s["rows"])
     return pool
 
 
@@ -531,9 +538,9 @@ def work(case):
         pages = sum(-(-x // pr) for x in ctx)
         return dict(bytes=c["tokens"] * (4 * sum(x % pr for x in ctx) * hk * row + 24 * pages), flops=0)
     ctx = _context(c)
-    P = _cap(c, c["tokens"]) // pr
+    # the entries of the pages that are given back and taken, each in the table, the counts and the list
     moved = sum(-(-(x + c["tokens"]) // pr) - -(-x // pr) for x in ctx)
-    return dict(bytes=4 * len(ctx) * P * 2 + 24 * moved, flops=0)
+    return dict(bytes=12 * len(ctx) + 48 * moved + 4, flops=0)
 
 
 # ------------------------------------------------------------------------------------------------- the definition, fp64
