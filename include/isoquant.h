@@ -23,7 +23,7 @@
  *   - Device-side conditions that cannot be known on the host are reported through an optional
  *     `status_dev` array of 4 uint32 (zeroed by the caller): [0] bit mask of IQ_STATUS_* flags,
  *     [1] rows whose codes were re-decided in fp64 (see iq_quantize_append), [2] rows skipped because they fell outside the
- *     cache, [3] reserved. Nothing on the device traps or spins without a bound: the waits of the
+ *     cache (the page pool's calls: entries or forks that they could not serve), [3] reserved. Nothing on the device traps or spins without a bound: the waits of the
  *     decode, bulk append and reconstruction kernels on asynchronous copies and tensor-core results give up after 65536 polls
  *     of at most 20 us each (about a second at worst; a wait that works lasts microseconds). Decode and append then flag
  *     IQ_STATUS_WAIT_TIMEOUT and return with invalid results; iq_reconstruct_rows, which has no status array, writes NaN
@@ -96,8 +96,11 @@ enum {
   IQ_STATUS_ROW_OUT_OF_RANGE = 1u, /* quantize-append: append_pos + i >= t_cap, row skipped */
   IQ_STATUS_WAIT_TIMEOUT = 2u,     /* decode, bulk append: a bounded wait on an asynchronous copy or tensor-core result ran out; results invalid */
   IQ_STATUS_SCALE_OVERFLOW = 8u,   /* binary16 scales: a row norm above 65504 was stored as 65504 */
-  IQ_STATUS_BAD_PAGE = 4u          /* paged cache: a block-table entry outside [0, num_pages) was met: read as page 0 by
-                                      decode / reconstruct, the rows skipped (and counted in [2]) by quantize-append */
+  IQ_STATUS_BAD_PAGE = 4u,         /* paged cache: a block-table entry outside [0, num_pages) was met: read as page 0 by
+                                      decode / tree attention / reconstruct, the rows skipped (and counted in [2]) by quantize-append
+                                      and iq_keep_rows; see the page pool's calls for theirs */
+  IQ_STATUS_NO_PAGE = 16u,         /* page pool: fewer free pages than a call needed; the entries that got none hold -1, counted in [2] */
+  IQ_STATUS_BAD_SEQUENCE = 32u     /* iq_fork_sequences: a fork whose numbers are out of range or that conflicts with another, skipped, counted in [2] */
 };
 
 typedef struct iq_shape {
@@ -443,6 +446,108 @@ int iq_decode_attention_static(const iq_shape* shape, const float* rot_dev, cons
  * most polls * 20 us.
  */
 int iq_selftest_bounded_wait(uint32_t* status_dev, uint32_t polls, void* stream);
+
+/*
+ * Attention for drafted tokens over the packed cache (the paper decodes one token at a time; this is the same compressed-space
+ * attention for the tokens that a speculative step verifies, for a short chunk of a prompt, and for sliding-window layers).
+ * A sequence holds ctx_lens[b] context rows and, behind them, the rows of its drafted tokens: token t at row ctx_lens[b] + t,
+ * appended with iq_quantize_append before the call. Token t attends to the context and to the drafted tokens that its mask names:
+ *   bit j % 32 of word tree_mask[b][t][j / 32]: token t sees drafted token j. A tree's tokens name their ancestors and themselves.
+ *   Any pattern is taken; bits of tokens that the sequence has not are ignored. NULL: a chain, token t sees tokens 0 .. t.
+ * Position of token t: pos_t = ctx_lens[b] + (number of drafted tokens that it sees) - 1. window > 0: of the context, rows below
+ * pos_t - window + 1 are left out, but for rows below `sinks`; a drafted token j is left out by the same rule for its position
+ * pos_j. A token that sees no row yields out = 0, lse = -inf.
+ *   q              device binary16, element (b, t, h, c) at b*stride_b + t*stride_t + h*stride_h + c (strides in elements,
+ *                  multiples of 8, not negative; 16-byte aligned); not quantised.
+ *   ctx_lens_dev   device int32 [batch], clamped to [0, t_cap]; rows from t_cap on are not seen.
+ *   tree_mask_dev  device uint32 [batch][n_tokens_max][(n_tokens_max + 31) / 32], or NULL.
+ *   n_tokens_dev   device int32 [batch] drafted tokens per sequence (clamped to [0, n_tokens_max]), or NULL for n_tokens_max
+ *                  everywhere. out and lse_out of the tokens from there on are left as they are.
+ *   n_tokens_max   0 .. IQ_TREE_MAX_TOKENS.
+ *   window, sinks  >= 0; window = 0: all of the context is seen.
+ *   workspace_dev  device, iq_tree_workspace_bytes(shape, n_tokens_max) bytes for the device the call runs on, 16-byte aligned; needs
+ *                  no initialisation. Calls that share a workspace must be ordered on one stream (a captured graph shares what
+ *                  it was captured with).
+ *   out            device [batch][n_tokens_max][n_q_heads][head_dim], fp32 or binary16 (out_is_fp16), 16-byte aligned.
+ *   lse_out        device fp32 [batch][n_tokens_max][n_q_heads] or NULL.
+ *   status_dev     optional (see top).
+ * Codebooks as for iq_decode_attention. Blocks of 128 rows that no token sees are not read, and their pages need not be in the
+ * block table. The cache is read once for up to IQ_TREE_TILE (token, query head) pairs of a KV head, in the order of tokens.
+ * The same inputs give the same bits in every call on the same kind of device.
+ * Limits: batch * n_kv_heads * ceil(n_tokens_max * heads per KV head / 16) and batch * n_tokens_max * n_q_heads below 2^31
+ * (IQ_ERR_LIMIT).
+ */
+#define IQ_TREE_MAX_TOKENS 256
+size_t iq_tree_workspace_bytes(const iq_shape* shape, int32_t n_tokens_max);
+int iq_tree_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                      int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                      const uint32_t* tree_mask_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int32_t window,
+                      int32_t sinks, void* workspace_dev, void* out, int32_t out_is_fp16, float* lse_out, uint32_t* status_dev,
+                      void* stream);
+
+/*
+ * Accepting drafted tokens: row base_pos[b] + i of every KV head receives what row base_pos[b] + keep[b][i] held when the call
+ * began, K and V, codes and scales, for i < n_keep[b]. The order of `keep` is free, an index may occur twice; other rows are left
+ * as they are. The caller advances its lengths.
+ *   keep_dev     device int32 [batch][n_keep_max]; n_keep_dev device int32 [batch] (clamped to [0, n_keep_max]) or NULL for n_keep_max.
+ *   n_keep_max   0 .. IQ_KEEP_MAX_ROWS.
+ *   status_dev   optional. A row whose source or destination lies outside [0, t_cap) is skipped (IQ_STATUS_ROW_OUT_OF_RANGE), as is
+ *                one in a page outside the pool (IQ_STATUS_BAD_PAGE); both are counted in [2], once per row and KV head.
+ * Only the bits of the destination rows change. Sequences whose tables share a page of destination rows must not be kept at once.
+ */
+#define IQ_KEEP_MAX_ROWS 256
+int iq_keep_rows(const iq_shape* shape, const iq_cache* cache, const int32_t* base_pos_dev, const int32_t* keep_dev,
+                 const int32_t* n_keep_dev, int32_t n_keep_max, uint32_t* status_dev, void* stream);
+
+/*
+ * A pool of pages on the device: which page holds which rows of which sequence, how many sequences hold a page, and which pages are
+ * free. The calls below update it on the device, ordered like kernels on their stream; nothing returns to the host.
+ *   block_table_dev  int32 [n_seqs][pages_per_seq]: the block table of iq_cache, -1 where a sequence holds no page. A step over the
+ *                    first B sequences takes the same table with iq_shape.batch = B.
+ *   ref_count_dev    int32 [num_pages]: table entries that hold the page; 0: free.
+ *   free_list_dev    int32 [num_pages]: the free pages, a stack: the first state_dev[0] entries.
+ *   state_dev        int32 [iq_page_pool_state_ints(num_pages)]: [0] the number of free pages, the rest 0 before the first call (and,
+ *                    as far as the caller sees, ever after).
+ * Calls that update a pool must be ordered on one stream. Two calls with the same arguments on equal pools leave equal pools.
+ */
+typedef struct iq_page_pool {
+  int32_t* block_table_dev;
+  int32_t* ref_count_dev;
+  int32_t* free_list_dev;
+  int32_t* state_dev;
+  int32_t n_seqs, pages_per_seq, num_pages, page_rows; /* page_rows: multiple of 128 */
+} iq_page_pool;
+size_t iq_page_pool_state_ints(int32_t num_pages);
+
+/* Pages for rows [first_row[b], end_row[b]) of every sequence b < n_seqs (device int32 [n_seqs]; clamped to the table): an entry below
+ * 0 gets a free page with count 1. The free pages are taken from the top of the stack, in the order of sequences and, in one, of
+ * rows; when they run out, the entries that got none keep -1 (IQ_STATUS_NO_PAGE, counted in status[2]). */
+int iq_reserve_pages(const iq_page_pool* pool, const int32_t* first_row_dev, const int32_t* end_row_dev, uint32_t* status_dev,
+                     void* stream);
+/* Gives back the pages of which all rows lie in [first_row[b], end_row[b]): the entry becomes -1, the page's count drops by one, and
+ * pages whose count reaches 0 are put on the stack in ascending order. An entry outside the pool, or of a page whose count is 0
+ * already, becomes -1 and changes nothing else (IQ_STATUS_BAD_PAGE, counted in status[2]). */
+int iq_release_pages(const iq_page_pool* pool, const int32_t* first_row_dev, const int32_t* end_row_dev, uint32_t* status_dev,
+                     void* stream);
+/*
+ * Sequence dst[i] becomes a branch of sequence src[i] after its first n_rows[i] rows (device int32 [n_forks] each): pages full of
+ * such rows are shared (their counts rise); a last page that is partly filled is copied (the 128-row blocks that hold rows) into a
+ * free one, taken from the top of the stack in the order of the forks; the rest of dst's entries become -1. What dst's entries held
+ * before is overwritten: release it first. A fork is skipped, its dst left as it was (IQ_STATUS_BAD_SEQUENCE, counted in status[2]),
+ * when src or dst is outside [0, n_seqs), n_rows outside [0, pages_per_seq * page_rows], or dst is the src of any fork of the call or
+ * the dst of an earlier one. No free page for the copy: IQ_STATUS_NO_PAGE, counted, the entry is -1. An entry of src outside the pool:
+ * IQ_STATUS_BAD_PAGE, counted, dst's entry is -1 (where a copy was due: a page that nothing was copied to).
+ * cache: the pool's arrays (its table pointer is not read: the pool's is); shape: its n_kv_heads, head_dim and bits.
+ * n_forks 0 .. IQ_MAX_FORKS.
+ */
+#define IQ_MAX_FORKS 1024
+int iq_fork_sequences(const iq_shape* shape, const iq_cache* cache, const iq_page_pool* pool, const int32_t* src_seq_dev,
+                      const int32_t* dst_seq_dev, const int32_t* n_rows_dev, int32_t n_forks, uint32_t* status_dev, void* stream);
+/* Whole pages copied within the cache's arrays: page dst[i] receives page src[i] (device int32 [n_pages]). A pair with a page
+ * outside the pool is skipped (IQ_STATUS_BAD_PAGE, counted in status[2]); src[i] = dst[i] does nothing. No page may be the
+ * destination of two pairs, or of one and the source of another. cache->block_table_dev must be set (its page_rows and num_pages are used). */
+int iq_copy_pages(const iq_shape* shape, const iq_cache* cache, const int32_t* src_pages_dev, const int32_t* dst_pages_dev,
+                  int32_t n_pages, uint32_t* status_dev, void* stream);
 
 /* A slot count that leaves the decode kernel free to balance the launch when the longest sequence has
  * max_seq_len rows (more slots than needed only cost the writing and merging of unused ones). */

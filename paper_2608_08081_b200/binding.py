@@ -30,6 +30,11 @@ class _IqCache(ctypes.Structure):
                 ("block_table_dev", _vp), ("page_rows", _i32), ("num_pages", _i32), ("scales_fp16", _i32)]
 
 
+class _IqPagePool(ctypes.Structure):
+    _fields_ = [("block_table_dev", _vp), ("ref_count_dev", _vp), ("free_list_dev", _vp), ("state_dev", _vp),
+                ("n_seqs", _i32), ("pages_per_seq", _i32), ("num_pages", _i32), ("page_rows", _i32)]
+
+
 class IQError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -89,6 +94,17 @@ def _load():
     lib.iq_decode_step_workspace_bytes.restype = ctypes.c_size_t
     lib.iq_decode_step_fused.argtypes = [ctypes.POINTER(_IqShape), _vp, ctypes.POINTER(_IqCodebook), _vp, _vp, _vp,
                                          ctypes.POINTER(_IqCache), _vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp]
+    lib.iq_tree_workspace_bytes.argtypes = [ctypes.POINTER(_IqShape), _i32]
+    lib.iq_tree_workspace_bytes.restype = ctypes.c_size_t
+    lib.iq_tree_attention.argtypes = [ctypes.POINTER(_IqShape), _vp, ctypes.POINTER(_IqCodebook), _vp, _i64, _i64, _i64,
+                                      ctypes.POINTER(_IqCache), _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp]
+    lib.iq_keep_rows.argtypes = [ctypes.POINTER(_IqShape), ctypes.POINTER(_IqCache), _vp, _vp, _vp, _i32, _vp, _vp]
+    lib.iq_page_pool_state_ints.argtypes = [_i32]
+    lib.iq_page_pool_state_ints.restype = ctypes.c_size_t
+    lib.iq_reserve_pages.argtypes = lib.iq_release_pages.argtypes = [ctypes.POINTER(_IqPagePool), _vp, _vp, _vp, _vp]
+    lib.iq_fork_sequences.argtypes = [ctypes.POINTER(_IqShape), ctypes.POINTER(_IqCache), ctypes.POINTER(_IqPagePool), _vp, _vp, _vp,
+                                      _i32, _vp, _vp]
+    lib.iq_copy_pages.argtypes = [ctypes.POINTER(_IqShape), ctypes.POINTER(_IqCache), _vp, _vp, _i32, _vp, _vp]
     return lib
 
 
@@ -453,6 +469,102 @@ def iq_selftest_bounded_wait(status, polls: int, stream=None) -> None:
     _check(_lib.iq_selftest_bounded_wait(_ptr(status), int(polls), _stream(stream)), "iq_selftest_bounded_wait")
 
 
+# ------------------------------------------------------------------ drafted tokens, rows and pages
+@dataclass
+class PagePool:
+    """Which page holds which rows, on the device: block_table int32 [n_seqs][pages_per_seq] (-1: no page; the same tensor as the
+    Cache's), ref_count int32 [num_pages], free_list int32 [num_pages] (a stack), state int32 [iq_page_pool_state_ints(num_pages)]
+    ([0]: free pages, the rest zero). new_page_pool makes one with every page free."""
+    block_table: torch.Tensor
+    ref_count: torch.Tensor
+    free_list: torch.Tensor
+    state: torch.Tensor
+    page_rows: int
+
+    def c(self) -> _IqPagePool:
+        for t in (self.block_table, self.ref_count, self.free_list, self.state):
+            assert t.dtype == torch.int32 and t.is_contiguous()
+        n = self.ref_count.numel()
+        assert self.block_table.dim() == 2 and self.free_list.numel() == n and self.state.numel() >= 4 + (n + 31) // 32
+        return _IqPagePool(self.block_table.data_ptr(), self.ref_count.data_ptr(), self.free_list.data_ptr(), self.state.data_ptr(),
+                           self.block_table.shape[0], self.block_table.shape[1], n, self.page_rows)
+
+
+def iq_page_pool_state_ints(num_pages: int) -> int:
+    return int(_lib.iq_page_pool_state_ints(num_pages))
+
+
+def _ints(t, numel=None):
+    assert t is None or (t.dtype in (torch.int32, torch.uint32) and t.is_contiguous() and (numel is None or t.numel() == numel))
+    return _ptr(t)
+
+
+def iq_tree_workspace_bytes(shape: Shape, n_tokens_max: int) -> int:
+    cs = shape.c()
+    return int(_lib.iq_tree_workspace_bytes(ctypes.byref(cs), n_tokens_max))
+
+
+def iq_tree_attention(shape: Shape, rot_dev, codebook: Codebook, q, cache: Cache, ctx_lens_dev, tree_mask_dev, n_tokens_dev, workspace, out,
+                      lse_out=None, window: int = 0, sinks: int = 0, status_dev=None, stream=None) -> None:
+    """Attention of drafted tokens: q fp16 [B][T][H_q][d] (any strides with a contiguous last dim), the tokens' own rows appended
+    behind the ctx_lens[b] context rows. tree_mask_dev: int32 / uint32 [B][T][ceil(T / 32)], bit j: the token sees drafted token j
+    (None: a chain); n_tokens_dev: int32 [B] or None (all T). out fp16 or fp32 [B][T][H_q][d], lse_out fp32 [B][T][H_q].
+    window > 0: only the window's context rows and the first `sinks` are seen. workspace: a device uint8 tensor of
+    iq_tree_workspace_bytes(shape, T) bytes."""
+    B, T, H, d = q.shape
+    assert q.dtype == torch.float16 and q.stride(3) == 1 and (B, H, d) == (shape.batch, shape.n_q_heads, shape.head_dim)
+    assert tuple(out.shape) == (B, T, H, d) and out.is_contiguous() and out.dtype in (torch.float16, torch.float32)
+    assert lse_out is None or (lse_out.dtype == torch.float32 and tuple(lse_out.shape) == (B, T, H) and lse_out.is_contiguous())
+    need = iq_tree_workspace_bytes(shape, T)
+    assert workspace.is_contiguous() and workspace.numel() * workspace.element_size() >= need
+    cs, cb, cc = shape.c(), codebook.c(), cache.c()
+    _check(_lib.iq_tree_attention(ctypes.byref(cs), _ptr(rot_dev), ctypes.byref(cb), _ptr(q), q.stride(0), q.stride(1), q.stride(2),
+                                  ctypes.byref(cc), _ints(ctx_lens_dev, B), _ints(tree_mask_dev, B * T * ((T + 31) // 32)),
+                                  _ints(n_tokens_dev, B), T, window, sinks, _ptr(workspace), _ptr(out),
+                                  1 if out.dtype == torch.float16 else 0, _ptr(lse_out), _ptr(status_dev), _stream(stream)),
+           "iq_tree_attention")
+
+
+def iq_keep_rows(shape: Shape, cache: Cache, base_pos_dev, keep_dev, n_keep_dev=None, status_dev=None, stream=None) -> None:
+    """Row base_pos[b] + i receives what row base_pos[b] + keep[b][i] held: keep_dev int32 [B][n], n_keep_dev int32 [B] or None (n)."""
+    assert keep_dev.dim() == 2 and keep_dev.shape[0] == shape.batch
+    cs, cc = shape.c(), cache.c()
+    _check(_lib.iq_keep_rows(ctypes.byref(cs), ctypes.byref(cc), _ints(base_pos_dev, shape.batch), _ints(keep_dev),
+                             _ints(n_keep_dev, shape.batch), keep_dev.shape[1], _ptr(status_dev), _stream(stream)), "iq_keep_rows")
+
+
+def iq_reserve_pages(pool: PagePool, first_row_dev, end_row_dev, status_dev=None, stream=None) -> None:
+    """A page for every entry without one among rows [first_row[b], end_row[b]) (int32 [n_seqs] each)."""
+    cp, n = pool.c(), pool.block_table.shape[0]
+    _check(_lib.iq_reserve_pages(ctypes.byref(cp), _ints(first_row_dev, n), _ints(end_row_dev, n), _ptr(status_dev), _stream(stream)),
+           "iq_reserve_pages")
+
+
+def iq_release_pages(pool: PagePool, first_row_dev, end_row_dev, status_dev=None, stream=None) -> None:
+    """Gives back the pages of which all rows lie in [first_row[b], end_row[b])."""
+    cp, n = pool.c(), pool.block_table.shape[0]
+    _check(_lib.iq_release_pages(ctypes.byref(cp), _ints(first_row_dev, n), _ints(end_row_dev, n), _ptr(status_dev), _stream(stream)),
+           "iq_release_pages")
+
+
+def iq_fork_sequences(shape: Shape, cache: Cache, pool: PagePool, src_seq_dev, dst_seq_dev, n_rows_dev, status_dev=None, stream=None) -> None:
+    """Sequence dst[i] becomes a branch of sequence src[i] after its first n_rows[i] rows (int32 [n] each): whole pages are shared,
+    a partly filled one is copied."""
+    assert cache.k_scales.shape[0] == pool.ref_count.numel() and cache.k_scales.shape[2] == pool.page_rows
+    n = src_seq_dev.numel()
+    cs, cc, cp = shape.c(), cache.c(), pool.c()
+    _check(_lib.iq_fork_sequences(ctypes.byref(cs), ctypes.byref(cc), ctypes.byref(cp), _ints(src_seq_dev, n), _ints(dst_seq_dev, n),
+                                  _ints(n_rows_dev, n), n, _ptr(status_dev), _stream(stream)), "iq_fork_sequences")
+
+
+def iq_copy_pages(shape: Shape, cache: Cache, src_pages_dev, dst_pages_dev, status_dev=None, stream=None) -> None:
+    """Page dst[i] of a paged cache receives page src[i] (int32 [n] each)."""
+    n = src_pages_dev.numel()
+    cs, cc = shape.c(), cache.c()
+    _check(_lib.iq_copy_pages(ctypes.byref(cs), ctypes.byref(cc), _ints(src_pages_dev, n), _ints(dst_pages_dev, n), n, _ptr(status_dev),
+                              _stream(stream)), "iq_copy_pages")
+
+
 # ------------------------------------------------------------------ small conveniences (allocation only)
 def new_cache(shape: Shape, device="cuda", scales_dtype=torch.float32) -> Cache:
     """scales_dtype: torch.float32, or torch.float16 for binary16 scale arrays."""
@@ -473,6 +585,16 @@ def new_paged_cache(shape: Shape, num_pages: int, page_rows: int, block_table: t
     return Cache(torch.zeros(n + (P,), dtype=torch.uint8, device=device), torch.zeros(n, dtype=scales_dtype, device=device),
                  torch.zeros(n + (P,), dtype=torch.uint8, device=device), torch.zeros(n, dtype=scales_dtype, device=device),
                  block_table, page_rows)
+
+
+def new_page_pool(n_seqs: int, pages_per_seq: int, num_pages: int, page_rows: int, device="cuda") -> PagePool:
+    """A pool with every page free (page 0 is taken first) and no page in the table; pool.block_table is the table to give to
+    new_paged_cache."""
+    state = torch.zeros(iq_page_pool_state_ints(num_pages), dtype=torch.int32, device=device)
+    state[0] = num_pages
+    return PagePool(torch.full((n_seqs, pages_per_seq), -1, dtype=torch.int32, device=device),
+                    torch.zeros(num_pages, dtype=torch.int32, device=device),
+                    torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device), state, page_rows)
 
 
 class DecodeWorkspace:

@@ -89,6 +89,18 @@ iq::PageMap page_map(const iq_cache* c, const iq_shape* shape) {
   return m;
 }
 
+// SMs of the current device (148 where there is none).
+int sm_count() {
+  static int n_sm_cached[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+  if (n_sm_cached[dev] == 0) {
+    int v = 0;
+    if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && v > 0) n_sm_cached[dev] = v;
+  }
+  return n_sm_cached[dev] > 0 ? n_sm_cached[dev] : 148;
+}
+
 // Lloyd's iteration for the marginal of one coordinate of a uniform point on S^{d-1}, unit-variance units:
 // density ~ (1 - u^2/d)^((d-3)/2). Cell integrals by composite Simpson on a fixed fine grid.
 struct SphereMarginal {
@@ -830,17 +842,214 @@ int iq_selftest_bounded_wait(uint32_t* status_dev, uint32_t polls, void* stream)
   return iq::launch_bounded_wait_selftest(status_dev, polls, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
 }
 
+// ---- drafted tokens, rows and pages
+// Items, tile and CTAs of a tree attention launch, and the sections of its workspace, in bytes from its start.
+namespace {
+struct TreePlan {
+  int tile, tiles, ctas;
+  long long items;
+  size_t part_acc, part_ml, item_info, total;
+};
+int tree_plan(const iq_shape* s, int32_t n_tokens_max, TreePlan& w) {
+  const int rc = check_shape(s);
+  if (rc) return rc;
+  if (n_tokens_max < 0) return IQ_ERR_SHAPE;
+  if (n_tokens_max > IQ_TREE_MAX_TOKENS) return IQ_ERR_LIMIT;
+  const long long queries = (long long)n_tokens_max * (s->n_q_heads / s->n_kv_heads);
+  if ((long long)s->batch * s->n_kv_heads * ((queries + 15) / 16) >= (1ll << 31) - (1 << 20) || (long long)s->batch * n_tokens_max * s->n_q_heads >= (1ll << 31))
+    return IQ_ERR_LIMIT;
+  w.tile = iq::tree_tile(s->head_dim, (int)queries);
+  w.tiles = (int)((queries + w.tile - 1) / w.tile);
+  w.ctas = sm_count() * iq::tree_ctas_per_sm(s->head_dim, w.tile);
+  w.items = (long long)s->batch * s->n_kv_heads * w.tiles;
+  auto up = [](size_t x) { return (x + 15) & ~(size_t)15; };
+  const size_t parts = (size_t)(w.items + w.ctas) * w.tile;
+  size_t o = 0;
+  w.part_acc = o; o += up(parts * s->head_dim * 4);
+  w.part_ml = o; o += up(parts * 8);
+  w.item_info = o; o += up((size_t)w.items * 8);
+  w.total = o;
+  return IQ_OK;
+}
+iq::CacheArrays cache_arrays(const iq_cache* c) { return {c->k_codes, c->k_scales, c->v_codes, c->v_scales, c->scales_fp16 ? 1 : 0}; }
+
+int check_pool(const iq_page_pool* p) {
+  if (!p || !p->block_table_dev || !p->ref_count_dev || !p->free_list_dev || !p->state_dev) return IQ_ERR_NULL;
+  if (p->n_seqs < 0 || p->n_seqs > 65535 || p->pages_per_seq <= 0 || p->num_pages <= 0 || p->page_rows <= 0 || (p->page_rows & 127)) return IQ_ERR_SHAPE;
+  if ((long long)p->pages_per_seq * p->page_rows > INT32_MAX) return IQ_ERR_SHAPE;  // rows are counted in 31 bits
+  if ((long long)p->n_seqs * p->pages_per_seq > (1ll << 30)) return IQ_ERR_LIMIT;
+  return IQ_OK;
+}
+iq::PoolParams pool_params(const iq_page_pool* p, const int32_t* first_row, const int32_t* end_row, uint32_t* status) {
+  return {p->block_table_dev, p->ref_count_dev, p->free_list_dev, p->state_dev, p->n_seqs, p->pages_per_seq, p->num_pages, p->page_rows, first_row, end_row, status};
+}
+}  // namespace
+
+size_t iq_tree_workspace_bytes(const iq_shape* shape, int32_t n_tokens_max) {
+  TreePlan w;
+  return tree_plan(shape, n_tokens_max, w) == IQ_OK ? w.total : 0;
+}
+
+int iq_tree_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                      int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                      const uint32_t* tree_mask_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int32_t window,
+                      int32_t sinks, void* workspace_dev, void* out, int32_t out_is_fp16, float* lse_out, uint32_t* status_dev,
+                      void* stream) {
+  TreePlan w;
+  int rc = tree_plan(shape, n_tokens_max, w);
+  if (rc) return rc;
+  if (!rot_dev || !ctx_lens_dev) return IQ_ERR_NULL;
+  if ((rc = check_codebook(codebook, shape->bits, false))) return rc;
+  int n8[2][16];
+  float delta[2];
+  const bool grid8 = int8_grid(codebook, n8[0], delta[0], n8[1], delta[1]);
+  if (!grid8 && (rc = check_codebook(codebook, shape->bits, true))) return rc;
+  if (!grid8) delta[0] = delta[1] = 1.f;  // levels as they are
+  if ((rc = check_cache(cache, shape))) return rc;
+  if (window < 0 || sinks < 0 || stride_b < 0 || stride_t < 0 || stride_h < 0) return IQ_ERR_SHAPE;
+  if (shape->batch == 0 || n_tokens_max == 0) return IQ_OK;
+  if (!q || !workspace_dev || !out) return IQ_ERR_NULL;
+  if (!aligned16(q) || !aligned16(rot_dev) || !aligned16(workspace_dev) || !aligned16(out)) return IQ_ERR_ALIGN;
+  if ((stride_b & 7) || (stride_t & 7) || (stride_h & 7)) return IQ_ERR_ALIGN;
+
+  iq::TreeParams p = {};
+  p.k_codes = cache->k_codes;
+  p.k_scales = cache->k_scales;
+  p.v_codes = cache->v_codes;
+  p.v_scales = cache->v_scales;
+  p.q = static_cast<const __half*>(q);
+  p.qs_b = stride_b;
+  p.qs_t = stride_t;
+  p.qs_h = stride_h;
+  p.rot = rot_dev;
+  p.ctx_lens = ctx_lens_dev;
+  p.mask = tree_mask_dev;
+  p.n_tokens = n_tokens_dev;
+  p.n_tokens_max = n_tokens_max;
+  p.mask_words = (n_tokens_max + 31) / 32;
+  p.window = window;
+  p.sinks = sinks;
+  p.batch = shape->batch;
+  p.n_q_heads = shape->n_q_heads;
+  p.n_kv_heads = shape->n_kv_heads;
+  p.group = shape->n_q_heads / shape->n_kv_heads;
+  p.t_cap = shape->t_cap;
+  p.pm = page_map(cache, shape);
+  p.scale_f16 = cache->scales_fp16 ? 1 : 0;
+  p.bits = shape->bits;
+  for (int v = 0; v < 2; v++)
+    for (int i = 0; i < 1 << shape->bits; i++) {
+      const __half hv = __float2half_rn(grid8 ? (float)n8[v][i] : side_levels(codebook, v)[i]);
+      uint16_t bits;
+      std::memcpy(&bits, &hv, 2);
+      (v ? p.lut_v_lo : p.lut_lo)[i >> 2] |= (uint32_t)(bits & 0xFFu) << (8 * (i & 3));
+      (v ? p.lut_v_hi : p.lut_hi)[i >> 2] |= (uint32_t)(bits >> 8) << (8 * (i & 3));
+    }
+  p.lookup = iq::LOOKUP_CONST;
+  const double root_d = std::sqrt((double)shape->head_dim), sm = shape->sm_scale > 0.f ? (double)shape->sm_scale : 1.0 / root_d;
+  p.score_unit = (float)(sm * 1.4426950408889634 * delta[0] / root_d);
+  p.value_unit = (float)(delta[1] / root_d);
+  p.tile = w.tile;
+  p.tiles = w.tiles;
+  p.ctas = w.ctas;
+  uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
+  p.part_acc = reinterpret_cast<float*>(ws + w.part_acc);
+  p.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
+  p.item_info = reinterpret_cast<int2*>(ws + w.item_info);
+  p.out = out;
+  p.out_is_fp16 = out_is_fp16;
+  p.lse = lse_out;
+  p.status = status_dev;
+  return iq::launch_tree_attention(p, shape->head_dim, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+int iq_keep_rows(const iq_shape* shape, const iq_cache* cache, const int32_t* base_pos_dev, const int32_t* keep_dev,
+                 const int32_t* n_keep_dev, int32_t n_keep_max, uint32_t* status_dev, void* stream) {
+  int rc = check_shape(shape);
+  if (rc) return rc;
+  if (!base_pos_dev) return IQ_ERR_NULL;
+  if ((rc = check_cache(cache, shape))) return rc;
+  if (n_keep_max < 0) return IQ_ERR_SHAPE;
+  if (n_keep_max > IQ_KEEP_MAX_ROWS) return IQ_ERR_LIMIT;
+  if (shape->batch == 0 || n_keep_max == 0) return IQ_OK;
+  if (!keep_dev) return IQ_ERR_NULL;
+  const iq::KeepParams p = {cache_arrays(cache), page_map(cache, shape), base_pos_dev, keep_dev, n_keep_dev, n_keep_max, status_dev};
+  return iq::launch_keep_rows(p, shape->head_dim, shape->bits, shape->batch, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+size_t iq_page_pool_state_ints(int32_t num_pages) { return num_pages > 0 ? (size_t)iq::POOL_MARKS + ((size_t)num_pages + 31) / 32 : 0; }
+
+int iq_reserve_pages(const iq_page_pool* pool, const int32_t* first_row_dev, const int32_t* end_row_dev, uint32_t* status_dev, void* stream) {
+  const int rc = check_pool(pool);
+  if (rc) return rc;
+  if (!first_row_dev || !end_row_dev) return IQ_ERR_NULL;
+  if (pool->n_seqs == 0) return IQ_OK;
+  return iq::launch_reserve_pages(pool_params(pool, first_row_dev, end_row_dev, status_dev), static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+int iq_release_pages(const iq_page_pool* pool, const int32_t* first_row_dev, const int32_t* end_row_dev, uint32_t* status_dev, void* stream) {
+  const int rc = check_pool(pool);
+  if (rc) return rc;
+  if (!first_row_dev || !end_row_dev) return IQ_ERR_NULL;
+  if (pool->n_seqs == 0) return IQ_OK;
+  return iq::launch_release_pages(pool_params(pool, first_row_dev, end_row_dev, status_dev), static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+// The arrays of a pool of pages: like check_cache, without a sequence's capacity.
+static int check_pages(const iq_shape* shape, const iq_cache* c, int page_rows) {
+  if (!shape || !c || !c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales) return IQ_ERR_NULL;
+  if (!iq_row_bytes_bits(shape->head_dim, shape->bits) || shape->n_kv_heads <= 0) return IQ_ERR_SHAPE;
+  if (!aligned16(c->k_codes) || !aligned16(c->k_scales) || !aligned16(c->v_codes) || !aligned16(c->v_scales)) return IQ_ERR_ALIGN;
+  if ((long long)shape->n_kv_heads * (page_rows / 128) >= INT32_MAX) return IQ_ERR_LIMIT;  // a CTA to a block of a page
+  return IQ_OK;
+}
+
+int iq_fork_sequences(const iq_shape* shape, const iq_cache* cache, const iq_page_pool* pool, const int32_t* src_seq_dev,
+                      const int32_t* dst_seq_dev, const int32_t* n_rows_dev, int32_t n_forks, uint32_t* status_dev, void* stream) {
+  int rc = check_pool(pool);
+  if (rc) return rc;
+  if ((rc = check_pages(shape, cache, pool->page_rows))) return rc;
+  if (n_forks < 0) return IQ_ERR_SHAPE;
+  if (n_forks > IQ_MAX_FORKS) return IQ_ERR_LIMIT;
+  if (n_forks == 0) return IQ_OK;
+  if (!src_seq_dev || !dst_seq_dev || !n_rows_dev) return IQ_ERR_NULL;
+  iq::CopyParams p = {};
+  p.c = cache_arrays(cache);
+  p.n_kv_heads = shape->n_kv_heads;
+  p.row_bytes = (int)iq_row_bytes_bits(shape->head_dim, shape->bits);
+  p.pool = pool_params(pool, nullptr, nullptr, status_dev);
+  p.src = src_seq_dev;
+  p.dst = dst_seq_dev;
+  p.rows = n_rows_dev;
+  p.n = n_forks;
+  p.status = status_dev;
+  return iq::launch_fork_sequences(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+int iq_copy_pages(const iq_shape* shape, const iq_cache* cache, const int32_t* src_pages_dev, const int32_t* dst_pages_dev,
+                  int32_t n_pages, uint32_t* status_dev, void* stream) {
+  const int rc = check_pages(shape, cache, cache ? cache->page_rows : 0);
+  if (rc) return rc;
+  if (!cache->block_table_dev) return IQ_ERR_NULL;
+  if (cache->page_rows <= 0 || (cache->page_rows & 127) || cache->num_pages <= 0 || n_pages < 0) return IQ_ERR_SHAPE;
+  if (n_pages == 0) return IQ_OK;
+  if (!src_pages_dev || !dst_pages_dev) return IQ_ERR_NULL;
+  iq::CopyParams p = {};
+  p.c = cache_arrays(cache);
+  p.n_kv_heads = shape->n_kv_heads;
+  p.row_bytes = (int)iq_row_bytes_bits(shape->head_dim, shape->bits);
+  p.pool.page_rows = cache->page_rows;
+  p.pool.num_pages = cache->num_pages;
+  p.src = src_pages_dev;
+  p.dst = dst_pages_dev;
+  p.n = n_pages;
+  p.status = status_dev;
+  return iq::launch_copy_pages(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
 int32_t iq_suggest_splits(const iq_shape* shape, int32_t max_seq_len) {
   if (check_shape(shape) != IQ_OK || max_seq_len <= 0) return 1;
-  static int n_sm_cached[64] = {};
-  int dev = 0, n_sm = 148;
-  if (cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < 64) {
-    if (n_sm_cached[dev] == 0) {
-      int v = 0;
-      if (cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && v > 0) n_sm_cached[dev] = v;
-    }
-    if (n_sm_cached[dev] > 0) n_sm = n_sm_cached[dev];
-  }
+  const int n_sm = sm_count();
   const int group = shape->n_q_heads / shape->n_kv_heads;
   const long long items = (long long)(shape->batch > 0 ? shape->batch : 1) * shape->n_kv_heads * ((group + iq::DEC_HEADS - 1) / iq::DEC_HEADS);
   const long long ctas = (long long)n_sm * iq::decode_ctas_per_sm(shape->head_dim);

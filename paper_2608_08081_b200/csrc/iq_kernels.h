@@ -169,6 +169,92 @@ cudaError_t launch_reconstruct_rows(const ReconstructParams& p, int head_dim, in
 // The same on the tensor cores; false: the levels are not binary16 values times one factor per side.
 bool launch_reconstruct_tiles(const ReconstructParams& p, int head_dim, int batch, cudaStream_t stream, cudaError_t& e);
 
+// ---- tree attention: drafted tokens over the packed cache
+constexpr int TREE_SEG_COST = 1;  // what an item of the launch costs beside its blocks, in blocks (see tree_kernel)
+struct TreeParams {
+  const uint8_t* k_codes;
+  const float* k_scales;
+  const uint8_t* v_codes;
+  const float* v_scales;
+  const __half* q;
+  long long qs_b, qs_t, qs_h;  // strides of q, in elements
+  const float* rot;
+  const int32_t* ctx_lens;
+  const uint32_t* mask;      // [batch][n_tokens_max][mask_words], or nullptr: a chain
+  const int32_t* n_tokens;   // [batch], or nullptr
+  int n_tokens_max, mask_words, window, sinks;
+  int batch, n_q_heads, n_kv_heads, group, t_cap;
+  PageMap pm;
+  int scale_f16;
+  int bits;
+  // The levels as exact binary16 values times a unit per side (8-bit grid: the integers and delta; else the levels and 1): low and
+  // high bytes, 4 per register (2^bits / 4 registers used).
+  uint32_t lut_lo[4], lut_hi[4], lut_v_lo[4], lut_v_hi[4];
+  LookupConst lookup;
+  float score_unit;          // sm_scale log2(e) unit_K / sqrt(d): a score in units of log2 is this times scale times the product
+  float value_unit;          // unit_V / sqrt(d)
+  int tile, tiles;           // (token, head) pairs of an item, items per (sequence, KV head)
+  int ctas;                  // CTAs of the launch
+  // Workspace. A partial belongs to (item, CTA): its number is the item's plus the CTA's, both of which only grow along the launch's
+  // order of blocks.
+  float* part_acc;           // [items + ctas][tile][head_dim], rotated space
+  float* part_ml;            // [items + ctas][tile][2]: reference (log2 units), sum
+  int2* item_info;           // [items]: first CTA, number of CTAs
+  void* out;
+  int out_is_fp16;
+  float* lse;
+  uint32_t* status;
+};
+cudaError_t launch_tree_attention(const TreeParams& p, int head_dim, cudaStream_t stream);
+int tree_tile(int head_dim, int queries);  // tile for that many (token, head) pairs of a KV head
+int tree_ctas_per_sm(int head_dim, int tile);
+
+// ---- rows and pages of the cache
+struct CacheArrays {
+  uint8_t* k_codes;
+  float* k_scales;
+  uint8_t* v_codes;
+  float* v_scales;
+  int scale_f16;
+};
+struct KeepParams {
+  CacheArrays c;
+  PageMap pm;
+  const int32_t* base;
+  const int32_t* keep;
+  const int32_t* n_keep;
+  int n_keep_max;
+  uint32_t* status;
+};
+cudaError_t launch_keep_rows(const KeepParams& p, int head_dim, int bits, int batch, cudaStream_t stream);
+
+struct PoolParams {
+  int32_t* table;
+  int32_t* ref;
+  int32_t* free_list;
+  int32_t* state;  // [0] free pages, [1] arrivals (0 between launches), [4..] one bit per page (0 between launches)
+  int n_seqs, pages_per_seq, num_pages, page_rows;
+  const int32_t* first_row;
+  const int32_t* end_row;
+  uint32_t* status;
+};
+constexpr int POOL_MARKS = 4;  // where the bits start
+cudaError_t launch_reserve_pages(const PoolParams& p, cudaStream_t stream);
+cudaError_t launch_release_pages(const PoolParams& p, cudaStream_t stream);
+
+struct CopyParams {
+  CacheArrays c;
+  int n_kv_heads, row_bytes;  // packed bytes of a row, a side
+  PoolParams pool;            // (iq_copy_pages: only page_rows and num_pages)
+  const int32_t* src;
+  const int32_t* dst;
+  const int32_t* rows;        // forks: rows of the branch
+  int n;
+  uint32_t* status;
+};
+cudaError_t launch_fork_sequences(const CopyParams& p, cudaStream_t stream);
+cudaError_t launch_copy_pages(const CopyParams& p, cudaStream_t stream);
+
 // ---- rotation parameters
 cudaError_t launch_make_rotation(float* rot, int n_quats, uint64_t seed, cudaStream_t stream);
 cudaError_t launch_normalize_rotation(float* rot, int n_quats, cudaStream_t stream);
