@@ -7,20 +7,24 @@
 
 namespace iq {
 
-constexpr int TREE_COMPUTE = 256;                // two groups of four warps
-constexpr int TREE_THREADS = TREE_COMPUTE + 32;  // and the control warp
-constexpr float TREE_RAISE = 4.f;                // a score this far (log2) above its column's reference raises the references,
-constexpr float TREE_HEADROOM = 3.f;             // to this far above the block's maximum
-constexpr float TREE_P_UNIT = 1024.f;            // a probability of 1 of a row with the longest V scale as a binary16 operand
+// Warps 0 .. 3 take the softmax (a thread to a cache row), warps 4 .. 7 the dequantisation (a thread to a row of K, a coordinate of V), warp 8
+// loads and issues the products. (The three warps behind it only make the block whole warpgroups, as a change of register shares wants.)
+constexpr int TREE_THREADS = 384;
+constexpr float TREE_RAISE = 9.f;      // a score this far (log2) above its column's reference raises the references,
+constexpr float TREE_HEADROOM = 2.f;   // to this far above the block's maximum
+constexpr float TREE_V_ROOM = 2.f;     // and the reference of the V scales to at least this times their maximum
+// A probability of 1 of a row with the longest V scale as a binary16 operand: the largest, 2^9, stays below 2^15, and of one of 2^-20
+// the second term still holds 9 bits.
+constexpr float TREE_P_UNIT = 32.f;
 
 template <int N>
 struct TreeShared {
-  uint64_t full[4], k_ready, s_done, p_ready, o_done, drain;
+  uint64_t full[4], q_ready, k_ready, v_ready, s_done[2], p_ready, o_done, drain;  // s_done: of even and odd blocks
   uint32_t tmem, failed;
-  float neg_ref[N];                 // minus the reference of each column, log2 units
+  alignas(16) float neg_ref[N];     // minus the reference of each column, log2 units
   float l_factor[N], o_factor[N];   // of the last raise
   float warp_max[4][N];             // per quarter of the rows; at the end of a piece: sums
-  float warp_v[8], warp_q[8];
+  float warp_v[4], warp_q[8];
   int token[N];                     // the token of a column, counted from the tile's first
   TreeMasks<N> masks;
   long long scratch[TREE_THREADS / 32 + 2];
@@ -44,8 +48,13 @@ struct TreeLayout {
   static constexpr int STAGES = FIT < 4 ? FIT : 4;
   static constexpr int SMEM = FIXED + STAGES * STAGE_BYTES;
   // tensor memory: K tile (binary16, two to a column), V tile, scores, values
-  static constexpr int K_COL = 0, V_COL = D / 2, S_COL = V_COL + 64 * DJ, O_COL = S_COL + N;
   static constexpr int COLS = 512 / CTAS;
+  static constexpr int S_BUFS = D / 2 + 64 * DJ + (2 + DJ) * N <= COLS && STAGES >= 3 ? 2 : 1;
+  static constexpr int K_COL = 0, V_COL = D / 2, S_COL = V_COL + 64 * DJ, O_COL = S_COL + S_BUFS * N;
+  // Registers of a thread of the softmax, the dequantisation and the control warps where two CTAs share an SM: 80 each at launch, and a
+  // softmax thread holds N sums and up to 32 scores.
+  static constexpr bool SHARES = CTAS == 2;
+  static constexpr int SOFTMAX_REGS = N == 64 ? 136 : 120, DEQUANT_REGS = N == 64 ? 56 : 64, CONTROL_REGS = 240 - SOFTMAX_REGS - DEQUANT_REGS;
   static_assert(O_COL + DJ * N <= COLS, "tensor memory");
   static_assert(STAGES >= 2 && SMEM <= ROOM, "shared memory");
   // fp32 result, binary16 operands, M = 128; B_Q K-major, B_P MN-major
@@ -147,30 +156,132 @@ __device__ __forceinline__ void tree_dequant(const uint8_t* run, const uint32_t 
   }
 }
 
+// Sum over the warp's lanes of each of C values per lane, the lanes trading halves of their values: lane l ends with the sum of value
+// l / (32 / C).
+template <int C, int X = 16>
+__device__ __forceinline__ float tree_reduce(const float (&v)[C], int lane) {
+  if constexpr (C == 1) {
+    float r = v[0];
+#pragma unroll
+    for (int x = X; x > 0; x >>= 1) r += __shfl_xor_sync(FULL, r, x);
+    return r;
+  } else {
+    float h[C / 2];
+    const bool up = lane & X;
+#pragma unroll
+    for (int i = 0; i < C / 2; i++) h[i] = (up ? v[i + C / 2] : v[i]) + __shfl_xor_sync(FULL, up ? v[i] : v[i + C / 2], X);
+    return tree_reduce<C / 2, X / 2>(h, lane);
+  }
+}
+__device__ __forceinline__ float tree_warp_max(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+
+// The queries of a piece by W warps (this one is warp w): q~ = R q as two binary16 terms of the operand B_Q, times one power of two for
+// all of the tile (|q~_i| <= sqrt(d) max |q|). Returns that power's exponent. Two barriers `bar` of `threads`.
+template <int D, int BITS, int N>
+__device__ __forceinline__ int tree_queries(const TreeParams& p, TreeShared<N>& s, uint8_t* bq, const TreePiece& c, int q0, int nq, int w, int W,
+                                            int bar, int threads, int lane) {
+  using L = TreeLayout<D, BITS, N>;
+  constexpr int E = D / 32;
+  auto load = [&](int n, uint32_t (&raw)[E / 2]) {
+    if (n < nq) {
+      const int t = (q0 + n) / p.group, h = c.g * p.group + (q0 + n) - t * p.group;
+      const __half* q = p.q + c.b * p.qs_b + t * p.qs_t + h * p.qs_h + lane * E;
+      if constexpr (E == 4) {
+        const uint2 x = *reinterpret_cast<const uint2*>(q);
+        raw[0] = x.x; raw[1] = x.y;
+      } else {
+        const uint4 x = *reinterpret_cast<const uint4*>(q);
+        raw[0] = x.x; raw[1] = x.y; raw[E / 2 - 2] = x.z; raw[E / 2 - 1] = x.w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < E / 2; e++) raw[e] = 0u;
+    }
+  };
+  float qmax = 0.f;
+#pragma unroll 4
+  for (int n = w; n < nq; n += W) {
+    uint32_t raw[E / 2];
+    load(n, raw);
+#pragma unroll
+    for (int e = 0; e < E / 2; e++) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&raw[e]));
+      qmax = fmaxf(qmax, fminf(fmaxf(fabsf(f.x), fabsf(f.y)), 65504.f));  // (an infinite query is its own affair)
+    }
+  }
+  qmax = tree_warp_max(qmax);
+  if (lane == 0) s.warp_q[w] = qmax;
+  QuatPairs<E> qp;
+  qp.load(p.rot + (size_t)c.g * (D / 4) * 8, lane);
+  cta_bar_sync_n(bar, threads);
+  for (int k = 0; k < W; k++) qmax = fmaxf(qmax, s.warp_q[k]);
+  const int e2 = qmax > 0.f ? 13 - ((int)(__float_as_uint(qmax) >> 23) - 126 + 4) : 0;  // (sqrt(d) <= 2^4; at most 2^13)
+  const float scale = rsqrtf((float)D) * __uint_as_float((uint32_t)(127 + e2) << 23);
+#pragma unroll 2
+  for (int n = w; n < N; n += W) {
+    uint32_t raw[E / 2];
+    load(n, raw);
+    float x[E];
+#pragma unroll
+    for (int e = 0; e < E / 2; e++) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&raw[e]));
+      x[2 * e] = f.x; x[2 * e + 1] = f.y;
+    }
+    wht_warp<float, E>(x, lane);
+    qp.template apply<false>(x);
+    uint32_t hi[E / 2], lo[E / 2];
+#pragma unroll
+    for (int e = 0; e < E / 2; e++) {
+      const float a0 = x[2 * e] * scale, a1 = x[2 * e + 1] * scale;
+      hi[e] = pack_half2(a0, a1);
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[e]));
+      lo[e] = pack_half2(a0 - f.x, a1 - f.y);
+    }
+    uint8_t* const dst = bq + (n >> 3) * 128 + (n & 7) * 16 + (E == 4 ? (lane >> 1) * L::BQ_LBO + (lane & 1) * 8 : lane * L::BQ_LBO);
+    if constexpr (E == 4) {
+      *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(dst + L::BQ_TERM) = make_uint2(lo[0], lo[1]);
+    } else {
+      *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[E / 2 - 2], hi[E / 2 - 1]);
+      *reinterpret_cast<uint4*>(dst + L::BQ_TERM) = make_uint4(lo[0], lo[1], lo[E / 2 - 2], lo[E / 2 - 1]);
+    }
+  }
+  fence_proxy_async();
+  cta_bar_sync_n(bar, threads);
+  return e2;
+}
+
 template <int D, int BITS, int N>
 __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) tree_kernel(const __grid_constant__ TreeParams p) {
   using L = TreeLayout<D, BITS, N>;
-  constexpr int DJ = L::DJ, E = D / 32, NH = N / 2, NW = N / 8, NST = L::STAGES;
+  constexpr int DJ = L::DJ, NST = L::STAGES, SB = L::S_BUFS;
+  constexpr int CH = N < 32 ? N : 32;  // columns that a softmax thread has in registers at a time
   extern __shared__ __align__(1024) uint8_t smem[];
   TreeShared<N>& s = *reinterpret_cast<TreeShared<N>*>(smem);
   uint8_t* const bp = smem + L::SHARED;
   uint8_t* const bq = bp + 2 * L::BP_TERM;
   uint8_t* const stages = bq + 2 * L::BQ_TERM;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
-  const bool control = warp == TREE_COMPUTE / 32;
 
   if (tid == 0) {
     for (int i = 0; i < NST; i++) mbar_init(&s.full[i], 1);
+    mbar_init(&s.q_ready, 4);
     mbar_init(&s.k_ready, 4);
-    mbar_init(&s.s_done, 1);
-    mbar_init(&s.p_ready, 8);
+    mbar_init(&s.v_ready, 4);
+    mbar_init(&s.s_done[0], 1);
+    mbar_init(&s.s_done[1], 1);
+    mbar_init(&s.p_ready, 4);
     mbar_init(&s.o_done, 1);
     mbar_init(&s.drain, 1);
     s.failed = 0;
     fence_mbar_init();
     fence_proxy_async();
   }
-  if (control) {
+  if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "r"(L::COLS));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
   }
@@ -179,19 +290,22 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   const TreeRange range = tree_range<TREE_THREADS>(p, s.scratch);  // (its barriers also cover the set-up above)
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(FULL, s.tmem, 0);
+  const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the tensor-memory lanes
   TreeWalk walk;
   walk.start(range);
   TreePiece c;
   uint32_t i = 0;  // blocks of the CTA so far
 
-  if (control) {
+  if (warp >= 8) {
+    if constexpr (L::SHARES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::CONTROL_REGS));
+   if (warp == 8) {
     // ---- loads and products
     TreeWalk ahead;
     ahead.start(range);
     TreePiece a;
     bool more = ahead.next(p, range, a, false);
     int av = more ? a.lo : 0;
-    uint32_t loads = 0;
+    uint32_t loads = 0, pieces = 0;
     const uint32_t sc_bytes = p.scale_f16 ? 256u : 512u;
     const size_t sc_size = p.scale_f16 ? 2 : 4;
     auto load_next = [&]() {
@@ -215,20 +329,31 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
     };
     for (int st = 0; st < NST; st++) load_next();
     const uint64_t desc_q = smem_desc_mn(smem_u32(bq), L::BQ_LBO, 128), desc_p = smem_desc_mn(smem_u32(bp), L::BP_LBO, L::BP_SBO);
+    auto scores = [&](uint32_t n) {  // block n of the CTA
+      tree_wait(&s.k_ready, n & 1, &s.failed);
+      tc_fence_after();
+      if (!tree_failed(&s.failed) && elect_one()) {
+        const uint32_t d = tmem + L::S_COL + (SB == 2 ? (n & 1) * N : 0);
+#pragma unroll
+        for (int t = 0; t < 2; t++)
+#pragma unroll
+          for (int k = 0; k < D / 16; k++)
+            tc_mma_f16(d, tmem + L::K_COL + 8 * k, desc_q + ((t * L::BQ_TERM + 2 * k * L::BQ_LBO) >> 4), L::IDESC_Q, t || k);
+        tc_commit(&s.s_done[n & 1]);
+      }
+      __syncwarp();
+    };
     while (walk.next(p, range, c, false)) {
+      tree_wait(&s.q_ready, pieces & 1, &s.failed);
+      pieces++;
+      scores(i);
       for (int v = c.lo; v < c.hi; v++, i++) {
-        tree_wait(&s.k_ready, i & 1, &s.failed);
-        tc_fence_after();
-        if (!tree_failed(&s.failed) && elect_one()) {
-#pragma unroll
-          for (int t = 0; t < 2; t++)
-#pragma unroll
-            for (int k = 0; k < D / 16; k++)
-              tc_mma_f16(tmem + L::S_COL, tmem + L::K_COL + 8 * k, desc_q + ((t * L::BQ_TERM + 2 * k * L::BQ_LBO) >> 4), L::IDESC_Q, t || k);
-          tc_commit(&s.s_done);
-        }
-        __syncwarp();
+        // the scores of the next block: beside this one's softmax where there are two buffers for them, else behind it. (Those of the next
+        // piece wait for its queries, which wait for this piece's values.)
+        if (SB == 2 && v + 1 < c.hi) scores(i + 1);
         tree_wait(&s.p_ready, i & 1, &s.failed);
+        if (SB == 1 && v + 1 < c.hi) scores(i + 1);
+        tree_wait(&s.v_ready, i & 1, &s.failed);
         tc_fence_after();
         if (!tree_failed(&s.failed) && elect_one()) {
 #pragma unroll
@@ -247,173 +372,146 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
     }
     // every copy that was asked for has landed (where no wait gave up: at once)
     for (uint32_t n = loads > NST ? loads - NST : 0; n < loads; n++) mbar_wait_bounded(&s.full[n % NST], (n / NST) & 1, DEC_WAIT_LIMIT);
+   }
+  } else if (warp >= 4) {
+    // ---- dequantisation: K of block n + 1, then V of block n
+    if constexpr (L::SHARES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::DEQUANT_REGS));
+    const int r = tid & 127;
+    auto k_tile = [&](uint32_t n) {
+      tree_wait(&s.full[n % NST], (n / NST) & 1, &s.failed);
+      if (n > 0) tree_wait(&s.s_done[(n - 1) & 1], ((n - 1) >> 1) & 1, &s.failed);
+      tc_fence_after();
+      const uint8_t* const st = stages + (n % NST) * L::STAGE_BYTES;
+#pragma unroll
+      for (int j = 0; j < DJ; j++)
+        tree_dequant<BITS>(st + r * L::P + j * (16 * BITS), p.lut_lo, p.lut_hi, p.lookup, tmem + lanes + L::K_COL + 64 * j);
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s.k_ready);
+    };
+    auto v_tile = [&](uint32_t n) {
+      if (n > 0) tree_wait(&s.o_done, (n - 1) & 1, &s.failed);
+      tc_fence_after();
+      const uint8_t* const st = stages + (n % NST) * L::STAGE_BYTES + L::TILE_BYTES;
+#pragma unroll
+      for (int j = 0; j < DJ; j++)
+        tree_dequant<BITS>(st + (r + 128 * j) * (16 * BITS), p.lut_v_lo, p.lut_v_hi, p.lookup, tmem + lanes + L::V_COL + 64 * j);
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s.v_ready);
+    };
+    uint32_t blocks = 0;
+    if (walk.next(p, range, c, false)) {  // a hand with the first piece's queries
+      const int q0 = c.tile * N, nq = min(N, c.sq.tokens * p.group - q0);
+      tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, 8, 2, 256, lane);
+      k_tile(0);
+      do blocks += c.hi - c.lo;
+      while (walk.next(p, range, c, false));
+    }
+    for (; i < blocks; i++) {
+      if (i + 1 < blocks) k_tile(i + 1);
+      v_tile(i);
+    }
   } else {
-    const int wg = warp >> 2, r = tid & 127;
-    const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the tensor-memory lanes
-    const uint32_t s_col = tmem + lanes + L::S_COL + wg * NH, o_col = tmem + lanes + L::O_COL + wg * NH;
-    uint8_t* const bp_row = bp + wg * (NH / 8) * L::BP_SBO + (r & 7) * 16 + (r >> 3) * L::BP_LBO;
+    // ---- softmax
+    if constexpr (L::SHARES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
+    const int r = tid;
+    const uint32_t o_col = tmem + lanes + L::O_COL;
+    uint8_t* const bp_row = bp + (r & 7) * 16 + (r >> 3) * L::BP_LBO;
     while (walk.next(p, range, c, tid == 0)) {
-      // ---- the piece's queries: q~ = R q as two binary16 terms, one power of two for all of the tile. |q~_i| <= sqrt(d) max |q|.
       const int q0 = c.tile * N, nq = min(N, c.sq.tokens * p.group - q0), t0 = q0 / p.group;
-      cta_bar_sync_n(1, TREE_COMPUTE);  // the last piece's references have been read
-      uint32_t raw[NW][E / 2];
-      float qmax = 0.f;
-#pragma unroll
-      for (int k = 0; k < NW; k++) {
-        const int n = warp * NW + k;
-        if (n < nq) {
-          const int t = (q0 + n) / p.group, h = c.g * p.group + (q0 + n) - t * p.group;
-          const __half* q = p.q + c.b * p.qs_b + t * p.qs_t + h * p.qs_h + lane * E;
-          if constexpr (E == 4) {
-            const uint2 x = *reinterpret_cast<const uint2*>(q);
-            raw[k][0] = x.x; raw[k][1] = x.y;
-          } else {
-            const uint4 x = *reinterpret_cast<const uint4*>(q);
-            raw[k][0] = x.x; raw[k][1] = x.y; raw[k][E / 2 - 2] = x.z; raw[k][E / 2 - 1] = x.w;
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < E / 2; e++) raw[k][e] = 0u;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < NW; k++)
-#pragma unroll
-        for (int e = 0; e < E / 2; e++) {
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&raw[k][e]));
-          qmax = fmaxf(qmax, fminf(fmaxf(fabsf(f.x), fabsf(f.y)), 65504.f));  // (an infinite query is its own affair)
-        }
-      qmax = warp_max(qmax);
-      if (lane == 0) s.warp_q[warp] = qmax;
       if (tid == 0) s.masks.from_max = 0;
-      cta_bar_sync_n(1, TREE_COMPUTE);
-#pragma unroll
-      for (int k = 0; k < 8; k++) qmax = fmaxf(qmax, s.warp_q[k]);
-      // the power of two that brings sqrt(d) max |q| to at most 2^13
-      const int e2 = qmax > 0.f ? (int)(__float_as_uint(qmax) >> 23) - 126 + 4 : 13;  // (sqrt(d) <= 2^4)
-      const float q_scale = __uint_as_float((uint32_t)(127 + 13 - e2) << 23), score_unit = p.score_unit * __uint_as_float((uint32_t)(127 - 13 + e2) << 23);
-      tree_masks(p, s.masks, c.b, c.sq, t0, (q0 + nq - 1) / p.group - t0 + 1, tid, TREE_COMPUTE);
+      cta_bar_sync_n(1, 128);  // the last piece's references have been read
+      tree_masks(p, s.masks, c.b, c.sq, t0, (q0 + nq - 1) / p.group - t0 + 1, tid, 128);
       if (tid < N) {
         s.neg_ref[tid] = 1e30f;
         s.token[tid] = (q0 + tid) / p.group - t0;
       }
-      {
-        QuatPairs<E> qp;
-        qp.load(p.rot + (size_t)c.g * (D / 4) * 8, lane);
-#pragma unroll
-        for (int k = 0; k < NW; k++) {
-          const int n = warp * NW + k;
-          float x[E];
-#pragma unroll
-          for (int e = 0; e < E / 2; e++) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&raw[k][e]));
-            x[2 * e] = f.x; x[2 * e + 1] = f.y;
-          }
-          wht_warp<float, E>(x, lane);
-          qp.template apply<false>(x);
-          uint32_t hi[E / 2], lo[E / 2];
-#pragma unroll
-          for (int e = 0; e < E / 2; e++) {
-            const float a0 = x[2 * e] * (rsqrtf((float)D) * q_scale), a1 = x[2 * e + 1] * (rsqrtf((float)D) * q_scale);
-            hi[e] = pack_half2(a0, a1);
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[e]));
-            lo[e] = pack_half2(a0 - f.x, a1 - f.y);
-          }
-          uint8_t* const dst = bq + (n >> 3) * 128 + (n & 7) * 16 + (E == 4 ? (lane >> 1) * L::BQ_LBO + (lane & 1) * 8 : lane * L::BQ_LBO);
-          if constexpr (E == 4) {
-            *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
-            *reinterpret_cast<uint2*>(dst + L::BQ_TERM) = make_uint2(lo[0], lo[1]);
-          } else {
-            *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[E / 2 - 2], hi[E / 2 - 1]);
-            *reinterpret_cast<uint4*>(dst + L::BQ_TERM) = make_uint4(lo[0], lo[1], lo[E / 2 - 2], lo[E / 2 - 1]);
-          }
-        }
-      }
-      fence_proxy_async();
-      cta_bar_sync_n(1, TREE_COMPUTE);
+      const int e2 = i == 0 ? tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, 8, 2, 256, lane)
+                            : tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, 4, 1, 128, lane);
+      if (lane == 0) mbar_arrive(&s.q_ready);
+      const float score_unit = p.score_unit * __uint_as_float((uint32_t)(127 - e2) << 23);
 
-      float l[NH];
+      float l[N];
 #pragma unroll
-      for (int n = 0; n < NH; n++) l[n] = 0.f;
+      for (int n = 0; n < N; n++) l[n] = 0.f;
       float v_ref = 0.f;  // a power of two at least as large as every V scale so far
       for (int v = c.lo; v < c.hi; v++, i++) {
-        const uint8_t* const st = stages + (i % NST) * L::STAGE_BYTES;
+        const uint8_t* const st = stages + (i % NST) * L::STAGE_BYTES + 2 * L::TILE_BYTES;
+        const uint32_t s_col = tmem + lanes + L::S_COL + (SB == 2 ? (i & 1) * N : 0);
         tree_wait(&s.full[i % NST], (i / NST) & 1, &s.failed);
-        if (wg == 0) {
-#pragma unroll
-          for (int j = 0; j < DJ; j++)
-            tree_dequant<BITS>(st + r * L::P + j * (16 * BITS), p.lut_lo, p.lut_hi, p.lookup, tmem + lanes + L::K_COL + 64 * j);
-          tc_wait_st();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&s.k_ready);
-        } else {
-          if (i > 0) tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
-          tc_fence_after();
-#pragma unroll
-          for (int j = 0; j < DJ; j++)
-            tree_dequant<BITS>(st + L::TILE_BYTES + (r + 128 * j) * (16 * BITS), p.lut_v_lo, p.lut_v_hi, p.lookup, tmem + lanes + L::V_COL + 64 * j);
-          tc_wait_st();
-        }
-        const float ks = load_scale(st + 2 * L::TILE_BYTES, r, p.scale_f16) * score_unit;
-        float vs = load_scale(st + 2 * L::TILE_BYTES + 512, r, p.scale_f16);
-        const int row0 = c.sq.block(v) * 128, row = row0 + r;
+        const float ks = load_scale(st, r, p.scale_f16) * score_unit;
+        float vs = load_scale(st + 512, r, p.scale_f16);
+        const int row0 = c.sq.block(v) * 128;
         const bool masked = row0 + 128 > c.sq.ctx || !(row0 >= s.masks.from_max || row0 + 128 <= p.sinks);
-        tree_wait(&s.s_done, i & 1, &s.failed);
+        uint32_t sees[(N + 31) / 32];  // bit n: column n sees the row
+        if (masked) {
+          bool any = false;
+#pragma unroll 1
+          for (int w = 0; w < (N + 31) / 32; w++) {
+            uint32_t bits = 0;
+#pragma unroll 1
+            for (int n = 0; n < 32 && 32 * w + n < nq; n++)
+              if (tree_sees(s.masks, s.token[32 * w + n], row0 + r, c.sq.ctx, c.sq.rows, p.sinks)) bits |= 1u << n;
+            any = any || bits;
+            if (w == 0) sees[0] = bits;
+            else sees[(N + 31) / 32 - 1] = bits;
+          }
+          if (!any) vs = 0.f;
+        } else {
+#pragma unroll
+          for (int w = 0; w < (N + 31) / 32; w++) sees[w] = 0xFFFFFFFFu;
+        }
+        const float vs_fin = vs < INFINITY ? vs : 0.f;  // (an infinite or undefined scale is its own row's affair)
+        tree_wait(&s.s_done[i & 1], (i >> 1) & 1, &s.failed);
         tc_fence_after();
 
         // scores relative to the references; -inf where the token does not see the row
-        float t[NH];
-        auto scores = [&]() {
-          tree_ld<NH>(s_col, t);
-          const float4* ref = reinterpret_cast<const float4*>(s.neg_ref + wg * NH);
+        float t[CH];
+        auto relative = [&](int n0) {
+          tree_ld<CH>(s_col + n0, t);
+          const float4* ref = reinterpret_cast<const float4*>(s.neg_ref + n0);
 #pragma unroll
-          for (int n = 0; n < NH; n += 4) {
+          for (int n = 0; n < CH; n += 4) {
             const float4 f = ref[n / 4];
-            t[n] = fmaf(t[n], ks, f.x);
-            t[n + 1] = fmaf(t[n + 1], ks, f.y);
-            t[n + 2] = fmaf(t[n + 2], ks, f.z);
-            t[n + 3] = fmaf(t[n + 3], ks, f.w);
+            const F32x2 a = fma2(f32x2(t[n], t[n + 1]), f32x2(ks, ks), f32x2(f.x, f.y)), b = fma2(f32x2(t[n + 2], t[n + 3]), f32x2(ks, ks), f32x2(f.z, f.w));
+            t[n] = a.lo(); t[n + 1] = a.hi(); t[n + 2] = b.lo(); t[n + 3] = b.hi();
+          }
+          if (masked) {
+#pragma unroll
+            for (int n = 0; n < CH; n++)
+              if (!(sees[n0 / 32] >> (n % 32) & 1u)) t[n] = -INFINITY;
           }
         };
-        uint32_t sees = 0xFFFFFFFFu;  // bit n: column n of this thread sees the row
-        scores();
-        if (masked) {
-          sees = 0;
+        float top = -INFINITY;
 #pragma unroll
-          for (int n = 0; n < NH; n++)
-            if (wg * NH + n < nq && tree_sees(s.masks, s.token[wg * NH + n], row, c.sq.ctx, c.sq.rows, p.sinks)) sees |= 1u << n;
+        for (int n0 = 0; n0 < N; n0 += CH) {
+          relative(n0);
 #pragma unroll
-          for (int n = 0; n < NH; n++)
-            if (!(sees >> n & 1u)) t[n] = -INFINITY;
-          if (!sees) vs = 0.f;
+          for (int n = 0; n < CH; n += 2) top = max3f(top, t[n], t[n + 1]);
         }
-        float top = t[0];
-#pragma unroll
-        for (int n = 1; n + 1 < NH; n += 2) top = max3f(top, t[n], t[n + 1]);
-        top = fmaxf(top, t[NH - 1]);
-        const float vs_fin = vs < INFINITY ? vs : 0.f;  // (an infinite or undefined scale is its own row's affair)
-        if (cta_bar_or_n(1, TREE_COMPUTE, top > TREE_RAISE || vs_fin > v_ref)) {
+        if (cta_bar_or_n(1, 128, top > TREE_RAISE || vs_fin > v_ref)) {
           // ---- new references: the maximum of each column over the block, and of the V scales
-          const float vm = warp_max(vs_fin);
+          const float vm = tree_warp_max(vs_fin);
           if (lane == 0) s.warp_v[warp] = vm;
-#pragma unroll
-          for (int n0 = 0; n0 < NH; n0 += 8) {
+#pragma unroll 1
+          for (int n0 = 0; n0 < N; n0 += 8) {
             float z[8];
             tree_ld<8>(s_col + n0, z);
+            const uint32_t on = (n0 < 32 ? sees[0] : sees[(N + 31) / 32 - 1]) >> (n0 & 31);
 #pragma unroll
             for (int n = 0; n < 8; n++) {
-              const float m = warp_max((sees >> (n0 + n) & 1u) ? z[n] * ks : -3e38f);
-              if (lane == 0) s.warp_max[warp & 3][wg * NH + n0 + n] = m;
+              const float m = tree_warp_max((on >> n & 1u) ? z[n] * ks : -3e38f);
+              if (lane == 0) s.warp_max[warp][n0 + n] = m;
             }
           }
-          cta_bar_sync_n(1, TREE_COMPUTE);
-          float v_new = v_ref;
-#pragma unroll
-          for (int k = 0; k < 8; k++) v_new = fmaxf(v_new, s.warp_v[k]);
-          // the power of two at or above it, not below 2^-100
-          v_new = v_new > v_ref ? fmaxf(__uint_as_float((__float_as_uint(v_new) + 0x7FFFFFu) & 0x7F800000u), 7.888609e-31f) : v_ref;
-          if (!(v_new < INFINITY)) v_new = 1.7014118e38f;  // 2^127
+          cta_bar_sync_n(1, 128);
+          float v_new = fmaxf(fmaxf(s.warp_v[0], s.warp_v[1]), fmaxf(s.warp_v[2], s.warp_v[3]));
+          // the power of two at or above it, with room, within 2^-100 .. 2^127
+          v_new = v_new > v_ref ? fmaxf(__uint_as_float((__float_as_uint(v_new) + 0x7FFFFFu) & 0x7F800000u) * TREE_V_ROOM, 7.888609e-31f) : v_ref;
+          if (!(v_new < INFINITY)) v_new = 1.7014118e38f;
           if (tid < N) {
             const float m = fmaxf(fmaxf(s.warp_max[0][tid], s.warp_max[1][tid]), fmaxf(s.warp_max[2][tid], s.warp_max[3][tid]));
             const float old = -s.neg_ref[tid];
@@ -423,46 +521,43 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
             s.l_factor[tid] = f;
             s.o_factor[tid] = v_new > 0.f ? f * (v_ref / v_new) : f;
           }
-          cta_bar_sync_n(1, TREE_COMPUTE);
+          cta_bar_sync_n(1, 128);
           v_ref = v_new;
 #pragma unroll
-          for (int n = 0; n < NH; n++) l[n] *= s.l_factor[wg * NH + n];
+          for (int n = 0; n < N; n++) l[n] *= s.l_factor[n];
           if (v > c.lo) {
             tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
             tc_fence_after();
 #pragma unroll 1
-            for (int j = 0; j < DJ; j++)
-#pragma unroll 1
-              for (int n0 = 0; n0 < NH; n0 += 8) {
-                float o[8];
-                tree_ld<8>(o_col + j * N + n0, o);
+            for (int n0 = 0; n0 < DJ * N; n0 += 8) {
+              float o[8];
+              tree_ld<8>(o_col + n0, o);
 #pragma unroll
-                for (int n = 0; n < 8; n++) o[n] *= s.o_factor[wg * NH + n0 + n];
-                tree_st8(o_col + j * N + n0, o);
-              }
+              for (int n = 0; n < 8; n++) o[n] *= s.o_factor[(n0 & (N - 1)) + n];
+              tree_st8(o_col + n0, o);
+            }
             tc_wait_st();
           }
-          scores();
-#pragma unroll
-          for (int n = 0; n < NH; n++)
-            if (!(sees >> n & 1u)) t[n] = -INFINITY;
+          if (CH == N) relative(0);
         }
         // ---- probabilities, and times the V scale as two binary16 terms of the operand B_P
-        if (wg == 0 && i > 0) tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
+        if (i > 0) tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
         const float vn = v_ref > 0.f ? vs * (TREE_P_UNIT / v_ref) : 0.f;
 #pragma unroll
-        for (int n0 = 0; n0 < NH; n0 += 8) {
+        for (int n0 = 0; n0 < N; n0 += 8) {
+          if (CH < N && n0 % CH == 0) relative(n0);
           uint32_t hi[4], lo[4];
 #pragma unroll
           for (int k = 0; k < 4; k++) {
             const int n = n0 + 2 * k;
-            const float p0 = ex2f(t[n]), p1 = ex2f(t[n + 1]);
-            l[n] += p0;
-            l[n + 1] += p1;
-            float x0 = p0 * vn, x1 = p1 * vn;
+            const float p0 = ex2f(t[n % CH]), p1 = ex2f(t[n % CH + 1]);
+            const F32x2 ls = add2(f32x2(l[n], l[n + 1]), f32x2(p0, p1)), x = mul2(f32x2(p0, p1), f32x2(vn, vn));
+            l[n] = ls.lo();
+            l[n + 1] = ls.hi();
+            float x0 = x.lo(), x1 = x.hi();
             if (masked) {  // (0 times an infinite scale)
-              if (!(sees >> n & 1u)) x0 = 0.f;
-              if (!(sees >> (n + 1) & 1u)) x1 = 0.f;
+              if (!(sees[n / 32] >> (n % 32) & 1u)) x0 = 0.f;
+              if (!(sees[n / 32] >> (n % 32 + 1) & 1u)) x1 = 0.f;
             }
             hi[k] = pack_half2(x0, x1);
             const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[k]));
@@ -477,17 +572,18 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.p_ready);
       }
-      // ---- the piece's partial
+      // ---- the piece's partial. Sums over the rows: in the warp, then over the four warps, in a fixed order.
       const size_t part = (walk.item(p, c) + blockIdx.x) * N;
-      // sums over the rows: lane by lane in the warp, then over its four warps, in a fixed order
+      cta_bar_sync_n(1, 128);  // (warp_max of a raise has been read)
 #pragma unroll
-      for (int n = 0; n < NH; n++) {
-        float x = l[n];
+      for (int n0 = 0; n0 < N; n0 += CH) {
+        float x[CH];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(FULL, x, o);
-        if (lane == 0) s.warp_max[warp & 3][wg * NH + n] = x;
+        for (int n = 0; n < CH; n++) x[n] = l[n0 + n];
+        const float sum = tree_reduce<CH>(x, lane);
+        if (lane % (32 / CH) == 0) s.warp_max[warp][n0 + lane / (32 / CH)] = sum;
       }
-      cta_bar_sync_n(1, TREE_COMPUTE);
+      cta_bar_sync_n(1, 128);
       if (tid < nq) {
         const float sum = (s.warp_max[0][tid] + s.warp_max[1][tid]) + (s.warp_max[2][tid] + s.warp_max[3][tid]);
         *reinterpret_cast<float2*>(p.part_ml + 2 * (part + tid)) = make_float2(-s.neg_ref[tid], sum);
@@ -498,14 +594,13 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
 #pragma unroll 1
       for (int j = 0; j < DJ; j++)
 #pragma unroll 1
-        for (int n0 = 0; n0 < NH; n0 += 8) {
-          if (wg * NH + n0 >= nq) break;
+        for (int n0 = 0; n0 < nq; n0 += 8) {
           float o[8];
           tree_ld<8>(o_col + j * N + n0, o);
-          float* const dst = p.part_acc + (part + wg * NH + n0) * D + 128 * j + r;
+          float* const dst = p.part_acc + (part + n0) * D + 128 * j + r;
 #pragma unroll
           for (int n = 0; n < 8; n++)
-            if (wg * NH + n0 + n < nq) dst[n * D] = o[n] * unit;
+            if (n0 + n < nq) dst[n * D] = o[n] * unit;
         }
       tc_fence_before();
     }
@@ -515,7 +610,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   __syncthreads();
   if (*(volatile uint32_t*)&s.failed) {  // (nobody writes it any more)
     if (tid == 0 && p.status) atomicOr(&p.status[0], IQ_STATUS_WAIT_TIMEOUT);
-    if (control) {  // MMAs may still be running: they are waited for, with a limit, before the tensor memory goes
+    if (warp == 8) {  // MMAs may still be running: they are waited for, with a limit, before the tensor memory goes
       if (elect_one()) tc_commit(&s.drain);
       __syncwarp();
       mbar_wait_bounded(&s.drain, 0u, DEC_WAIT_LIMIT);
@@ -524,7 +619,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   }
   tc_fence_before();
   __syncthreads();
-  if (control) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS));
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS));
 }
 
 template <int D, int BITS, int N>
