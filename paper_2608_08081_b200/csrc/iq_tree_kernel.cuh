@@ -7,9 +7,11 @@
 
 namespace iq {
 
-// Warps 0 .. 3 take the softmax (a thread to a cache row), warps 4 .. 7 the dequantisation (a thread to a row of K, a coordinate of V), warp 8
-// loads and issues the products. (The three warps behind it only make the block whole warpgroups, as a change of register shares wants.)
-constexpr int TREE_THREADS = 384;
+// Four warpgroups: warps 0 .. 3 take the softmax (a thread to a cache row), 4 .. 7 dequantise K (a thread to a row), 8 .. 11 V (a thread to
+// a coordinate), and of the last four one issues the score products, one the value products, one the loads (the fourth is there because
+// register shares change by whole warpgroups).
+constexpr int TREE_THREADS = 512;
+constexpr int TREE_QK_WARP = 12, TREE_PV_WARP = 13, TREE_LOAD_WARP = 14;
 constexpr float TREE_RAISE = 9.f;      // a score this far (log2) above its column's reference raises the references,
 constexpr float TREE_HEADROOM = 2.f;   // to this far above the block's maximum
 constexpr float TREE_V_ROOM = 2.f;     // and the reference of the V scales to at least this times their maximum
@@ -19,7 +21,7 @@ constexpr float TREE_P_UNIT = 32.f;
 
 template <int N>
 struct TreeShared {
-  uint64_t full[4], q_ready, k_ready, v_ready, s_done[2], p_ready, o_done, drain;  // s_done: of even and odd blocks
+  uint64_t full[4], q_ready, k_ready, v_ready, s_done[2], s_read[2], p_ready, o_done, taken[4], drain;  // s_done, s_read: of even and odd blocks
   uint32_t tmem, failed;
   alignas(16) float neg_ref[N];     // minus the reference of each column, log2 units
   float l_factor[N], o_factor[N];   // of the last raise
@@ -51,10 +53,10 @@ struct TreeLayout {
   static constexpr int COLS = 512 / CTAS;
   static constexpr int S_BUFS = D / 2 + 64 * DJ + (2 + DJ) * N <= COLS && STAGES >= 3 ? 2 : 1;
   static constexpr int K_COL = 0, V_COL = D / 2, S_COL = V_COL + 64 * DJ, O_COL = S_COL + S_BUFS * N;
-  // Registers of a thread of the softmax, the dequantisation and the control warps where two CTAs share an SM: 80 each at launch, and a
-  // softmax thread holds N sums and up to 32 scores.
-  static constexpr bool SHARES = CTAS == 2;
-  static constexpr int SOFTMAX_REGS = N == 64 ? 136 : 120, DEQUANT_REGS = N == 64 ? 56 : 64, CONTROL_REGS = 240 - SOFTMAX_REGS - DEQUANT_REGS;
+  // Registers of a thread: at launch 64 where two CTAs share an SM, else 128, four times that over the four groups. A softmax thread holds N
+  // sums and up to 32 scores.
+  static constexpr int SOFTMAX_REGS = CTAS == 1 ? 200 : N == 64 ? 136 : N == 32 ? 112 : 88;
+  static constexpr int OTHER_REGS = (512 / CTAS - SOFTMAX_REGS) / 3 / 8 * 8;
   static_assert(O_COL + DJ * N <= COLS, "tensor memory");
   static_assert(STAGES >= 2 && SMEM <= ROOM, "shared memory");
   // fp32 result, binary16 operands, M = 128; B_Q K-major, B_P MN-major
@@ -105,7 +107,7 @@ struct TreeWalk {
 // goes on through the same loops and barriers over whatever is there, so that the CTA ends together.
 __device__ __forceinline__ void tree_wait(uint64_t* bar, uint32_t parity, uint32_t* failed) {
   for (uint32_t i = 0; !mbar_try_wait(bar, parity); i++)
-    if (*(volatile uint32_t*)failed || i >= DEC_WAIT_LIMIT) { *(volatile uint32_t*)failed = 1; break; }
+    if (i >= DEC_WAIT_LIMIT || *(volatile uint32_t*)failed) { *(volatile uint32_t*)failed = 1; break; }
   __syncwarp();
 }
 
@@ -268,20 +270,25 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
 
   if (tid == 0) {
-    for (int i = 0; i < NST; i++) mbar_init(&s.full[i], 1);
+    for (int i = 0; i < NST; i++) {
+      mbar_init(&s.full[i], 1);
+      mbar_init(&s.taken[i], 1);
+    }
     mbar_init(&s.q_ready, 4);
     mbar_init(&s.k_ready, 4);
     mbar_init(&s.v_ready, 4);
     mbar_init(&s.s_done[0], 1);
     mbar_init(&s.s_done[1], 1);
+    mbar_init(&s.s_read[0], 4);
+    mbar_init(&s.s_read[1], 4);
     mbar_init(&s.p_ready, 4);
     mbar_init(&s.o_done, 1);
-    mbar_init(&s.drain, 1);
+    mbar_init(&s.drain, 2);
     s.failed = 0;
     fence_mbar_init();
     fence_proxy_async();
   }
-  if (warp == 8) {
+  if (warp == 12) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "r"(L::COLS));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
   }
@@ -296,127 +303,122 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   TreePiece c;
   uint32_t i = 0;  // blocks of the CTA so far
 
-  if (warp >= 8) {
-    if constexpr (L::SHARES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::CONTROL_REGS));
-   if (warp == 8) {
-    // ---- loads and products
-    TreeWalk ahead;
-    ahead.start(range);
-    TreePiece a;
-    bool more = ahead.next(p, range, a, false);
-    int av = more ? a.lo : 0;
-    uint32_t loads = 0, pieces = 0;
-    const uint32_t sc_bytes = p.scale_f16 ? 256u : 512u;
-    const size_t sc_size = p.scale_f16 ? 2 : 4;
-    auto load_next = [&]() {
-      if (!more || tree_failed(&s.failed)) return;
-      const int st = loads % NST;
-      const size_t row0 = cache_row(p.pm, a.b, a.g, (long long)a.sq.block(av) * 128, lane == 0 ? p.status : nullptr);
-      if (elect_one()) {
-        uint8_t* const dst = stages + st * L::STAGE_BYTES;
-        mbar_expect_tx(&s.full[st], 2 * L::TILE_BYTES + 2 * sc_bytes);
-        bulk_g2s(dst, p.k_codes + row0 * L::P, L::TILE_BYTES, &s.full[st]);
-        bulk_g2s(dst + 2 * L::TILE_BYTES, reinterpret_cast<const uint8_t*>(p.k_scales) + row0 * sc_size, sc_bytes, &s.full[st]);
-        bulk_g2s(dst + L::TILE_BYTES, p.v_codes + row0 * L::P, L::TILE_BYTES, &s.full[st]);
-        bulk_g2s(dst + 2 * L::TILE_BYTES + 512, reinterpret_cast<const uint8_t*>(p.v_scales) + row0 * sc_size, sc_bytes, &s.full[st]);
+  if (warp >= 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
+    if (warp == TREE_LOAD_WARP) {
+      // ---- loads: block n into stage n % NST, when the values of block n - NST have been taken (and with them its scores)
+      const uint32_t sc_bytes = p.scale_f16 ? 256u : 512u;
+      const size_t sc_size = p.scale_f16 ? 2 : 4;
+      while (walk.next(p, range, c, false)) {
+        for (int v = c.lo; v < c.hi && !tree_failed(&s.failed); v++, i++) {
+          const int st = i % NST;
+          const size_t row0 = cache_row(p.pm, c.b, c.g, (long long)c.sq.block(v) * 128, lane == 0 ? p.status : nullptr);
+          if (i >= NST) tree_wait(&s.taken[st], (i / NST - 1) & 1, &s.failed);
+          if (elect_one()) {
+            uint8_t* const dst = stages + st * L::STAGE_BYTES;
+            mbar_expect_tx(&s.full[st], 2 * L::TILE_BYTES + 2 * sc_bytes);
+            bulk_g2s(dst, p.k_codes + row0 * L::P, L::TILE_BYTES, &s.full[st]);
+            bulk_g2s(dst + 2 * L::TILE_BYTES, reinterpret_cast<const uint8_t*>(p.k_scales) + row0 * sc_size, sc_bytes, &s.full[st]);
+            bulk_g2s(dst + L::TILE_BYTES, p.v_codes + row0 * L::P, L::TILE_BYTES, &s.full[st]);
+            bulk_g2s(dst + 2 * L::TILE_BYTES + 512, reinterpret_cast<const uint8_t*>(p.v_scales) + row0 * sc_size, sc_bytes, &s.full[st]);
+          }
+          __syncwarp();
+        }
       }
-      __syncwarp();
-      loads++;
-      if (++av == a.hi) {
-        more = ahead.next(p, range, a, false);
-        av = a.lo;
-      }
-    };
-    for (int st = 0; st < NST; st++) load_next();
-    const uint64_t desc_q = smem_desc_mn(smem_u32(bq), L::BQ_LBO, 128), desc_p = smem_desc_mn(smem_u32(bp), L::BP_LBO, L::BP_SBO);
-    auto scores = [&](uint32_t n) {  // block n of the CTA
-      tree_wait(&s.k_ready, n & 1, &s.failed);
-      tc_fence_after();
-      if (!tree_failed(&s.failed) && elect_one()) {
-        const uint32_t d = tmem + L::S_COL + (SB == 2 ? (n & 1) * N : 0);
-#pragma unroll
-        for (int t = 0; t < 2; t++)
-#pragma unroll
-          for (int k = 0; k < D / 16; k++)
-            tc_mma_f16(d, tmem + L::K_COL + 8 * k, desc_q + ((t * L::BQ_TERM + 2 * k * L::BQ_LBO) >> 4), L::IDESC_Q, t || k);
-        tc_commit(&s.s_done[n & 1]);
-      }
-      __syncwarp();
-    };
-    while (walk.next(p, range, c, false)) {
-      tree_wait(&s.q_ready, pieces & 1, &s.failed);
-      pieces++;
-      scores(i);
-      for (int v = c.lo; v < c.hi; v++, i++) {
-        // the scores of the next block: beside this one's softmax where there are two buffers for them, else behind it. (Those of the next
-        // piece wait for its queries, which wait for this piece's values.)
-        if (SB == 2 && v + 1 < c.hi) scores(i + 1);
-        tree_wait(&s.p_ready, i & 1, &s.failed);
-        if (SB == 1 && v + 1 < c.hi) scores(i + 1);
-        tree_wait(&s.v_ready, i & 1, &s.failed);
-        tc_fence_after();
-        if (!tree_failed(&s.failed) && elect_one()) {
-#pragma unroll
-          for (int j = 0; j < DJ; j++)
-#pragma unroll
-            for (int t = 0; t < 2; t++)
+      // every copy that was asked for has landed (where no wait gave up: at once)
+      for (uint32_t n = i > NST ? i - NST : 0; n < i; n++) mbar_wait_bounded(&s.full[n % NST], (n / NST) & 1, DEC_WAIT_LIMIT);
+    } else if (warp == TREE_QK_WARP) {
+      // ---- score products, one block ahead of the softmax where there are two buffers for them. (Those of a piece's first block wait for
+      // its queries, which wait for the piece before.)
+      const uint64_t desc = smem_desc_mn(smem_u32(bq), L::BQ_LBO, 128);
+      uint32_t pieces = 0;
+      while (walk.next(p, range, c, false)) {
+        tree_wait(&s.q_ready, pieces & 1, &s.failed);
+        pieces++;
+        for (int v = c.lo; v < c.hi; v++, i++) {
+          if (i >= SB) tree_wait(&s.s_read[(i - SB) & 1], ((i - SB) >> 1) & 1, &s.failed);
+          tree_wait(&s.k_ready, i & 1, &s.failed);
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t d = tmem + L::S_COL + (SB == 2 ? (i & 1) * N : 0);
+#pragma unroll 1
+            for (int t = 0; t < 2 * DJ; t++) {  // halves of the coordinates, terms of q~
+              const uint32_t at = (t & (DJ - 1)) * 16 * L::BQ_LBO + t / DJ * L::BQ_TERM;
 #pragma unroll
               for (int k = 0; k < 8; k++)
-                tc_mma_f16(tmem + L::O_COL + j * N, tmem + L::V_COL + 64 * j + 8 * k, desc_p + ((t * L::BP_TERM + 2 * k * L::BP_LBO) >> 4), L::IDESC_P,
-                           v > c.lo || t || k);
-          tc_commit(&s.o_done);
+                tc_mma_f16(d, tmem + L::K_COL + (t & (DJ - 1)) * 64 + 8 * k, desc + ((at + 2 * k * L::BQ_LBO) >> 4), L::IDESC_Q, t || k);
+            }
+            tc_commit(&s.s_done[i & 1]);
+          }
+          __syncwarp();
         }
-        __syncwarp();
-        load_next();
+      }
+    } else if (warp == TREE_PV_WARP) {
+      // ---- value products
+      const uint64_t desc = smem_desc_mn(smem_u32(bp), L::BP_LBO, L::BP_SBO);
+      while (walk.next(p, range, c, false)) {
+        for (int v = c.lo; v < c.hi; v++, i++) {
+          tree_wait(&s.v_ready, i & 1, &s.failed);
+          tree_wait(&s.p_ready, i & 1, &s.failed);
+          tc_fence_after();
+          if (elect_one()) {
+            mbar_arrive(&s.taken[i % NST]);
+#pragma unroll 1
+            for (int t = 0; t < 2 * DJ; t++) {  // terms of the probabilities, halves of the coordinates
+              const uint32_t j = t >> 1, at = (t & 1) * L::BP_TERM;
+#pragma unroll
+              for (int k = 0; k < 8; k++)
+                tc_mma_f16(tmem + L::O_COL + j * N, tmem + L::V_COL + 64 * j + 8 * k, desc + ((at + 2 * k * L::BP_LBO) >> 4), L::IDESC_P,
+                           v > c.lo || (t & 1) || k);
+            }
+            tc_commit(&s.o_done);
+          }
+          __syncwarp();
+        }
       }
     }
-    // every copy that was asked for has landed (where no wait gave up: at once)
-    for (uint32_t n = loads > NST ? loads - NST : 0; n < loads; n++) mbar_wait_bounded(&s.full[n % NST], (n / NST) & 1, DEC_WAIT_LIMIT);
-   }
   } else if (warp >= 4) {
-    // ---- dequantisation: K of block n + 1, then V of block n
-    if constexpr (L::SHARES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::DEQUANT_REGS));
+    // ---- dequantisation
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
     const int r = tid & 127;
-    auto k_tile = [&](uint32_t n) {
-      tree_wait(&s.full[n % NST], (n / NST) & 1, &s.failed);
-      if (n > 0) tree_wait(&s.s_done[(n - 1) & 1], ((n - 1) >> 1) & 1, &s.failed);
-      tc_fence_after();
-      const uint8_t* const st = stages + (n % NST) * L::STAGE_BYTES;
-#pragma unroll
-      for (int j = 0; j < DJ; j++)
-        tree_dequant<BITS>(st + r * L::P + j * (16 * BITS), p.lut_lo, p.lut_hi, p.lookup, tmem + lanes + L::K_COL + 64 * j);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&s.k_ready);
-    };
-    auto v_tile = [&](uint32_t n) {
-      if (n > 0) tree_wait(&s.o_done, (n - 1) & 1, &s.failed);
-      tc_fence_after();
-      const uint8_t* const st = stages + (n % NST) * L::STAGE_BYTES + L::TILE_BYTES;
-#pragma unroll
-      for (int j = 0; j < DJ; j++)
-        tree_dequant<BITS>(st + (r + 128 * j) * (16 * BITS), p.lut_v_lo, p.lut_v_hi, p.lookup, tmem + lanes + L::V_COL + 64 * j);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&s.v_ready);
-    };
+    const bool k_side = warp < 8;
     uint32_t blocks = 0;
-    if (walk.next(p, range, c, false)) {  // a hand with the first piece's queries
-      const int q0 = c.tile * N, nq = min(N, c.sq.tokens * p.group - q0);
-      tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, 8, 2, 256, lane);
-      k_tile(0);
+    if (walk.next(p, range, c, false)) {
+      if (!k_side) {  // a hand with the first piece's queries
+        const int q0 = c.tile * N, nq = min(N, c.sq.tokens * p.group - q0);
+        tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp - 4, 8, 2, 256, lane);
+      }
       do blocks += c.hi - c.lo;
       while (walk.next(p, range, c, false));
     }
+    // one loop for both sides (and its parts rolled up where they repeat): the code that the SM's warps run side by side has to fit its
+    // instruction cache
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int x = 0; x < 4; x++) {
+      lo[x] = k_side ? p.lut_lo[x] : p.lut_v_lo[x];
+      hi[x] = k_side ? p.lut_hi[x] : p.lut_v_hi[x];
+    }
+    const uint8_t* const run = stages + (k_side ? r * L::P : L::TILE_BYTES + r * (16 * BITS));
+    const int step = k_side ? 16 * BITS : 128 * 16 * BITS;
+    const uint32_t col = tmem + lanes + (k_side ? L::K_COL : L::V_COL);
+    uint64_t* const ready = k_side ? &s.k_ready : &s.v_ready;
     for (; i < blocks; i++) {
-      if (i + 1 < blocks) k_tile(i + 1);
-      v_tile(i);
+      const uint32_t st = i % NST, before = i - 1;
+      tree_wait(&s.full[st], (i / NST) & 1, &s.failed);
+      // the tile before is read no more
+      if (i > 0) tree_wait(k_side ? &s.s_done[before & 1] : &s.o_done, (k_side ? before >> 1 : before) & 1, &s.failed);
+      tc_fence_after();
+#pragma unroll 1
+      for (int j = 0; j < DJ; j++) tree_dequant<BITS>(run + st * L::STAGE_BYTES + j * step, lo, hi, p.lookup, col + 64 * j);
+      tc_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(ready);
     }
   } else {
     // ---- softmax
-    if constexpr (L::SHARES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
     const int r = tid;
     const uint32_t o_col = tmem + lanes + L::O_COL;
     uint8_t* const bp_row = bp + (r & 7) * 16 + (r >> 3) * L::BP_LBO;
@@ -570,7 +572,10 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
         fence_proxy_async();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s.p_ready);
+        if (lane == 0) {
+          mbar_arrive(&s.s_read[i & 1]);
+          mbar_arrive(&s.p_ready);
+        }
       }
       // ---- the piece's partial. Sums over the rows: in the warp, then over the four warps, in a fixed order.
       const size_t part = (walk.item(p, c) + blockIdx.x) * N;
@@ -610,7 +615,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   __syncthreads();
   if (*(volatile uint32_t*)&s.failed) {  // (nobody writes it any more)
     if (tid == 0 && p.status) atomicOr(&p.status[0], IQ_STATUS_WAIT_TIMEOUT);
-    if (warp == 8) {  // MMAs may still be running: they are waited for, with a limit, before the tensor memory goes
+    if (warp == TREE_QK_WARP || warp == TREE_PV_WARP) {  // MMAs may still be running: they are waited for, with a limit, before the tensor memory goes
       if (elect_one()) tc_commit(&s.drain);
       __syncwarp();
       mbar_wait_bounded(&s.drain, 0u, DEC_WAIT_LIMIT);
@@ -619,7 +624,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS));
+  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS));
 }
 
 template <int D, int BITS, int N>
