@@ -8,10 +8,9 @@
 namespace iq {
 
 // Four warpgroups: warps 0 .. 3 take the softmax (a thread to a cache row), 4 .. 7 dequantise K (a thread to a row), 8 .. 11 V (a thread to
-// a coordinate), and of the last four one issues the score products, one the value products, one the loads (the fourth is there because
-// register shares change by whole warpgroups).
+// a coordinate), and of the last four one issues the score products, one the value products, one the loads, and one finds the work.
 constexpr int TREE_THREADS = 512;
-constexpr int TREE_QK_WARP = 12, TREE_PV_WARP = 13, TREE_LOAD_WARP = 14;
+constexpr int TREE_QK_WARP = 12, TREE_PV_WARP = 13, TREE_LOAD_WARP = 14, TREE_WALK_WARP = 15;
 constexpr float TREE_RAISE = 9.f;      // a score this far (log2) above its column's reference raises the references,
 constexpr float TREE_HEADROOM = 2.f;   // to this far above the block's maximum
 constexpr float TREE_V_ROOM = 2.f;     // and the reference of the V scales to at least this times their maximum
@@ -19,16 +18,31 @@ constexpr float TREE_V_ROOM = 2.f;     // and the reference of the V scales to a
 // the second term still holds 9 bits.
 constexpr float TREE_P_UNIT = 32.f;
 
+// The pieces of a CTA's range: runs of blocks of an item. One warp walks along the range and leaves the pieces in shared memory, up to
+// TREE_BATCH at a time, the next ones while the others work on these.
+struct TreePiece {
+  TreeSeq sq;
+  int b, g, tile, lo, hi;
+  size_t item;
+};
+constexpr int TREE_BATCH = 16;
+struct TreeBatch {
+  int pieces, blocks;
+  TreePiece piece[TREE_BATCH];
+};
+
 template <int N>
 struct TreeShared {
   uint64_t full[4], q_ready, k_ready, v_ready, s_done[2], s_read[2], p_ready, o_done, taken[4], drain;  // s_done, s_read: of even and odd blocks
   uint32_t tmem, failed;
   alignas(16) float neg_ref[N];     // minus the reference of each column, log2 units
-  float l_factor[N], o_factor[N];   // of the last raise
-  float warp_max[4][N];             // per quarter of the rows; at the end of a piece: sums
+  alignas(16) float l_factor[N];    // of the last raise
+  alignas(16) float o_factor[N];
+  alignas(16) float warp_max[4][N];             // per quarter of the rows; at the end of a piece: sums
   float warp_v[4], warp_q[8];
   int token[N];                     // the token of a column, counted from the tile's first
   TreeMasks<N> masks;
+  TreeBatch batch[2];
   long long scratch[TREE_THREADS / 32 + 2];
 };
 
@@ -62,45 +76,6 @@ struct TreeLayout {
   // fp32 result, binary16 operands, M = 128; B_Q K-major, B_P MN-major
   static constexpr uint32_t IDESC_Q = (1u << 4) | (((uint32_t)N >> 3) << 17) | ((128u >> 4) << 24);
   static constexpr uint32_t IDESC_P = IDESC_Q | (1u << 16);
-};
-
-// The pieces of a CTA's range: runs of blocks of an item.
-struct TreePiece {
-  TreeSeq sq;
-  int b, g, tile, lo, hi;
-};
-struct TreeWalk {
-  long long at, seq_at;
-  int b;
-  __device__ __forceinline__ void start(const TreeRange& r) { at = r.at; seq_at = r.seq_at; b = r.b; }
-  __device__ __forceinline__ size_t item(const TreeParams& p, const TreePiece& c) const { return ((size_t)c.b * p.n_kv_heads + c.g) * p.tiles + c.tile; }
-  // The next piece with blocks; false: the range has no more. `write`: this thread notes the items that start in the range.
-  __device__ __forceinline__ bool next(const TreeParams& p, const TreeRange& r, TreePiece& c, bool write) {
-    while (at < r.end) {
-      c.sq = tree_seq(p, b);
-      if (at >= seq_at + c.sq.weight) { seq_at += c.sq.weight; b++; continue; }
-      const int len = c.sq.blocks + TREE_SEG_COST;
-      const int k = (int)((at - seq_at) / len);  // item of the sequence
-      const long long item_at = seq_at + (long long)k * len;
-      const int off = (int)(at - item_at), take = (int)min((long long)(len - off), r.end - at);
-      c.b = b;
-      c.g = k / c.sq.tiles;
-      c.tile = k - c.g * c.sq.tiles;
-      c.lo = max(off - TREE_SEG_COST, 0);
-      c.hi = max(off + take - TREE_SEG_COST, 0);
-      at += take;
-      if (off == 0 && write) {
-        int2 info = make_int2(0, 0);
-        if (c.sq.blocks) {
-          info.x = tree_cta_of(item_at + TREE_SEG_COST, r.total, r.ctas);
-          info.y = tree_cta_of(item_at + len - 1, r.total, r.ctas) - info.x + 1;
-        }
-        p.item_info[item(p, c)] = info;
-      }
-      if (c.lo < c.hi) return true;
-    }
-    return false;
-  }
 };
 
 // Bounded wait of a converged warp. A wait that gives up is noted in `failed`, and from then on no wait of the CTA lasts: every thread
@@ -298,10 +273,12 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(FULL, s.tmem, 0);
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the tensor-memory lanes
-  TreeWalk walk;
-  walk.start(range);
-  TreePiece c;
   uint32_t i = 0;  // blocks of the CTA so far
+  // Batch k of pieces is there (false: an empty one, the range is done), and the one before it has been worked off by everybody.
+  auto batch = [&](int k) {
+    cta_bar_sync_n(3, TREE_THREADS);
+    return s.batch[k & 1].pieces != 0;
+  };
 
   if (warp >= 12) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
@@ -309,7 +286,8 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
       // ---- loads: block n into stage n % NST, when the values of block n - NST have been taken (and with them its scores)
       const uint32_t sc_bytes = p.scale_f16 ? 256u : 512u;
       const size_t sc_size = p.scale_f16 ? 2 : 4;
-      while (walk.next(p, range, c, false)) {
+      for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
+        const TreePiece c = s.batch[k & 1].piece[j];
         for (int v = c.lo; v < c.hi && !tree_failed(&s.failed); v++, i++) {
           const int st = i % NST;
           const size_t row0 = cache_row(p.pm, c.b, c.g, (long long)c.sq.block(v) * 128, lane == 0 ? p.status : nullptr);
@@ -332,10 +310,10 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
       // its queries, which wait for the piece before.)
       const uint64_t desc = smem_desc_mn(smem_u32(bq), L::BQ_LBO, 128);
       uint32_t pieces = 0;
-      while (walk.next(p, range, c, false)) {
+      for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
         tree_wait(&s.q_ready, pieces & 1, &s.failed);
         pieces++;
-        for (int v = c.lo; v < c.hi; v++, i++) {
+        for (const uint32_t end = i + s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo; i < end; i++) {
           if (i >= SB) tree_wait(&s.s_read[(i - SB) & 1], ((i - SB) >> 1) & 1, &s.failed);
           tree_wait(&s.k_ready, i & 1, &s.failed);
           tc_fence_after();
@@ -356,8 +334,9 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
     } else if (warp == TREE_PV_WARP) {
       // ---- value products
       const uint64_t desc = smem_desc_mn(smem_u32(bp), L::BP_LBO, L::BP_SBO);
-      while (walk.next(p, range, c, false)) {
-        for (int v = c.lo; v < c.hi; v++, i++) {
+      for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
+        const uint32_t first = i;
+        for (const uint32_t end = i + s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo; i < end; i++) {
           tree_wait(&s.v_ready, i & 1, &s.failed);
           tree_wait(&s.p_ready, i & 1, &s.failed);
           tc_fence_after();
@@ -365,11 +344,11 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
             mbar_arrive(&s.taken[i % NST]);
 #pragma unroll 1
             for (int t = 0; t < 2 * DJ; t++) {  // terms of the probabilities, halves of the coordinates
-              const uint32_t j = t >> 1, at = (t & 1) * L::BP_TERM;
+              const uint32_t h = t >> 1, at = (t & 1) * L::BP_TERM;
 #pragma unroll
               for (int k = 0; k < 8; k++)
-                tc_mma_f16(tmem + L::O_COL + j * N, tmem + L::V_COL + 64 * j + 8 * k, desc + ((at + 2 * k * L::BP_LBO) >> 4), L::IDESC_P,
-                           v > c.lo || (t & 1) || k);
+                tc_mma_f16(tmem + L::O_COL + h * N, tmem + L::V_COL + 64 * h + 8 * k, desc + ((at + 2 * k * L::BP_LBO) >> 4), L::IDESC_P,
+                           i > first || (t & 1) || k);
             }
             tc_commit(&s.o_done);
           }
@@ -377,20 +356,48 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
         }
       }
     }
+    else if (warp == TREE_WALK_WARP) {
+      // ---- the pieces
+      long long at = range.at, seq_at = range.seq_at;
+      int b = range.b;
+      TreeSeq sq;
+      if (at < range.end) sq = tree_seq(p, b);
+      for (int k = 0;; k++) {
+        TreeBatch& out = s.batch[k & 1];
+        int n = 0, blocks = 0;
+        while (n < TREE_BATCH && at < range.end) {
+          if (at >= seq_at + sq.weight) { seq_at += sq.weight; sq = tree_seq(p, ++b); continue; }
+          const int len = sq.blocks + TREE_SEG_COST;
+          const int m = (int)((at - seq_at) / len);  // item of the sequence
+          const long long item_at = seq_at + (long long)m * len;
+          const int off = (int)(at - item_at), take = (int)min((long long)(len - off), range.end - at);
+          const int lo = max(off - TREE_SEG_COST, 0), hi = max(off + take - TREE_SEG_COST, 0), g = m / sq.tiles, tile = m - g * sq.tiles;
+          const size_t item = ((size_t)b * p.n_kv_heads + g) * p.tiles + tile;
+          at += take;
+          if (off == 0 && lane == 0) {  // the item starts here: which CTAs have its blocks
+            int2 info = make_int2(0, 0);
+            if (sq.blocks) {
+              info.x = tree_cta_of(item_at + TREE_SEG_COST, range.total, range.ctas);
+              info.y = tree_cta_of(item_at + len - 1, range.total, range.ctas) - info.x + 1;
+            }
+            p.item_info[item] = info;
+          }
+          if (lo < hi) {
+            if (lane == 0) out.piece[n] = {sq, b, g, tile, lo, hi, item};
+            n++;
+            blocks += hi - lo;
+          }
+        }
+        if (lane == 0) { out.pieces = n; out.blocks = blocks; }
+        cta_bar_sync_n(3, TREE_THREADS);
+        if (n == 0) break;
+      }
+    }
   } else if (warp >= 4) {
     // ---- dequantisation
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
     const int r = tid & 127;
     const bool k_side = warp < 8;
-    uint32_t blocks = 0;
-    if (walk.next(p, range, c, false)) {
-      if (!k_side) {  // a hand with the first piece's queries
-        const int q0 = c.tile * N, nq = min(N, c.sq.tokens * p.group - q0);
-        tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp - 4, 8, 2, 256, lane);
-      }
-      do blocks += c.hi - c.lo;
-      while (walk.next(p, range, c, false));
-    }
     // one loop for both sides (and its parts rolled up where they repeat): the code that the SM's warps run side by side has to fit its
     // instruction cache
     uint32_t lo[4], hi[4];
@@ -403,7 +410,13 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
     const int step = k_side ? 16 * BITS : 128 * 16 * BITS;
     const uint32_t col = tmem + lanes + (k_side ? L::K_COL : L::V_COL);
     uint64_t* const ready = k_side ? &s.k_ready : &s.v_ready;
-    for (; i < blocks; i++) {
+    for (int k = 0; batch(k); k++) {
+     if (k == 0 && !k_side) {  // a hand with the first piece's queries
+      const TreePiece c = s.batch[0].piece[0];
+      const int q0 = c.tile * N;
+      tree_queries<D, BITS, N>(p, s, bq, c, q0, min(N, c.sq.tokens * p.group - q0), warp - 4, 8, 2, 256, lane);
+     }
+     for (const uint32_t end = i + s.batch[k & 1].blocks; i < end; i++) {
       const uint32_t st = i % NST, before = i - 1;
       tree_wait(&s.full[st], (i / NST) & 1, &s.failed);
       // the tile before is read no more
@@ -415,6 +428,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(ready);
+     }
     }
   } else {
     // ---- softmax
@@ -422,7 +436,8 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
     const int r = tid;
     const uint32_t o_col = tmem + lanes + L::O_COL;
     uint8_t* const bp_row = bp + (r & 7) * 16 + (r >> 3) * L::BP_LBO;
-    while (walk.next(p, range, c, tid == 0)) {
+    for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
+      const TreePiece c = s.batch[k & 1].piece[j];
       const int q0 = c.tile * N, nq = min(N, c.sq.tokens * p.group - q0), t0 = q0 / p.group;
       if (tid == 0) s.masks.from_max = 0;
       cta_bar_sync_n(1, 128);  // the last piece's references have been read
@@ -431,8 +446,8 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
         s.neg_ref[tid] = 1e30f;
         s.token[tid] = (q0 + tid) / p.group - t0;
       }
-      const int e2 = i == 0 ? tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, 8, 2, 256, lane)
-                            : tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, 4, 1, 128, lane);
+      const bool first = i == 0;
+      const int e2 = tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, first ? 8 : 4, 2, first ? 256 : 128, lane);
       if (lane == 0) mbar_arrive(&s.q_ready);
       const float score_unit = p.score_unit * __uint_as_float((uint32_t)(127 - e2) << 23);
 
@@ -449,7 +464,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
         const int row0 = c.sq.block(v) * 128;
         const bool masked = row0 + 128 > c.sq.ctx || !(row0 >= s.masks.from_max || row0 + 128 <= p.sinks);
         uint32_t sees[(N + 31) / 32];  // bit n: column n sees the row
-        if (masked) {
+        if (__builtin_expect(masked, 0)) {
           bool any = false;
 #pragma unroll 1
           for (int w = 0; w < (N + 31) / 32; w++) {
@@ -481,7 +496,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
             const F32x2 a = fma2(f32x2(t[n], t[n + 1]), f32x2(ks, ks), f32x2(f.x, f.y)), b = fma2(f32x2(t[n + 2], t[n + 3]), f32x2(ks, ks), f32x2(f.z, f.w));
             t[n] = a.lo(); t[n + 1] = a.hi(); t[n + 2] = b.lo(); t[n + 3] = b.hi();
           }
-          if (masked) {
+          if (__builtin_expect(masked, 0)) {
 #pragma unroll
             for (int n = 0; n < CH; n++)
               if (!(sees[n0 / 32] >> (n % 32) & 1u)) t[n] = -INFINITY;
@@ -494,7 +509,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
 #pragma unroll
           for (int n = 0; n < CH; n += 2) top = max3f(top, t[n], t[n + 1]);
         }
-        if (cta_bar_or_n(1, 128, top > TREE_RAISE || vs_fin > v_ref)) {
+        if (__builtin_expect(cta_bar_or_n(1, 128, top > TREE_RAISE || vs_fin > v_ref), 0)) {
           // ---- new references: the maximum of each column over the block, and of the V scales
           const float vm = tree_warp_max(vs_fin);
           if (lane == 0) s.warp_v[warp] = vm;
@@ -503,10 +518,12 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
             float z[8];
             tree_ld<8>(s_col + n0, z);
             const uint32_t on = (n0 < 32 ? sees[0] : sees[(N + 31) / 32 - 1]) >> (n0 & 31);
+            float m[8];
 #pragma unroll
-            for (int n = 0; n < 8; n++) {
-              const float m = tree_warp_max((on >> n & 1u) ? z[n] * ks : -3e38f);
-              if (lane == 0) s.warp_max[warp][n0 + n] = m;
+            for (int n = 0; n < 8; n++) m[n] = tree_warp_max((on >> n & 1u) ? z[n] * ks : -3e38f);
+            if (lane == 0) {
+              *reinterpret_cast<float4*>(&s.warp_max[warp][n0]) = make_float4(m[0], m[1], m[2], m[3]);
+              *reinterpret_cast<float4*>(&s.warp_max[warp][n0 + 4]) = make_float4(m[4], m[5], m[6], m[7]);
             }
           }
           cta_bar_sync_n(1, 128);
@@ -526,7 +543,10 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
           cta_bar_sync_n(1, 128);
           v_ref = v_new;
 #pragma unroll
-          for (int n = 0; n < N; n++) l[n] *= s.l_factor[n];
+          for (int n = 0; n < N; n += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(s.l_factor + n);
+            l[n] *= f.x; l[n + 1] *= f.y; l[n + 2] *= f.z; l[n + 3] *= f.w;
+          }
           if (v > c.lo) {
             tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
             tc_fence_after();
@@ -556,18 +576,22 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
             const F32x2 ls = add2(f32x2(l[n], l[n + 1]), f32x2(p0, p1)), x = mul2(f32x2(p0, p1), f32x2(vn, vn));
             l[n] = ls.lo();
             l[n + 1] = ls.hi();
-            float x0 = x.lo(), x1 = x.hi();
-            if (masked) {  // (0 times an infinite scale)
-              if (!(sees[n / 32] >> (n % 32) & 1u)) x0 = 0.f;
-              if (!(sees[n / 32] >> (n % 32 + 1) & 1u)) x1 = 0.f;
-            }
-            hi[k] = pack_half2(x0, x1);
+            hi[k] = pack_half2(x.lo(), x.hi());
             const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[k]));
-            lo[k] = pack_half2(x0 - f.x, x1 - f.y);
+            lo[k] = pack_half2(x.lo() - f.x, x.hi() - f.y);
           }
           uint8_t* const dst = bp_row + (n0 / 8) * L::BP_SBO;
           *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
           *reinterpret_cast<uint4*>(dst + L::BP_TERM) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+        if (__builtin_expect(masked && vs_fin != vs, 0)) {  // an infinite scale, and tokens that do not see its row: 0 instead of 0 times infinity
+#pragma unroll 1
+          for (int n = 0; n < N; n++)
+            if (!((n < 32 ? sees[0] : sees[(N + 31) / 32 - 1]) >> (n & 31) & 1u)) {
+              uint8_t* const dst = bp_row + (n / 8) * L::BP_SBO + (n & 7) * 2;
+              *reinterpret_cast<uint16_t*>(dst) = 0;
+              *reinterpret_cast<uint16_t*>(dst + L::BP_TERM) = 0;
+            }
         }
         fence_proxy_async();
         tc_fence_before();
@@ -578,7 +602,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
         }
       }
       // ---- the piece's partial. Sums over the rows: in the warp, then over the four warps, in a fixed order.
-      const size_t part = (walk.item(p, c) + blockIdx.x) * N;
+      const size_t part = (c.item + blockIdx.x) * N;
       cta_bar_sync_n(1, 128);  // (warp_max of a raise has been read)
 #pragma unroll
       for (int n0 = 0; n0 < N; n0 += CH) {
