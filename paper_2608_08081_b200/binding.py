@@ -202,13 +202,15 @@ class Cache:
     page_rows: int = 0
 
     def c(self) -> _IqCache:
-        assert self.k_scales.dtype == self.v_scales.dtype and self.k_scales.dtype in (torch.float32, torch.float16)
-        f16 = 1 if self.k_scales.dtype == torch.float16 else 0   # binary16 scale arrays: 50 instead of 52 bytes per row
-        if self.block_table is None:
-            return _IqCache(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr(), None, 0, 0, f16)
-        assert self.block_table.dtype == torch.int32 and self.block_table.is_contiguous()
-        return _IqCache(self.k_codes.data_ptr(), self.k_scales.data_ptr(), self.v_codes.data_ptr(), self.v_scales.data_ptr(),
-                        self.block_table.data_ptr(), self.page_rows, self.k_scales.shape[0], f16)
+        ks, vs, table = self.k_scales, self.v_scales, self.block_table
+        dtype = ks.dtype
+        assert dtype is vs.dtype and (dtype is torch.float32 or dtype is torch.float16)
+        f16 = 1 if dtype is torch.float16 else 0   # binary16 scale arrays: 50 instead of 52 bytes per row
+        if table is None:
+            return _IqCache(self.k_codes.data_ptr(), ks.data_ptr(), self.v_codes.data_ptr(), vs.data_ptr(), None, 0, 0, f16)
+        assert table.dtype is torch.int32 and table.is_contiguous()
+        return _IqCache(self.k_codes.data_ptr(), ks.data_ptr(), self.v_codes.data_ptr(), vs.data_ptr(), table.data_ptr(), self.page_rows,
+                        ks.shape[0], f16)
 
 
 def _ptr(t):
@@ -470,11 +472,12 @@ def iq_selftest_bounded_wait(status, polls: int, stream=None) -> None:
 
 
 # ------------------------------------------------------------------ drafted tokens, rows and pages
-@dataclass
+@dataclass(frozen=True, eq=False)
 class PagePool:
     """Which page holds which rows, on the device: block_table int32 [n_seqs][pages_per_seq] (-1: no page; the same tensor as the
     Cache's), ref_count int32 [num_pages], free_list int32 [num_pages] (a stack), state int32 [iq_page_pool_state_ints(num_pages)]
-    ([0]: free pages, the rest zero). new_page_pool makes one with every page free."""
+    ([0]: free pages, the rest zero). new_page_pool makes one with every page free. The calls update the tensors in place; the pool
+    keeps their addresses (like Shape and Codebook it builds its C struct once)."""
     block_table: torch.Tensor
     ref_count: torch.Tensor
     free_list: torch.Tensor
@@ -482,21 +485,28 @@ class PagePool:
     page_rows: int
 
     def c(self) -> _IqPagePool:
-        for t in (self.block_table, self.ref_count, self.free_list, self.state):
-            assert t.dtype == torch.int32 and t.is_contiguous()
-        n = self.ref_count.numel()
-        assert self.block_table.dim() == 2 and self.free_list.numel() == n and self.state.numel() >= 4 + (n + 31) // 32
-        return _IqPagePool(self.block_table.data_ptr(), self.ref_count.data_ptr(), self.free_list.data_ptr(), self.state.data_ptr(),
-                           self.block_table.shape[0], self.block_table.shape[1], n, self.page_rows)
+        cp = self.__dict__.get("_c")
+        if cp is None:
+            for t in (self.block_table, self.ref_count, self.free_list, self.state):
+                assert t.dtype == torch.int32 and t.is_contiguous()
+            n = self.ref_count.numel()
+            assert self.block_table.dim() == 2 and self.free_list.numel() == n and self.state.numel() >= iq_page_pool_state_ints(n)
+            cp = _IqPagePool(self.block_table.data_ptr(), self.ref_count.data_ptr(), self.free_list.data_ptr(), self.state.data_ptr(),
+                             self.block_table.shape[0], self.block_table.shape[1], n, self.page_rows)
+            object.__setattr__(self, "_c", cp)
+        return cp
 
 
 def iq_page_pool_state_ints(num_pages: int) -> int:
     return int(_lib.iq_page_pool_state_ints(num_pages))
 
 
-def _ints(t, numel=None):
-    assert t is None or (t.dtype in (torch.int32, torch.uint32) and t.is_contiguous() and (numel is None or t.numel() == numel))
-    return _ptr(t)
+def _ints(t, numel):
+    """Address of a contiguous int32 (or uint32) tensor of so many elements; None: none."""
+    if t is None:
+        return None
+    assert (t.dtype is torch.int32 or t.dtype is torch.uint32) and t.numel() == numel and t.is_contiguous()
+    return t.data_ptr()
 
 
 def iq_tree_workspace_bytes(shape: Shape, n_tokens_max: int) -> int:
@@ -511,50 +521,65 @@ def iq_tree_attention(shape: Shape, rot_dev, codebook: Codebook, q, cache: Cache
     (None: a chain); n_tokens_dev: int32 [B] or None (all T). out fp16 or fp32 [B][T][H_q][d], lse_out fp32 [B][T][H_q].
     window > 0: only the window's context rows and the first `sinks` are seen. workspace: a device uint8 tensor of
     iq_tree_workspace_bytes(shape, T) bytes."""
-    B, T, H, d = q.shape
-    assert q.dtype == torch.float16 and q.stride(3) == 1 and (B, H, d) == (shape.batch, shape.n_q_heads, shape.head_dim)
-    assert tuple(out.shape) == (B, T, H, d) and out.is_contiguous() and out.dtype in (torch.float16, torch.float32)
-    assert lse_out is None or (lse_out.dtype == torch.float32 and tuple(lse_out.shape) == (B, T, H) and lse_out.is_contiguous())
-    need = iq_tree_workspace_bytes(shape, T)
-    assert workspace.is_contiguous() and workspace.numel() * workspace.element_size() >= need
-    cs, cb, cc = shape.c(), codebook.c(), cache.c()
-    _check(_lib.iq_tree_attention(ctypes.byref(cs), _ptr(rot_dev), ctypes.byref(cb), _ptr(q), q.stride(0), q.stride(1), q.stride(2),
-                                  ctypes.byref(cc), _ints(ctx_lens_dev, B), _ints(tree_mask_dev, B * T * ((T + 31) // 32)),
-                                  _ints(n_tokens_dev, B), T, window, sinks, _ptr(workspace), _ptr(out),
-                                  1 if out.dtype == torch.float16 else 0, _ptr(lse_out), _ptr(status_dev), _stream(stream)),
-           "iq_tree_attention")
+    size = q.shape
+    B, T, H, d = size
+    f16 = out.dtype is torch.float16
+    assert q.dtype is torch.float16 and B == shape.batch and H == shape.n_q_heads and d == shape.head_dim
+    assert out.shape == size and out.is_contiguous() and (f16 or out.dtype is torch.float32)
+    assert lse_out is None or (lse_out.dtype is torch.float32 and lse_out.shape == size[:3] and lse_out.is_contiguous())
+    sb, st, sh, sd = q.stride()
+    assert sd == 1
+    sizes = shape.__dict__.get("_tree_bytes")  # (kept with the shape, like its C struct: the call below is bound by the host's time)
+    if sizes is None:
+        object.__setattr__(shape, "_tree_bytes", {})
+        sizes = shape._tree_bytes
+    if T not in sizes:
+        sizes[T] = iq_tree_workspace_bytes(shape, T)
+    assert workspace.nbytes >= sizes[T] and workspace.is_contiguous()
+    rc = _lib.iq_tree_attention(ctypes.byref(shape.c()), rot_dev.data_ptr(), ctypes.byref(codebook.c()), q.data_ptr(), sb, st, sh,
+                                ctypes.byref(cache.c()), _ints(ctx_lens_dev, B), _ints(tree_mask_dev, B * T * ((T + 31) // 32)),
+                                _ints(n_tokens_dev, B), T, window, sinks, workspace.data_ptr(), out.data_ptr(), 1 if f16 else 0, _ptr(lse_out),
+                                _ptr(status_dev), _stream(stream))
+    if rc:
+        raise IQError(rc, "iq_tree_attention")
 
 
 def iq_keep_rows(shape: Shape, cache: Cache, base_pos_dev, keep_dev, n_keep_dev=None, status_dev=None, stream=None) -> None:
     """Row base_pos[b] + i receives what row base_pos[b] + keep[b][i] held: keep_dev int32 [B][n], n_keep_dev int32 [B] or None (n)."""
-    assert keep_dev.dim() == 2 and keep_dev.shape[0] == shape.batch
-    cs, cc = shape.c(), cache.c()
-    _check(_lib.iq_keep_rows(ctypes.byref(cs), ctypes.byref(cc), _ints(base_pos_dev, shape.batch), _ints(keep_dev),
-                             _ints(n_keep_dev, shape.batch), keep_dev.shape[1], _ptr(status_dev), _stream(stream)), "iq_keep_rows")
+    B, n = keep_dev.shape
+    assert B == shape.batch
+    rc = _lib.iq_keep_rows(ctypes.byref(shape.c()), ctypes.byref(cache.c()), _ints(base_pos_dev, B), _ints(keep_dev, B * n), _ints(n_keep_dev, B), n,
+                           _ptr(status_dev), _stream(stream))
+    if rc:
+        raise IQError(rc, "iq_keep_rows")
 
 
 def iq_reserve_pages(pool: PagePool, first_row_dev, end_row_dev, status_dev=None, stream=None) -> None:
     """A page for every entry without one among rows [first_row[b], end_row[b]) (int32 [n_seqs] each)."""
-    cp, n = pool.c(), pool.block_table.shape[0]
-    _check(_lib.iq_reserve_pages(ctypes.byref(cp), _ints(first_row_dev, n), _ints(end_row_dev, n), _ptr(status_dev), _stream(stream)),
-           "iq_reserve_pages")
+    cp = pool.c()
+    rc = _lib.iq_reserve_pages(ctypes.byref(cp), _ints(first_row_dev, cp.n_seqs), _ints(end_row_dev, cp.n_seqs), _ptr(status_dev), _stream(stream))
+    if rc:
+        raise IQError(rc, "iq_reserve_pages")
 
 
 def iq_release_pages(pool: PagePool, first_row_dev, end_row_dev, status_dev=None, stream=None) -> None:
     """Gives back the pages of which all rows lie in [first_row[b], end_row[b])."""
-    cp, n = pool.c(), pool.block_table.shape[0]
-    _check(_lib.iq_release_pages(ctypes.byref(cp), _ints(first_row_dev, n), _ints(end_row_dev, n), _ptr(status_dev), _stream(stream)),
-           "iq_release_pages")
+    cp = pool.c()
+    rc = _lib.iq_release_pages(ctypes.byref(cp), _ints(first_row_dev, cp.n_seqs), _ints(end_row_dev, cp.n_seqs), _ptr(status_dev), _stream(stream))
+    if rc:
+        raise IQError(rc, "iq_release_pages")
 
 
 def iq_fork_sequences(shape: Shape, cache: Cache, pool: PagePool, src_seq_dev, dst_seq_dev, n_rows_dev, status_dev=None, stream=None) -> None:
     """Sequence dst[i] becomes a branch of sequence src[i] after its first n_rows[i] rows (int32 [n] each): whole pages are shared,
     a partly filled one is copied."""
-    assert cache.k_scales.shape[0] == pool.ref_count.numel() and cache.k_scales.shape[2] == pool.page_rows
+    cc, cp = cache.c(), pool.c()
+    assert cc.num_pages == cp.num_pages and cc.page_rows == cp.page_rows  # the pool is the cache's
     n = src_seq_dev.numel()
-    cs, cc, cp = shape.c(), cache.c(), pool.c()
-    _check(_lib.iq_fork_sequences(ctypes.byref(cs), ctypes.byref(cc), ctypes.byref(cp), _ints(src_seq_dev, n), _ints(dst_seq_dev, n),
-                                  _ints(n_rows_dev, n), n, _ptr(status_dev), _stream(stream)), "iq_fork_sequences")
+    rc = _lib.iq_fork_sequences(ctypes.byref(shape.c()), ctypes.byref(cc), ctypes.byref(cp), _ints(src_seq_dev, n), _ints(dst_seq_dev, n),
+                                _ints(n_rows_dev, n), n, _ptr(status_dev), _stream(stream))
+    if rc:
+        raise IQError(rc, "iq_fork_sequences")
 
 
 def iq_copy_pages(shape: Shape, cache: Cache, src_pages_dev, dst_pages_dev, status_dev=None, stream=None) -> None:
