@@ -207,7 +207,6 @@ struct TreeParams {
 };
 cudaError_t launch_tree_attention(const TreeParams& p, int head_dim, cudaStream_t stream);
 int tree_tile(int head_dim, int queries);  // tile for that many (token, head) pairs of a KV head
-int tree_ctas_per_sm(int head_dim, int tile);
 
 // ---- rows and pages of the cache
 struct CacheArrays {

@@ -68,7 +68,6 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(const __gr
 }  // namespace
 
 int tree_tile(int head_dim, int queries) { return queries <= 16 ? 16 : queries <= 32 ? 32 : 64; }
-int tree_ctas_per_sm(int head_dim, int tile) { return head_dim == 128 ? 2 : 1; }
 
 cudaError_t launch_tree_attention(const TreeParams& p, int head_dim, cudaStream_t stream) {
   const cudaError_t e = p.bits == 2 ? launch_tree_b2(p, head_dim, stream) : p.bits == 3 ? launch_tree_b3(p, head_dim, stream) : launch_tree_b4(p, head_dim, stream);

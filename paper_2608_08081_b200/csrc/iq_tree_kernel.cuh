@@ -7,10 +7,10 @@
 
 namespace iq {
 
-// Four warpgroups: warps 0 .. 3 take the softmax (a thread to a cache row), 4 .. 7 dequantise K (a thread to a row), 8 .. 11 V (a thread to
-// a coordinate), and of the last four one issues the score products, one the value products, one the loads, and one finds the work.
-constexpr int TREE_THREADS = 512;
-constexpr int TREE_QK_WARP = 12, TREE_PV_WARP = 13, TREE_LOAD_WARP = 14, TREE_WALK_WARP = 15;
+// Warpgroups of a CTA: two or four for the softmax (a thread to a cache row, a half or a quarter of the columns each), one that dequantises
+// K (a thread to a row), one that dequantises V (a thread to a coordinate), and one of which a warp each issues the score products, issues
+// the value products, loads, and finds the work.
+
 constexpr float TREE_RAISE = 9.f;      // a score this far (log2) above its column's reference raises the references,
 constexpr float TREE_HEADROOM = 2.f;   // to this far above the block's maximum
 constexpr float TREE_V_ROOM = 2.f;     // and the reference of the V scales to at least this times their maximum
@@ -27,23 +27,25 @@ struct TreePiece {
 };
 constexpr int TREE_BATCH = 16;
 struct TreeBatch {
-  int pieces, blocks;
+  int pieces;
   TreePiece piece[TREE_BATCH];
 };
 
+constexpr int TREE_STAGES = 6;  // at most
 template <int N>
 struct TreeShared {
-  uint64_t full[4], q_ready, k_ready, v_ready, s_done[2], s_read[2], p_ready, o_done, taken[4], drain;  // s_done, s_read: of even and odd blocks
+  uint64_t full[TREE_STAGES], taken[TREE_STAGES], q_ready, s_done, s_read, p_ready, o_done, drain;
+  uint64_t k_ready[2], k_free[2], v_ready[2], v_free[2];  // of even and odd tiles
   uint32_t tmem, failed;
   alignas(16) float neg_ref[N];     // minus the reference of each column, log2 units
   alignas(16) float l_factor[N];    // of the last raise
   alignas(16) float o_factor[N];
   alignas(16) float warp_max[4][N];             // per quarter of the rows; at the end of a piece: sums
-  float warp_v[4], warp_q[8];
+  float warp_v[16], warp_q[20];
   int token[N];                     // the token of a column, counted from the tile's first
   TreeMasks<N> masks;
   TreeBatch batch[2];
-  long long scratch[TREE_THREADS / 32 + 2];
+  long long scratch[32 + 2];
 };
 
 template <int D, int BITS, int N>
@@ -51,27 +53,29 @@ struct TreeLayout {
   static constexpr int DJ = D / 128;
   static constexpr int P = PackedFormat<BITS>::row_bytes(D);
   static constexpr int TILE_BYTES = 128 * P;                   // K rows of a block, or V records
-  static constexpr int STAGE_BYTES = 2 * TILE_BYTES + 2 * 512;
+  static constexpr int BLOCK_BYTES = 2 * TILE_BYTES + 2 * 512; // with the scales
+  static constexpr int BPS = D == 128 ? 2 : 1;                 // blocks of a step: what is waited for once
+  static constexpr int STAGE_BYTES = BPS * BLOCK_BYTES;
   static constexpr int BQ_LBO = N * 16 + 16;                   // bytes between the 8-coordinate groups of B_Q (16 more than they take: no bank conflicts)
   static constexpr int BQ_TERM = D / 8 * BQ_LBO;
   static constexpr int BP_LBO = 128, BP_SBO = 2048;
   static constexpr int BP_TERM = N / 8 * BP_SBO;
   static constexpr int SHARED = (sizeof(TreeShared<N>) + 127) / 128 * 128;
-  static constexpr int FIXED = SHARED + 2 * BP_TERM + 2 * BQ_TERM;
-  static constexpr int CTAS = D == 128 ? 2 : 1;                // per SM
-  static constexpr int ROOM = (228 / CTAS - 1) * 1024;         // shared memory of a CTA
+  static constexpr int FIXED = SHARED + BPS * 2 * BP_TERM + 2 * BQ_TERM;
+  static constexpr int ROOM = 227 * 1024;
   static constexpr int FIT = (ROOM - FIXED) / STAGE_BYTES;
-  static constexpr int STAGES = FIT < 4 ? FIT : 4;
+  static constexpr int STAGES = FIT < TREE_STAGES ? FIT : TREE_STAGES;
   static constexpr int SMEM = FIXED + STAGES * STAGE_BYTES;
-  // tensor memory: K tile (binary16, two to a column), V tile, scores, values
-  static constexpr int COLS = 512 / CTAS;
-  static constexpr int S_BUFS = D / 2 + 64 * DJ + (2 + DJ) * N <= COLS && STAGES >= 3 ? 2 : 1;
-  static constexpr int K_COL = 0, V_COL = D / 2, S_COL = V_COL + 64 * DJ, O_COL = S_COL + S_BUFS * N;
-  // Registers of a thread: at launch 64 where two CTAs share an SM, else 128, four times that over the four groups. A softmax thread holds N
-  // sums and up to 32 scores.
-  static constexpr int SOFTMAX_REGS = CTAS == 1 ? 200 : N == 64 ? 136 : N == 32 ? 112 : 88;
-  static constexpr int OTHER_REGS = (512 / CTAS - SOFTMAX_REGS) / 3 / 8 * 8;
-  static_assert(O_COL + DJ * N <= COLS, "tensor memory");
+  static constexpr int SW = N == 64 ? 4 : 2, NC = N / SW;      // warpgroups of the softmax, columns of a thread
+  static constexpr int SOFTMAX = 128 * SW, THREADS = SOFTMAX + 3 * 128;
+  static constexpr int K_WARP = 4 * SW, V_WARP = K_WARP + 4, QK_WARP = V_WARP + 4, PV_WARP = QK_WARP + 1, LOAD_WARP = QK_WARP + 2, WALK_WARP = QK_WARP + 3;
+  // tensor memory, all 512 columns: K tiles (binary16, two to a column), V tiles, the scores of a step, values; two tiles of a kind where
+  // they fit, so that the next one is dequantised while the products of this one run
+  static constexpr int TILE_COLS = 64 * DJ, S_COLS = BPS * N;
+  static constexpr int V_BUFS = 3 * TILE_COLS + S_COLS + DJ * N <= 512 ? 2 : 1;
+  static constexpr int K_BUFS = (2 + V_BUFS) * TILE_COLS + S_COLS + DJ * N <= 512 ? 2 : 1;
+  static constexpr int K_COL = 0, V_COL = K_BUFS * TILE_COLS, S_COL = V_COL + V_BUFS * TILE_COLS, O_COL = S_COL + S_COLS;
+  static_assert(O_COL + DJ * N <= 512, "tensor memory");
   static_assert(STAGES >= 2 && SMEM <= ROOM, "shared memory");
   // fp32 result, binary16 operands, M = 128; B_Q K-major, B_P MN-major
   static constexpr uint32_t IDESC_Q = (1u << 4) | (((uint32_t)N >> 3) << 17) | ((128u >> 4) << 24);
@@ -80,6 +84,9 @@ struct TreeLayout {
 
 // Bounded wait of a converged warp. A wait that gives up is noted in `failed`, and from then on no wait of the CTA lasts: every thread
 // goes on through the same loops and barriers over whatever is there, so that the CTA ends together.
+__device__ __forceinline__ void tree_wait(uint64_t* bar, uint32_t parity, uint32_t* failed);
+// The wait for tile n on a pair of barriers, one for even and one for odd tiles.
+__device__ __forceinline__ void tree_wait2(uint64_t* bars, uint32_t n, uint32_t* failed) { tree_wait(bars + (n & 1), (n >> 1) & 1, failed); }
 __device__ __forceinline__ void tree_wait(uint64_t* bar, uint32_t parity, uint32_t* failed) {
   for (uint32_t i = 0; !mbar_try_wait(bar, parity); i++)
     if (i >= DEC_WAIT_LIMIT || *(volatile uint32_t*)failed) { *(volatile uint32_t*)failed = 1; break; }
@@ -233,14 +240,13 @@ __device__ __forceinline__ int tree_queries(const TreeParams& p, TreeShared<N>& 
 }
 
 template <int D, int BITS, int N>
-__global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) tree_kernel(const __grid_constant__ TreeParams p) {
+__global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_kernel(const __grid_constant__ TreeParams p) {
   using L = TreeLayout<D, BITS, N>;
-  constexpr int DJ = L::DJ, NST = L::STAGES, SB = L::S_BUFS;
-  constexpr int CH = N < 32 ? N : 32;  // columns that a softmax thread has in registers at a time
+  constexpr int DJ = L::DJ, NST = L::STAGES, NC = L::NC, BPS = L::BPS;
   extern __shared__ __align__(1024) uint8_t smem[];
   TreeShared<N>& s = *reinterpret_cast<TreeShared<N>*>(smem);
   uint8_t* const bp = smem + L::SHARED;
-  uint8_t* const bq = bp + 2 * L::BP_TERM;
+  uint8_t* const bq = bp + BPS * 2 * L::BP_TERM;
   uint8_t* const stages = bq + 2 * L::BQ_TERM;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
 
@@ -249,114 +255,128 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
       mbar_init(&s.full[i], 1);
       mbar_init(&s.taken[i], 1);
     }
-    mbar_init(&s.q_ready, 4);
-    mbar_init(&s.k_ready, 4);
-    mbar_init(&s.v_ready, 4);
-    mbar_init(&s.s_done[0], 1);
-    mbar_init(&s.s_done[1], 1);
-    mbar_init(&s.s_read[0], 4);
-    mbar_init(&s.s_read[1], 4);
-    mbar_init(&s.p_ready, 4);
+    mbar_init(&s.q_ready, 4 * L::SW);
+    mbar_init(&s.s_done, 1);
+    mbar_init(&s.s_read, 4 * L::SW);
+    mbar_init(&s.p_ready, 4 * L::SW);
     mbar_init(&s.o_done, 1);
+    for (int i = 0; i < 2; i++) {
+      mbar_init(&s.k_ready[i], 4);
+      mbar_init(&s.k_free[i], 1);
+      mbar_init(&s.v_ready[i], 4);
+      mbar_init(&s.v_free[i], 1);
+    }
     mbar_init(&s.drain, 2);
     s.failed = 0;
     fence_mbar_init();
     fence_proxy_async();
   }
-  if (warp == 12) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "r"(L::COLS));
+  if (warp == L::QK_WARP) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "r"(512));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
   }
   grid_dependency_wait();
   tc_fence_before();
-  const TreeRange range = tree_range<TREE_THREADS>(p, s.scratch);  // (its barriers also cover the set-up above)
+  const TreeRange range = tree_range<L::THREADS>(p, s.scratch);  // (its barriers also cover the set-up above)
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(FULL, s.tmem, 0);
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the tensor-memory lanes
-  uint32_t i = 0;  // blocks of the CTA so far
+  uint32_t i = 0, n = 0;  // steps and tiles (blocks) of the CTA so far
   // Batch k of pieces is there (false: an empty one, the range is done), and the one before it has been worked off by everybody.
   auto batch = [&](int k) {
-    cta_bar_sync_n(3, TREE_THREADS);
+    cta_bar_sync_n(3, L::THREADS);
     return s.batch[k & 1].pieces != 0;
   };
 
-  if (warp >= 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
-    if (warp == TREE_LOAD_WARP) {
-      // ---- loads: block n into stage n % NST, when the values of block n - NST have been taken (and with them its scores)
+  if (warp >= L::QK_WARP) {
+    if (warp == L::LOAD_WARP) {
+      // ---- loads: step i into stage i % NST, when step i - NST has been taken
       const uint32_t sc_bytes = p.scale_f16 ? 256u : 512u;
       const size_t sc_size = p.scale_f16 ? 2 : 4;
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
         const TreePiece c = s.batch[k & 1].piece[j];
-        for (int v = c.lo; v < c.hi && !tree_failed(&s.failed); v++, i++) {
-          const int st = i % NST;
-          const size_t row0 = cache_row(p.pm, c.b, c.g, (long long)c.sq.block(v) * 128, lane == 0 ? p.status : nullptr);
+        for (int v = c.lo; v < c.hi && !tree_failed(&s.failed); v += BPS, i++) {
+          const int st = i % NST, blocks = min(BPS, c.hi - v);
+          size_t row0[BPS];
+#pragma unroll
+          for (int h = 0; h < BPS; h++) row0[h] = h < blocks ? cache_row(p.pm, c.b, c.g, (long long)c.sq.block(v + h) * 128, lane == 0 ? p.status : nullptr) : 0;
           if (i >= NST) tree_wait(&s.taken[st], (i / NST - 1) & 1, &s.failed);
           if (elect_one()) {
-            uint8_t* const dst = stages + st * L::STAGE_BYTES;
-            mbar_expect_tx(&s.full[st], 2 * L::TILE_BYTES + 2 * sc_bytes);
-            bulk_g2s(dst, p.k_codes + row0 * L::P, L::TILE_BYTES, &s.full[st]);
-            bulk_g2s(dst + 2 * L::TILE_BYTES, reinterpret_cast<const uint8_t*>(p.k_scales) + row0 * sc_size, sc_bytes, &s.full[st]);
-            bulk_g2s(dst + L::TILE_BYTES, p.v_codes + row0 * L::P, L::TILE_BYTES, &s.full[st]);
-            bulk_g2s(dst + 2 * L::TILE_BYTES + 512, reinterpret_cast<const uint8_t*>(p.v_scales) + row0 * sc_size, sc_bytes, &s.full[st]);
+            mbar_expect_tx(&s.full[st], blocks * (2 * L::TILE_BYTES + 2 * sc_bytes));
+            for (int h = 0; h < blocks; h++) {
+              uint8_t* const dst = stages + st * L::STAGE_BYTES + h * L::BLOCK_BYTES;
+              bulk_g2s(dst, p.k_codes + row0[h] * L::P, L::TILE_BYTES, &s.full[st]);
+              bulk_g2s(dst + 2 * L::TILE_BYTES, reinterpret_cast<const uint8_t*>(p.k_scales) + row0[h] * sc_size, sc_bytes, &s.full[st]);
+              bulk_g2s(dst + L::TILE_BYTES, p.v_codes + row0[h] * L::P, L::TILE_BYTES, &s.full[st]);
+              bulk_g2s(dst + 2 * L::TILE_BYTES + 512, reinterpret_cast<const uint8_t*>(p.v_scales) + row0[h] * sc_size, sc_bytes, &s.full[st]);
+            }
           }
           __syncwarp();
         }
       }
       // every copy that was asked for has landed (where no wait gave up: at once)
-      for (uint32_t n = i > NST ? i - NST : 0; n < i; n++) mbar_wait_bounded(&s.full[n % NST], (n / NST) & 1, DEC_WAIT_LIMIT);
-    } else if (warp == TREE_QK_WARP) {
-      // ---- score products, one block ahead of the softmax where there are two buffers for them. (Those of a piece's first block wait for
-      // its queries, which wait for the piece before.)
+      for (uint32_t m = i > NST ? i - NST : 0; m < i; m++) mbar_wait_bounded(&s.full[m % NST], (m / NST) & 1, DEC_WAIT_LIMIT);
+    } else if (warp == L::QK_WARP) {
+      // ---- score products. (Those of a piece's first step wait for its queries, which wait for the piece before.)
       const uint64_t desc = smem_desc_mn(smem_u32(bq), L::BQ_LBO, 128);
       uint32_t pieces = 0;
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
         tree_wait(&s.q_ready, pieces & 1, &s.failed);
         pieces++;
-        for (const uint32_t end = i + s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo; i < end; i++) {
-          if (i >= SB) tree_wait(&s.s_read[(i - SB) & 1], ((i - SB) >> 1) & 1, &s.failed);
-          tree_wait(&s.k_ready, i & 1, &s.failed);
-          tc_fence_after();
-          if (elect_one()) {
-            const uint32_t d = tmem + L::S_COL + (SB == 2 ? (i & 1) * N : 0);
+        const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
+        for (int v = 0; v < total; v += BPS, i++) {
+          if (i > 0) tree_wait(&s.s_read, (i - 1) & 1, &s.failed);  // the scores before have been read
 #pragma unroll 1
-            for (int t = 0; t < 2 * DJ; t++) {  // halves of the coordinates, terms of q~
-              const uint32_t at = (t & (DJ - 1)) * 16 * L::BQ_LBO + t / DJ * L::BQ_TERM;
+          for (int h = 0; h < min(BPS, total - v); h++, n++) {
+            tree_wait2(s.k_ready, n, &s.failed);
+            tc_fence_after();
+            if (elect_one()) {
+              const uint32_t d = tmem + L::S_COL + h * N, a = tmem + L::K_COL + (L::K_BUFS == 2 ? (n & 1) * L::TILE_COLS : 0);
+#pragma unroll 1
+              for (int t = 0; t < 2 * DJ; t++) {  // halves of the coordinates, terms of q~
+                const uint32_t at = (t & (DJ - 1)) * 16 * L::BQ_LBO + t / DJ * L::BQ_TERM;
 #pragma unroll
-              for (int k = 0; k < 8; k++)
-                tc_mma_f16(d, tmem + L::K_COL + (t & (DJ - 1)) * 64 + 8 * k, desc + ((at + 2 * k * L::BQ_LBO) >> 4), L::IDESC_Q, t || k);
+                for (int m = 0; m < 8; m++)
+                  tc_mma_f16(d, a + (t & (DJ - 1)) * 64 + 8 * m, desc + ((at + 2 * m * L::BQ_LBO) >> 4), L::IDESC_Q, t || m);
+              }
+              tc_commit(&s.k_free[n & 1]);
+              if (h + 1 == min(BPS, total - v)) tc_commit(&s.s_done);
             }
-            tc_commit(&s.s_done[i & 1]);
+            __syncwarp();
           }
-          __syncwarp();
         }
       }
-    } else if (warp == TREE_PV_WARP) {
+    } else if (warp == L::PV_WARP) {
       // ---- value products
       const uint64_t desc = smem_desc_mn(smem_u32(bp), L::BP_LBO, L::BP_SBO);
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
-        const uint32_t first = i;
-        for (const uint32_t end = i + s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo; i < end; i++) {
-          tree_wait(&s.v_ready, i & 1, &s.failed);
+        const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
+        for (int v = 0; v < total; v += BPS, i++) {
           tree_wait(&s.p_ready, i & 1, &s.failed);
-          tc_fence_after();
-          if (elect_one()) {
-            mbar_arrive(&s.taken[i % NST]);
 #pragma unroll 1
-            for (int t = 0; t < 2 * DJ; t++) {  // terms of the probabilities, halves of the coordinates
-              const uint32_t h = t >> 1, at = (t & 1) * L::BP_TERM;
+          for (int h = 0; h < min(BPS, total - v); h++, n++) {
+            tree_wait2(s.v_ready, n, &s.failed);
+            tc_fence_after();
+            if (elect_one()) {
+              const bool last = h + 1 == min(BPS, total - v);
+              if (last) mbar_arrive(&s.taken[i % NST]);
+              const uint32_t a = tmem + L::V_COL + (L::V_BUFS == 2 ? (n & 1) * L::TILE_COLS : 0);
+#pragma unroll 1
+              for (int t = 0; t < 2 * DJ; t++) {  // terms of the probabilities, halves of the coordinates
+                const uint32_t x = t >> 1, at = (t & 1) * L::BP_TERM + h * 2 * L::BP_TERM;
 #pragma unroll
-              for (int k = 0; k < 8; k++)
-                tc_mma_f16(tmem + L::O_COL + h * N, tmem + L::V_COL + 64 * h + 8 * k, desc + ((at + 2 * k * L::BP_LBO) >> 4), L::IDESC_P,
-                           i > first || (t & 1) || k);
+                for (int m = 0; m < 8; m++)
+                  tc_mma_f16(tmem + L::O_COL + x * N, a + 64 * x + 8 * m, desc + ((at + 2 * m * L::BP_LBO) >> 4), L::IDESC_P, v + h > 0 || (t & 1) || m);
+              }
+              tc_commit(&s.v_free[n & 1]);
+              if (last) tc_commit(&s.o_done);
             }
-            tc_commit(&s.o_done);
+            __syncwarp();
           }
-          __syncwarp();
         }
       }
     }
-    else if (warp == TREE_WALK_WARP) {
+    else if (warp == L::WALK_WARP) {
       // ---- the pieces
       long long at = range.at, seq_at = range.seq_at;
       int b = range.b;
@@ -364,8 +384,8 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
       if (at < range.end) sq = tree_seq(p, b);
       for (int k = 0;; k++) {
         TreeBatch& out = s.batch[k & 1];
-        int n = 0, blocks = 0;
-        while (n < TREE_BATCH && at < range.end) {
+        int count = 0;
+        while (count < TREE_BATCH && at < range.end) {
           if (at >= seq_at + sq.weight) { seq_at += sq.weight; sq = tree_seq(p, ++b); continue; }
           const int len = sq.blocks + TREE_SEG_COST;
           const int m = (int)((at - seq_at) / len);  // item of the sequence
@@ -383,23 +403,20 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
             p.item_info[item] = info;
           }
           if (lo < hi) {
-            if (lane == 0) out.piece[n] = {sq, b, g, tile, lo, hi, item};
-            n++;
-            blocks += hi - lo;
+            if (lane == 0) out.piece[count] = {sq, b, g, tile, lo, hi, item};
+            count++;
           }
         }
-        if (lane == 0) { out.pieces = n; out.blocks = blocks; }
-        cta_bar_sync_n(3, TREE_THREADS);
-        if (n == 0) break;
+        if (lane == 0) out.pieces = count;
+        cta_bar_sync_n(3, L::THREADS);
+        if (count == 0) break;
       }
     }
-  } else if (warp >= 4) {
-    // ---- dequantisation
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
+  } else if (warp >= L::K_WARP) {
+    // ---- dequantisation. One loop for both sides, and its parts rolled up where they repeat: the code that the SM's warps run side by
+    // side has to fit its instruction cache.
     const int r = tid & 127;
-    const bool k_side = warp < 8;
-    // one loop for both sides (and its parts rolled up where they repeat): the code that the SM's warps run side by side has to fit its
-    // instruction cache
+    const bool k_side = warp < L::V_WARP;
     uint32_t lo[4], hi[4];
 #pragma unroll
     for (int x = 0; x < 4; x++) {
@@ -407,127 +424,147 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
       hi[x] = k_side ? p.lut_hi[x] : p.lut_v_hi[x];
     }
     const uint8_t* const run = stages + (k_side ? r * L::P : L::TILE_BYTES + r * (16 * BITS));
-    const int step = k_side ? 16 * BITS : 128 * 16 * BITS;
-    const uint32_t col = tmem + lanes + (k_side ? L::K_COL : L::V_COL);
-    uint64_t* const ready = k_side ? &s.k_ready : &s.v_ready;
+    const int next = k_side ? 16 * BITS : 128 * 16 * BITS;
+    const uint32_t col = tmem + lanes + (k_side ? L::K_COL : L::V_COL), bufs = k_side ? L::K_BUFS : L::V_BUFS;
+    uint64_t* const ready = k_side ? s.k_ready : s.v_ready;
+    uint64_t* const free_tile = k_side ? s.k_free : s.v_free;
     for (int k = 0; batch(k); k++) {
-     if (k == 0 && !k_side) {  // a hand with the first piece's queries
-      const TreePiece c = s.batch[0].piece[0];
-      const int q0 = c.tile * N;
-      tree_queries<D, BITS, N>(p, s, bq, c, q0, min(N, c.sq.tokens * p.group - q0), warp - 4, 8, 2, 256, lane);
-     }
-     for (const uint32_t end = i + s.batch[k & 1].blocks; i < end; i++) {
-      const uint32_t st = i % NST, before = i - 1;
-      tree_wait(&s.full[st], (i / NST) & 1, &s.failed);
-      // the tile before is read no more
-      if (i > 0) tree_wait(k_side ? &s.s_done[before & 1] : &s.o_done, (k_side ? before >> 1 : before) & 1, &s.failed);
-      tc_fence_after();
+      if (k == 0 && !k_side) {  // a hand with the first piece's queries
+        const TreePiece c = s.batch[0].piece[0];
+        const int q0 = c.tile * N;
+        tree_queries<D, BITS, N>(p, s, bq, c, q0, min(N, c.sq.tokens * p.group - q0), warp - 4, 4 * L::SW + 4, 2, L::SOFTMAX + 128, lane);
+      }
+      for (int j = 0; j < s.batch[k & 1].pieces; j++) {
+        const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
+        for (int v = 0; v < total; v += BPS, i++) {
+          const uint32_t st = i % NST;
+          tree_wait(&s.full[st], (i / NST) & 1, &s.failed);
 #pragma unroll 1
-      for (int j = 0; j < DJ; j++) tree_dequant<BITS>(run + st * L::STAGE_BYTES + j * step, lo, hi, p.lookup, col + 64 * j);
-      tc_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(ready);
-     }
+          for (int h = 0; h < min(BPS, total - v); h++, n++) {
+            if (n >= bufs) tree_wait2(free_tile, n - bufs, &s.failed);  // the tile before is read no more
+            tc_fence_after();
+#pragma unroll 1
+            for (int x = 0; x < DJ; x++)
+              tree_dequant<BITS>(run + st * L::STAGE_BYTES + h * L::BLOCK_BYTES + x * next, lo, hi, p.lookup,
+                                 col + (bufs == 2 ? (n & 1) * L::TILE_COLS : 0) + 64 * x);
+            tc_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ready + (n & 1));
+          }
+        }
+      }
     }
   } else {
     // ---- softmax
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
-    const int r = tid;
-    const uint32_t o_col = tmem + lanes + L::O_COL;
-    uint8_t* const bp_row = bp + (r & 7) * 16 + (r >> 3) * L::BP_LBO;
+    const int r = tid & 127, c0 = (warp >> 2) * NC;  // the thread's row, its first column
+    const uint32_t o_col = tmem + lanes + L::O_COL + c0;
+    uint8_t* const bp_row = bp + c0 / 8 * L::BP_SBO + (r & 7) * 16 + (r >> 3) * L::BP_LBO;
     for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
       const TreePiece c = s.batch[k & 1].piece[j];
       const int q0 = c.tile * N, nq = min(N, c.sq.tokens * p.group - q0), t0 = q0 / p.group;
       if (tid == 0) s.masks.from_max = 0;
-      cta_bar_sync_n(1, 128);  // the last piece's references have been read
-      tree_masks(p, s.masks, c.b, c.sq, t0, (q0 + nq - 1) / p.group - t0 + 1, tid, 128);
+      cta_bar_sync_n(1, L::SOFTMAX);  // the last piece's references have been read
+      tree_masks(p, s.masks, c.b, c.sq, t0, (q0 + nq - 1) / p.group - t0 + 1, tid, L::SOFTMAX);
       if (tid < N) {
         s.neg_ref[tid] = 1e30f;
         s.token[tid] = (q0 + tid) / p.group - t0;
       }
       const bool first = i == 0;
-      const int e2 = tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, first ? 8 : 4, 2, first ? 256 : 128, lane);
+      const int e2 = tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, 4 * L::SW + (first ? 4 : 0), 2, L::SOFTMAX + (first ? 128 : 0), lane);
       if (lane == 0) mbar_arrive(&s.q_ready);
       const float score_unit = p.score_unit * __uint_as_float((uint32_t)(127 - e2) << 23);
 
-      float l[N];
+      float l[NC];
 #pragma unroll
-      for (int n = 0; n < N; n++) l[n] = 0.f;
-      float v_ref = 0.f;  // a power of two at least as large as every V scale so far
-      for (int v = c.lo; v < c.hi; v++, i++) {
+      for (int n = 0; n < NC; n++) l[n] = 0.f;
+      float v_ref = 0.f, v_unit = 0.f;  // a power of two at least as large as every V scale so far; TREE_P_UNIT over it
+      const uint32_t s_col = tmem + lanes + L::S_COL + c0;
+      for (int v = c.lo; v < c.hi; v += BPS, i++) {
         const uint8_t* const st = stages + (i % NST) * L::STAGE_BYTES + 2 * L::TILE_BYTES;
-        const uint32_t s_col = tmem + lanes + L::S_COL + (SB == 2 ? (i & 1) * N : 0);
+        const bool two = BPS == 2 && v + 1 < c.hi;
+        float ks[BPS], vs[BPS];
+        uint32_t sees[BPS];  // bit n: column c0 + n sees the row of block h
+        bool masked = BPS == 2 && !two;
         tree_wait(&s.full[i % NST], (i / NST) & 1, &s.failed);
-        const float ks = load_scale(st, r, p.scale_f16) * score_unit;
-        float vs = load_scale(st + 512, r, p.scale_f16);
-        const int row0 = c.sq.block(v) * 128;
-        const bool masked = row0 + 128 > c.sq.ctx || !(row0 >= s.masks.from_max || row0 + 128 <= p.sinks);
-        uint32_t sees[(N + 31) / 32];  // bit n: column n sees the row
-        if (__builtin_expect(masked, 0)) {
-          bool any = false;
-#pragma unroll 1
-          for (int w = 0; w < (N + 31) / 32; w++) {
-            uint32_t bits = 0;
-#pragma unroll 1
-            for (int n = 0; n < 32 && 32 * w + n < nq; n++)
-              if (tree_sees(s.masks, s.token[32 * w + n], row0 + r, c.sq.ctx, c.sq.rows, p.sinks)) bits |= 1u << n;
-            any = any || bits;
-            if (w == 0) sees[0] = bits;
-            else sees[(N + 31) / 32 - 1] = bits;
-          }
-          if (!any) vs = 0.f;
-        } else {
 #pragma unroll
-          for (int w = 0; w < (N + 31) / 32; w++) sees[w] = 0xFFFFFFFFu;
+        for (int h = 0; h < BPS; h++) {
+          ks[h] = load_scale(st + h * L::BLOCK_BYTES, r, p.scale_f16) * score_unit;
+          vs[h] = load_scale(st + h * L::BLOCK_BYTES + 512, r, p.scale_f16);
+          sees[h] = 0xFFFFFFFFu;
+          const int row0 = c.sq.block(v + h) * 128;
+          masked = masked || row0 + 128 > c.sq.ctx || !(row0 >= s.masks.from_max || row0 + 128 <= p.sinks);
         }
-        const float vs_fin = vs < INFINITY ? vs : 0.f;  // (an infinite or undefined scale is its own row's affair)
-        tree_wait(&s.s_done[i & 1], (i >> 1) & 1, &s.failed);
+        if (__builtin_expect(masked, 0)) {
+#pragma unroll
+          for (int h = 0; h < BPS; h++) {
+            const int row0 = c.sq.block(v + h) * 128;
+            uint32_t bits = 0;
+            if (h == 0 || two) {  // (a step of one block: nobody sees the other)
+#pragma unroll 1
+              for (int m = 0; m < NC && c0 + m < nq; m++)
+                if (tree_sees(s.masks, s.token[c0 + m], row0 + r, c.sq.ctx, c.sq.rows, p.sinks)) bits |= 1u << m;
+            }
+            sees[h] = bits;
+            if (!bits) vs[h] = 0.f;
+          }
+        }
+        float vs_fin = vs[0] < INFINITY ? vs[0] : 0.f;  // (an infinite or undefined scale is its own row's affair)
+        if constexpr (BPS == 2) vs_fin = fmaxf(vs_fin, vs[BPS - 1] < INFINITY ? vs[BPS - 1] : 0.f);
+        tree_wait(&s.s_done, i & 1, &s.failed);
         tc_fence_after();
 
         // scores relative to the references; -inf where the token does not see the row
-        float t[CH];
-        auto relative = [&](int n0) {
-          tree_ld<CH>(s_col + n0, t);
-          const float4* ref = reinterpret_cast<const float4*>(s.neg_ref + n0);
+        float t[BPS][NC];
+        auto relative = [&]() {
 #pragma unroll
-          for (int n = 0; n < CH; n += 4) {
-            const float4 f = ref[n / 4];
-            const F32x2 a = fma2(f32x2(t[n], t[n + 1]), f32x2(ks, ks), f32x2(f.x, f.y)), b = fma2(f32x2(t[n + 2], t[n + 3]), f32x2(ks, ks), f32x2(f.z, f.w));
-            t[n] = a.lo(); t[n + 1] = a.hi(); t[n + 2] = b.lo(); t[n + 3] = b.hi();
-          }
-          if (__builtin_expect(masked, 0)) {
+          for (int h = 0; h < BPS; h++) {
+            tree_ld<NC>(s_col + h * N, t[h]);
+            const float4* ref = reinterpret_cast<const float4*>(s.neg_ref + c0);
 #pragma unroll
-            for (int n = 0; n < CH; n++)
-              if (!(sees[n0 / 32] >> (n % 32) & 1u)) t[n] = -INFINITY;
+            for (int m = 0; m < NC; m += 4) {
+              const float4 f = ref[m / 4];
+              const F32x2 a = fma2(f32x2(t[h][m], t[h][m + 1]), f32x2(ks[h], ks[h]), f32x2(f.x, f.y));
+              const F32x2 b = fma2(f32x2(t[h][m + 2], t[h][m + 3]), f32x2(ks[h], ks[h]), f32x2(f.z, f.w));
+              t[h][m] = a.lo(); t[h][m + 1] = a.hi(); t[h][m + 2] = b.lo(); t[h][m + 3] = b.hi();
+            }
+            if (__builtin_expect(masked, 0)) {
+#pragma unroll
+              for (int m = 0; m < NC; m++)
+                if (!(sees[h] >> m & 1u)) t[h][m] = -INFINITY;
+            }
           }
         };
-        float top = -INFINITY;
+        relative();
+        float top = fmaxf(t[0][0], t[0][1]);
 #pragma unroll
-        for (int n0 = 0; n0 < N; n0 += CH) {
-          relative(n0);
+        for (int h = 0; h < BPS; h++)
 #pragma unroll
-          for (int n = 0; n < CH; n += 2) top = max3f(top, t[n], t[n + 1]);
-        }
-        if (__builtin_expect(cta_bar_or_n(1, 128, top > TREE_RAISE || vs_fin > v_ref), 0)) {
-          // ---- new references: the maximum of each column over the block, and of the V scales
+          for (int m = h ? 0 : 2; m < NC; m += 2) top = max3f(top, t[h][m], t[h][m + 1]);
+        if (__builtin_expect(cta_bar_or_n(1, L::SOFTMAX, top > TREE_RAISE || vs_fin > v_ref), 0)) {
+          // ---- new references: the maximum of each column over the step, and of the V scales
           const float vm = tree_warp_max(vs_fin);
           if (lane == 0) s.warp_v[warp] = vm;
 #pragma unroll 1
-          for (int n0 = 0; n0 < N; n0 += 8) {
-            float z[8];
-            tree_ld<8>(s_col + n0, z);
-            const uint32_t on = (n0 < 32 ? sees[0] : sees[(N + 31) / 32 - 1]) >> (n0 & 31);
-            float m[8];
+          for (int n0 = 0; n0 < NC; n0 += 8) {
+            float z[BPS][8], m[8];
 #pragma unroll
-            for (int n = 0; n < 8; n++) m[n] = tree_warp_max((on >> n & 1u) ? z[n] * ks : -3e38f);
+            for (int h = 0; h < BPS; h++) tree_ld<8>(s_col + h * N + n0, z[h]);
+#pragma unroll
+            for (int x = 0; x < 8; x++) {
+              float y = (sees[0] >> (n0 + x) & 1u) ? z[0][x] * ks[0] : -3e38f;
+              if constexpr (BPS == 2) y = fmaxf(y, (sees[BPS - 1] >> (n0 + x) & 1u) ? z[BPS - 1][x] * ks[BPS - 1] : -3e38f);
+              m[x] = tree_warp_max(y);
+            }
             if (lane == 0) {
-              *reinterpret_cast<float4*>(&s.warp_max[warp][n0]) = make_float4(m[0], m[1], m[2], m[3]);
-              *reinterpret_cast<float4*>(&s.warp_max[warp][n0 + 4]) = make_float4(m[4], m[5], m[6], m[7]);
+              *reinterpret_cast<float4*>(&s.warp_max[warp & 3][c0 + n0]) = make_float4(m[0], m[1], m[2], m[3]);
+              *reinterpret_cast<float4*>(&s.warp_max[warp & 3][c0 + n0 + 4]) = make_float4(m[4], m[5], m[6], m[7]);
             }
           }
-          cta_bar_sync_n(1, 128);
-          float v_new = fmaxf(fmaxf(s.warp_v[0], s.warp_v[1]), fmaxf(s.warp_v[2], s.warp_v[3]));
+          cta_bar_sync_n(1, L::SOFTMAX);
+          float v_new = s.warp_v[0];
+#pragma unroll 1
+          for (int x = 1; x < 4 * L::SW; x++) v_new = fmaxf(v_new, s.warp_v[x]);
           // the power of two at or above it, with room, within 2^-100 .. 2^127
           v_new = v_new > v_ref ? fmaxf(__uint_as_float((__float_as_uint(v_new) + 0x7FFFFFu) & 0x7F800000u) * TREE_V_ROOM, 7.888609e-31f) : v_ref;
           if (!(v_new < INFINITY)) v_new = 1.7014118e38f;
@@ -540,79 +577,80 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
             s.l_factor[tid] = f;
             s.o_factor[tid] = v_new > 0.f ? f * (v_ref / v_new) : f;
           }
-          cta_bar_sync_n(1, 128);
+          cta_bar_sync_n(1, L::SOFTMAX);
           v_ref = v_new;
+          v_unit = v_ref > 0.f ? TREE_P_UNIT / v_ref : 0.f;
 #pragma unroll
-          for (int n = 0; n < N; n += 4) {
-            const float4 f = *reinterpret_cast<const float4*>(s.l_factor + n);
-            l[n] *= f.x; l[n + 1] *= f.y; l[n + 2] *= f.z; l[n + 3] *= f.w;
+          for (int m = 0; m < NC; m += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(s.l_factor + c0 + m);
+            l[m] *= f.x; l[m + 1] *= f.y; l[m + 2] *= f.z; l[m + 3] *= f.w;
           }
           if (v > c.lo) {
             tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
             tc_fence_after();
 #pragma unroll 1
-            for (int n0 = 0; n0 < DJ * N; n0 += 8) {
+            for (int n0 = 0; n0 < DJ * NC; n0 += 8) {
+              const int n1 = n0 & (NC - 1), at = n1 + n0 / NC * N;
               float o[8];
-              tree_ld<8>(o_col + n0, o);
+              tree_ld<8>(o_col + at, o);
 #pragma unroll
-              for (int n = 0; n < 8; n++) o[n] *= s.o_factor[(n0 & (N - 1)) + n];
-              tree_st8(o_col + n0, o);
+              for (int x = 0; x < 8; x++) o[x] *= s.o_factor[c0 + n1 + x];
+              tree_st8(o_col + at, o);
             }
             tc_wait_st();
           }
-          if (CH == N) relative(0);
+          relative();
         }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.s_read);
         // ---- probabilities, and times the V scale as two binary16 terms of the operand B_P
-        if (i > 0) tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
-        const float vn = v_ref > 0.f ? vs * (TREE_P_UNIT / v_ref) : 0.f;
+        if (i > 0) tree_wait(&s.o_done, (i - 1) & 1, &s.failed);  // the probabilities before are read no more
 #pragma unroll
-        for (int n0 = 0; n0 < N; n0 += 8) {
-          if (CH < N && n0 % CH == 0) relative(n0);
-          uint32_t hi[4], lo[4];
+        for (int h = 0; h < BPS; h++) {
+          if (h == 1 && !two) break;
+          const float vn = vs[h] * v_unit;
 #pragma unroll
-          for (int k = 0; k < 4; k++) {
-            const int n = n0 + 2 * k;
-            const float p0 = ex2f(t[n % CH]), p1 = ex2f(t[n % CH + 1]);
-            const F32x2 ls = add2(f32x2(l[n], l[n + 1]), f32x2(p0, p1)), x = mul2(f32x2(p0, p1), f32x2(vn, vn));
-            l[n] = ls.lo();
-            l[n + 1] = ls.hi();
-            hi[k] = pack_half2(x.lo(), x.hi());
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[k]));
-            lo[k] = pack_half2(x.lo() - f.x, x.hi() - f.y);
-          }
-          uint8_t* const dst = bp_row + (n0 / 8) * L::BP_SBO;
-          *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(dst + L::BP_TERM) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        }
-        if (__builtin_expect(masked && vs_fin != vs, 0)) {  // an infinite scale, and tokens that do not see its row: 0 instead of 0 times infinity
-#pragma unroll 1
-          for (int n = 0; n < N; n++)
-            if (!((n < 32 ? sees[0] : sees[(N + 31) / 32 - 1]) >> (n & 31) & 1u)) {
-              uint8_t* const dst = bp_row + (n / 8) * L::BP_SBO + (n & 7) * 2;
-              *reinterpret_cast<uint16_t*>(dst) = 0;
-              *reinterpret_cast<uint16_t*>(dst + L::BP_TERM) = 0;
+          for (int n0 = 0; n0 < NC; n0 += 8) {
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+              const int m = n0 + 2 * x;
+              const float p0 = ex2f(t[h][m]), p1 = ex2f(t[h][m + 1]);
+              const F32x2 ls = add2(f32x2(l[m], l[m + 1]), f32x2(p0, p1)), y = mul2(f32x2(p0, p1), f32x2(vn, vn));
+              l[m] = ls.lo();
+              l[m + 1] = ls.hi();
+              hi[x] = pack_half2(y.lo(), y.hi());
+              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[x]));
+              lo[x] = pack_half2(y.lo() - f.x, y.hi() - f.y);
             }
+            uint8_t* const dst = bp_row + h * 2 * L::BP_TERM + (n0 / 8) * L::BP_SBO;
+            *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(dst + L::BP_TERM) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          }
+          if (__builtin_expect(masked && !(vs[h] < INFINITY), 0)) {  // an infinite scale, and tokens that do not see its row: 0 instead of 0 times infinity
+#pragma unroll 1
+            for (int m = 0; m < NC; m++)
+              if (!(sees[h] >> m & 1u)) {
+                uint8_t* const dst = bp_row + h * 2 * L::BP_TERM + (m / 8) * L::BP_SBO + (m & 7) * 2;
+                *reinterpret_cast<uint16_t*>(dst) = 0;
+                *reinterpret_cast<uint16_t*>(dst + L::BP_TERM) = 0;
+              }
+          }
         }
         fence_proxy_async();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&s.s_read[i & 1]);
-          mbar_arrive(&s.p_ready);
-        }
+        if (lane == 0) mbar_arrive(&s.p_ready);
       }
       // ---- the piece's partial. Sums over the rows: in the warp, then over the four warps, in a fixed order.
       const size_t part = (c.item + blockIdx.x) * N;
-      cta_bar_sync_n(1, 128);  // (warp_max of a raise has been read)
-#pragma unroll
-      for (int n0 = 0; n0 < N; n0 += CH) {
-        float x[CH];
-#pragma unroll
-        for (int n = 0; n < CH; n++) x[n] = l[n0 + n];
-        const float sum = tree_reduce<CH>(x, lane);
-        if (lane % (32 / CH) == 0) s.warp_max[warp][n0 + lane / (32 / CH)] = sum;
+      cta_bar_sync_n(1, L::SOFTMAX);  // (warp_max of a raise has been read)
+      {
+        const float sum = tree_reduce<NC>(l, lane);
+        if (lane % (32 / NC) == 0) s.warp_max[warp & 3][c0 + lane / (32 / NC)] = sum;
       }
-      cta_bar_sync_n(1, 128);
+      cta_bar_sync_n(1, L::SOFTMAX);
       if (tid < nq) {
         const float sum = (s.warp_max[0][tid] + s.warp_max[1][tid]) + (s.warp_max[2][tid] + s.warp_max[3][tid]);
         *reinterpret_cast<float2*>(p.part_ml + 2 * (part + tid)) = make_float2(-s.neg_ref[tid], sum);
@@ -621,15 +659,15 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
       tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
       tc_fence_after();
 #pragma unroll 1
-      for (int j = 0; j < DJ; j++)
+      for (int h = 0; h < DJ; h++)
 #pragma unroll 1
-        for (int n0 = 0; n0 < nq; n0 += 8) {
+        for (int n0 = 0; n0 < NC && c0 + n0 < nq; n0 += 8) {
           float o[8];
-          tree_ld<8>(o_col + j * N + n0, o);
-          float* const dst = p.part_acc + (part + n0) * D + 128 * j + r;
+          tree_ld<8>(o_col + h * N + n0, o);
+          float* const dst = p.part_acc + (part + c0 + n0) * D + 128 * h + r;
 #pragma unroll
           for (int n = 0; n < 8; n++)
-            if (n0 + n < nq) dst[n * D] = o[n] * unit;
+            if (c0 + n0 + n < nq) dst[n * D] = o[n] * unit;
         }
       tc_fence_before();
     }
@@ -639,7 +677,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   __syncthreads();
   if (*(volatile uint32_t*)&s.failed) {  // (nobody writes it any more)
     if (tid == 0 && p.status) atomicOr(&p.status[0], IQ_STATUS_WAIT_TIMEOUT);
-    if (warp == TREE_QK_WARP || warp == TREE_PV_WARP) {  // MMAs may still be running: they are waited for, with a limit, before the tensor memory goes
+    if (warp == L::QK_WARP || warp == L::PV_WARP) {  // MMAs may still be running: they are waited for, with a limit, before the tensor memory goes
       if (elect_one()) tc_commit(&s.drain);
       __syncwarp();
       mbar_wait_bounded(&s.drain, 0u, DEC_WAIT_LIMIT);
@@ -648,7 +686,7 @@ __global__ void __launch_bounds__(TREE_THREADS, (TreeLayout<D, BITS, N>::CTAS)) 
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS));
+  if (warp == L::QK_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
 }
 
 template <int D, int BITS, int N>
@@ -665,7 +703,7 @@ static cudaError_t tree_launch_one(const TreeParams& p, cudaStream_t stream) {
     if (e != cudaSuccess) return e;
     configured[dev] = true;
   }
-  return launch_after_predecessor(kern, dim3(p.ctas), dim3(TREE_THREADS), L::SMEM, stream, p);
+  return launch_after_predecessor(kern, dim3(p.ctas), dim3(L::THREADS), L::SMEM, stream, p);
 }
 template <int BITS>
 static cudaError_t tree_launch(const TreeParams& p, int head_dim, cudaStream_t stream) {
