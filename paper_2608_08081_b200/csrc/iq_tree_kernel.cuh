@@ -34,8 +34,9 @@ struct TreeBatch {
 constexpr int TREE_STAGES = 6;  // at most
 template <int N>
 struct TreeShared {
-  uint64_t full[TREE_STAGES], taken[TREE_STAGES], q_ready, s_done, s_read, p_ready, o_done, drain;
+  uint64_t full[TREE_STAGES], taken[TREE_STAGES], q_ready, s_done, s_read, p_ready, drain;
   uint64_t k_ready[2], k_free[2], v_ready[2], v_free[2];  // of even and odd tiles
+  uint64_t o_done[2];                                     // of even and odd steps
   uint32_t tmem, failed;
   alignas(16) float neg_ref[N];     // minus the reference of each column, log2 units
   alignas(16) float l_factor[N];    // of the last raise
@@ -54,14 +55,16 @@ struct TreeLayout {
   static constexpr int P = PackedFormat<BITS>::row_bytes(D);
   static constexpr int TILE_BYTES = 128 * P;                   // K rows of a block, or V records
   static constexpr int BLOCK_BYTES = 2 * TILE_BYTES + 2 * 512; // with the scales
-  static constexpr int BPS = D == 128 ? 2 : 1;                 // blocks of a step: what is waited for once
+  // blocks of a step, what is waited for once (64 columns and 4-bit tiles leave no room for two)
+  static constexpr int BPS = D == 128 && !(N == 64 && BITS == 4) ? 2 : 1;
   static constexpr int STAGE_BYTES = BPS * BLOCK_BYTES;
   static constexpr int BQ_LBO = N * 16 + 16;                   // bytes between the 8-coordinate groups of B_Q (16 more than they take: no bank conflicts)
   static constexpr int BQ_TERM = D / 8 * BQ_LBO;
   static constexpr int BP_LBO = 128, BP_SBO = 2048;
   static constexpr int BP_TERM = N / 8 * BP_SBO;
   static constexpr int SHARED = (sizeof(TreeShared<N>) + 127) / 128 * 128;
-  static constexpr int FIXED = SHARED + BPS * 2 * BP_TERM + 2 * BQ_TERM;
+  static constexpr int BP_STEP = BPS * 2 * BP_TERM;            // probabilities of a step; two steps' are kept
+  static constexpr int FIXED = SHARED + 2 * BP_STEP + 2 * BQ_TERM;
   static constexpr int ROOM = 227 * 1024;
   static constexpr int FIT = (ROOM - FIXED) / STAGE_BYTES;
   static constexpr int STAGES = FIT < TREE_STAGES ? FIT : TREE_STAGES;
@@ -246,7 +249,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
   extern __shared__ __align__(1024) uint8_t smem[];
   TreeShared<N>& s = *reinterpret_cast<TreeShared<N>*>(smem);
   uint8_t* const bp = smem + L::SHARED;
-  uint8_t* const bq = bp + BPS * 2 * L::BP_TERM;
+  uint8_t* const bq = bp + 2 * L::BP_STEP;
   uint8_t* const stages = bq + 2 * L::BQ_TERM;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
 
@@ -259,12 +262,12 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
     mbar_init(&s.s_done, 1);
     mbar_init(&s.s_read, 4 * L::SW);
     mbar_init(&s.p_ready, 4 * L::SW);
-    mbar_init(&s.o_done, 1);
     for (int i = 0; i < 2; i++) {
       mbar_init(&s.k_ready[i], 4);
       mbar_init(&s.k_free[i], 1);
       mbar_init(&s.v_ready[i], 4);
       mbar_init(&s.v_free[i], 1);
+      mbar_init(&s.o_done[i], 1);
     }
     mbar_init(&s.drain, 2);
     s.failed = 0;
@@ -326,6 +329,8 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
         const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
         for (int v = 0; v < total; v += BPS, i++) {
           if (i > 0) tree_wait(&s.s_read, (i - 1) & 1, &s.failed);  // the scores before have been read
+          // and the probabilities of the step before that: the softmax, which waits for the scores, need not ask
+          if (i > 1) tree_wait2(s.o_done, i - 2, &s.failed);
 #pragma unroll 1
           for (int h = 0; h < min(BPS, total - v); h++, n++) {
             tree_wait2(s.k_ready, n, &s.failed);
@@ -363,13 +368,13 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
               const uint32_t a = tmem + L::V_COL + (L::V_BUFS == 2 ? (n & 1) * L::TILE_COLS : 0);
 #pragma unroll 1
               for (int t = 0; t < 2 * DJ; t++) {  // terms of the probabilities, halves of the coordinates
-                const uint32_t x = t >> 1, at = (t & 1) * L::BP_TERM + h * 2 * L::BP_TERM;
+                const uint32_t x = t >> 1, at = (t & 1) * L::BP_TERM + h * 2 * L::BP_TERM + (i & 1) * L::BP_STEP;
 #pragma unroll
                 for (int m = 0; m < 8; m++)
                   tc_mma_f16(tmem + L::O_COL + x * N, a + 64 * x + 8 * m, desc + ((at + 2 * m * L::BP_LBO) >> 4), L::IDESC_P, v + h > 0 || (t & 1) || m);
               }
               tc_commit(&s.v_free[n & 1]);
-              if (last) tc_commit(&s.o_done);
+              if (last) tc_commit(&s.o_done[i & 1]);
             }
             __syncwarp();
           }
@@ -480,20 +485,22 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
       for (int n = 0; n < NC; n++) l[n] = 0.f;
       float v_ref = 0.f, v_unit = 0.f;  // a power of two at least as large as every V scale so far; TREE_P_UNIT over it
       const uint32_t s_col = tmem + lanes + L::S_COL + c0;
+      // blocks that every token of the tile sees in full (those of the sinks are looked at row by row)
+      const int from_max = s.masks.from_max, all_from = from_max ? max(c.sq.sink_blocks, ((from_max + 127) >> 7) - c.sq.skipped) : 0;
+      const int all_to = (c.sq.ctx >> 7) - c.sq.skipped;
       for (int v = c.lo; v < c.hi; v += BPS, i++) {
         const uint8_t* const st = stages + (i % NST) * L::STAGE_BYTES + 2 * L::TILE_BYTES;
         const bool two = BPS == 2 && v + 1 < c.hi;
         float ks[BPS], vs[BPS];
         uint32_t sees[BPS];  // bit n: column c0 + n sees the row of block h
-        bool masked = BPS == 2 && !two;
-        tree_wait(&s.full[i % NST], (i / NST) & 1, &s.failed);
+        const bool masked = v < all_from || v + BPS > all_to || (BPS == 2 && !two);
+        tree_wait(&s.s_done, i & 1, &s.failed);  // (and with it the step's copies and the room for its probabilities: see the score products)
+        tc_fence_after();
 #pragma unroll
         for (int h = 0; h < BPS; h++) {
           ks[h] = load_scale(st + h * L::BLOCK_BYTES, r, p.scale_f16) * score_unit;
           vs[h] = load_scale(st + h * L::BLOCK_BYTES + 512, r, p.scale_f16);
           sees[h] = 0xFFFFFFFFu;
-          const int row0 = c.sq.block(v + h) * 128;
-          masked = masked || row0 + 128 > c.sq.ctx || !(row0 >= s.masks.from_max || row0 + 128 <= p.sinks);
         }
         if (__builtin_expect(masked, 0)) {
 #pragma unroll
@@ -511,8 +518,6 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
         }
         float vs_fin = vs[0] < INFINITY ? vs[0] : 0.f;  // (an infinite or undefined scale is its own row's affair)
         if constexpr (BPS == 2) vs_fin = fmaxf(vs_fin, vs[BPS - 1] < INFINITY ? vs[BPS - 1] : 0.f);
-        tree_wait(&s.s_done, i & 1, &s.failed);
-        tc_fence_after();
 
         // scores relative to the references; -inf where the token does not see the row
         float t[BPS][NC];
@@ -586,7 +591,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
             l[m] *= f.x; l[m + 1] *= f.y; l[m + 2] *= f.z; l[m + 3] *= f.w;
           }
           if (v > c.lo) {
-            tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
+            tree_wait2(s.o_done, i - 1, &s.failed);
             tc_fence_after();
 #pragma unroll 1
             for (int n0 = 0; n0 < DJ * NC; n0 += 8) {
@@ -605,7 +610,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.s_read);
         // ---- probabilities, and times the V scale as two binary16 terms of the operand B_P
-        if (i > 0) tree_wait(&s.o_done, (i - 1) & 1, &s.failed);  // the probabilities before are read no more
+        uint8_t* const bp_step = bp_row + (i & 1) * L::BP_STEP;
 #pragma unroll
         for (int h = 0; h < BPS; h++) {
           if (h == 1 && !two) break;
@@ -624,7 +629,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
               const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[x]));
               lo[x] = pack_half2(y.lo() - f.x, y.hi() - f.y);
             }
-            uint8_t* const dst = bp_row + h * 2 * L::BP_TERM + (n0 / 8) * L::BP_SBO;
+            uint8_t* const dst = bp_step + h * 2 * L::BP_TERM + (n0 / 8) * L::BP_SBO;
             *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
             *reinterpret_cast<uint4*>(dst + L::BP_TERM) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
           }
@@ -632,7 +637,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
 #pragma unroll 1
             for (int m = 0; m < NC; m++)
               if (!(sees[h] >> m & 1u)) {
-                uint8_t* const dst = bp_row + h * 2 * L::BP_TERM + (m / 8) * L::BP_SBO + (m & 7) * 2;
+                uint8_t* const dst = bp_step + h * 2 * L::BP_TERM + (m / 8) * L::BP_SBO + (m & 7) * 2;
                 *reinterpret_cast<uint16_t*>(dst) = 0;
                 *reinterpret_cast<uint16_t*>(dst + L::BP_TERM) = 0;
               }
@@ -656,7 +661,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
         *reinterpret_cast<float2*>(p.part_ml + 2 * (part + tid)) = make_float2(-s.neg_ref[tid], sum);
       }
       const float unit = p.value_unit * (v_ref / TREE_P_UNIT);
-      tree_wait(&s.o_done, (i - 1) & 1, &s.failed);
+      tree_wait2(s.o_done, i - 1, &s.failed);
       tc_fence_after();
 #pragma unroll 1
       for (int h = 0; h < DJ; h++)
