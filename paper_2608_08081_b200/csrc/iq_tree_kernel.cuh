@@ -34,9 +34,9 @@ struct TreeBatch {
 constexpr int TREE_STAGES = 6;  // at most
 template <int N>
 struct TreeShared {
-  uint64_t full[TREE_STAGES], taken[TREE_STAGES], q_ready, s_done, s_read, p_ready, drain;
+  uint64_t full[TREE_STAGES], taken[TREE_STAGES], q_ready, p_ready, drain;
   uint64_t k_ready[2], k_free[2], v_ready[2], v_free[2];  // of even and odd tiles
-  uint64_t o_done[2];                                     // of even and odd steps
+  uint64_t s_done[2], s_read[2], o_done[2];               // of even and odd steps
   uint32_t tmem, failed;
   alignas(16) float neg_ref[N];     // minus the reference of each column, log2 units
   alignas(16) float l_factor[N];    // of the last raise
@@ -72,12 +72,13 @@ struct TreeLayout {
   static constexpr int SW = N == 64 ? 4 : 2, NC = N / SW;      // warpgroups of the softmax, columns of a thread
   static constexpr int SOFTMAX = 128 * SW, THREADS = SOFTMAX + 3 * 128;
   static constexpr int K_WARP = 4 * SW, V_WARP = K_WARP + 4, QK_WARP = V_WARP + 4, PV_WARP = QK_WARP + 1, LOAD_WARP = QK_WARP + 2, WALK_WARP = QK_WARP + 3;
-  // tensor memory, all 512 columns: K tiles (binary16, two to a column), V tiles, the scores of a step, values; two tiles of a kind where
-  // they fit, so that the next one is dequantised while the products of this one run
+  // tensor memory, all 512 columns: K tiles (binary16, two to a column), V tiles, the scores of a step, values; two of a kind where they
+  // fit, so that the next one is made while this one is used
   static constexpr int TILE_COLS = 64 * DJ, S_COLS = BPS * N;
   static constexpr int V_BUFS = 3 * TILE_COLS + S_COLS + DJ * N <= 512 ? 2 : 1;
   static constexpr int K_BUFS = (2 + V_BUFS) * TILE_COLS + S_COLS + DJ * N <= 512 ? 2 : 1;
-  static constexpr int K_COL = 0, V_COL = K_BUFS * TILE_COLS, S_COL = V_COL + V_BUFS * TILE_COLS, O_COL = S_COL + S_COLS;
+  static constexpr int S_BUFS = (K_BUFS + V_BUFS) * TILE_COLS + 2 * S_COLS + DJ * N <= 512 ? 2 : 1;
+  static constexpr int K_COL = 0, V_COL = K_BUFS * TILE_COLS, S_COL = V_COL + V_BUFS * TILE_COLS, O_COL = S_COL + S_BUFS * S_COLS;
   static_assert(O_COL + DJ * N <= 512, "tensor memory");
   static_assert(STAGES >= 2 && SMEM <= ROOM, "shared memory");
   // fp32 result, binary16 operands, M = 128; B_Q K-major, B_P MN-major
@@ -259,8 +260,6 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
       mbar_init(&s.taken[i], 1);
     }
     mbar_init(&s.q_ready, 4 * L::SW);
-    mbar_init(&s.s_done, 1);
-    mbar_init(&s.s_read, 4 * L::SW);
     mbar_init(&s.p_ready, 4 * L::SW);
     for (int i = 0; i < 2; i++) {
       mbar_init(&s.k_ready[i], 4);
@@ -268,6 +267,8 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
       mbar_init(&s.v_ready[i], 4);
       mbar_init(&s.v_free[i], 1);
       mbar_init(&s.o_done[i], 1);
+      mbar_init(&s.s_done[i], 1);
+      mbar_init(&s.s_read[i], 4 * L::SW);
     }
     mbar_init(&s.drain, 2);
     s.failed = 0;
@@ -328,15 +329,15 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
         pieces++;
         const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
         for (int v = 0; v < total; v += BPS, i++) {
-          if (i > 0) tree_wait(&s.s_read, (i - 1) & 1, &s.failed);  // the scores before have been read
-          // and the probabilities of the step before that: the softmax, which waits for the scores, need not ask
+          if (i >= L::S_BUFS) tree_wait2(s.s_read, i - L::S_BUFS, &s.failed);  // the scores before have been read
+          // and the probabilities of the step before last: the softmax, which waits for the scores, need not ask
           if (i > 1) tree_wait2(s.o_done, i - 2, &s.failed);
 #pragma unroll 1
           for (int h = 0; h < min(BPS, total - v); h++, n++) {
             tree_wait2(s.k_ready, n, &s.failed);
             tc_fence_after();
             if (elect_one()) {
-              const uint32_t d = tmem + L::S_COL + h * N, a = tmem + L::K_COL + (L::K_BUFS == 2 ? (n & 1) * L::TILE_COLS : 0);
+              const uint32_t d = tmem + L::S_COL + (L::S_BUFS == 2 ? (i & 1) * L::S_COLS : 0) + h * N, a = tmem + L::K_COL + (L::K_BUFS == 2 ? (n & 1) * L::TILE_COLS : 0);
 #pragma unroll 1
               for (int t = 0; t < 2 * DJ; t++) {  // halves of the coordinates, terms of q~
                 const uint32_t at = (t & (DJ - 1)) * 16 * L::BQ_LBO + t / DJ * L::BQ_TERM;
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
                   tc_mma_f16(d, a + (t & (DJ - 1)) * 64 + 8 * m, desc + ((at + 2 * m * L::BQ_LBO) >> 4), L::IDESC_Q, t || m);
               }
               tc_commit(&s.k_free[n & 1]);
-              if (h + 1 == min(BPS, total - v)) tc_commit(&s.s_done);
+              if (h + 1 == min(BPS, total - v)) tc_commit(&s.s_done[i & 1]);
             }
             __syncwarp();
           }
@@ -484,17 +485,17 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
 #pragma unroll
       for (int n = 0; n < NC; n++) l[n] = 0.f;
       float v_ref = 0.f, v_unit = 0.f;  // a power of two at least as large as every V scale so far; TREE_P_UNIT over it
-      const uint32_t s_col = tmem + lanes + L::S_COL + c0;
       // blocks that every token of the tile sees in full (those of the sinks are looked at row by row)
       const int from_max = s.masks.from_max, all_from = from_max ? max(c.sq.sink_blocks, ((from_max + 127) >> 7) - c.sq.skipped) : 0;
       const int all_to = (c.sq.ctx >> 7) - c.sq.skipped;
       for (int v = c.lo; v < c.hi; v += BPS, i++) {
         const uint8_t* const st = stages + (i % NST) * L::STAGE_BYTES + 2 * L::TILE_BYTES;
+        const uint32_t s_col = tmem + lanes + L::S_COL + (L::S_BUFS == 2 ? (i & 1) * L::S_COLS : 0) + c0;
         const bool two = BPS == 2 && v + 1 < c.hi;
         float ks[BPS], vs[BPS];
         uint32_t sees[BPS];  // bit n: column c0 + n sees the row of block h
         const bool masked = v < all_from || v + BPS > all_to || (BPS == 2 && !two);
-        tree_wait(&s.s_done, i & 1, &s.failed);  // (and with it the step's copies and the room for its probabilities: see the score products)
+        tree_wait2(s.s_done, i, &s.failed);  // (and with it the step's copies and the room for its probabilities: see the score products)
         tc_fence_after();
 #pragma unroll
         for (int h = 0; h < BPS; h++) {
@@ -608,7 +609,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s.s_read);
+        if (lane == 0) mbar_arrive(&s.s_read[i & 1]);
         // ---- probabilities, and times the V scale as two binary16 terms of the operand B_P
         uint8_t* const bp_step = bp_row + (i & 1) * L::BP_STEP;
 #pragma unroll
