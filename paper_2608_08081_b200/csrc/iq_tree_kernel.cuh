@@ -7,7 +7,7 @@
 
 namespace iq {
 
-// Warpgroups of a CTA: two or four for the softmax (a thread to a cache row, a half or a quarter of the columns each), one that dequantises
+// Warpgroups of a CTA: two for the softmax (a thread to a cache row, half of the columns each), one that dequantises
 // K (a thread to a row), one that dequantises V (a thread to a coordinate), and one of which a warp each issues the score products, issues
 // the value products, loads, and finds the work.
 
@@ -42,7 +42,7 @@ struct TreeShared {
   alignas(16) float l_factor[N];    // of the last raise
   alignas(16) float o_factor[N];
   alignas(16) float warp_max[4][N];             // per quarter of the rows; at the end of a piece: sums
-  float warp_v[16], warp_q[20];
+  float warp_v[8], warp_q[12];
   int token[N];                     // the token of a column, counted from the tile's first
   TreeMasks<N> masks;
   TreeBatch batch[2];
@@ -55,8 +55,9 @@ struct TreeLayout {
   static constexpr int P = PackedFormat<BITS>::row_bytes(D);
   static constexpr int TILE_BYTES = 128 * P;                   // K rows of a block, or V records
   static constexpr int BLOCK_BYTES = 2 * TILE_BYTES + 2 * 512; // with the scales
-  // blocks of a step, what is waited for once (64 columns and 4-bit tiles leave no room for two)
-  static constexpr int BPS = D == 128 && !(N == 64 && BITS == 4) ? 2 : 1;
+  // Blocks of a step, what is waited for once. Two where a block is little work: 16 columns, 16 x 16 K rows, 8 KV heads: 118 us
+  // instead of 146. With 64 columns one is faster (a sequence of 32 K rows and 240 columns: 120 us, with two 132).
+  static constexpr int BPS = D == 128 && N <= 32 ? 2 : 1;
   static constexpr int STAGE_BYTES = BPS * BLOCK_BYTES;
   static constexpr int BQ_LBO = N * 16 + 16;                   // bytes between the 8-coordinate groups of B_Q (16 more than they take: no bank conflicts)
   static constexpr int BQ_TERM = D / 8 * BQ_LBO;
@@ -69,7 +70,9 @@ struct TreeLayout {
   static constexpr int FIT = (ROOM - FIXED) / STAGE_BYTES;
   static constexpr int STAGES = FIT < TREE_STAGES ? FIT : TREE_STAGES;
   static constexpr int SMEM = FIXED + STAGES * STAGE_BYTES;
-  static constexpr int SW = N == 64 ? 4 : 2, NC = N / SW;      // warpgroups of the softmax, columns of a thread
+  // Warpgroups of the softmax, columns of a thread. Every thread has some 150 instructions a block beside those of its columns; a single
+  // group is slower all the same (32 columns: 165 us instead of 144), four are too (64 columns: 132 instead of 120).
+  static constexpr int SW = 2, NC = N / SW;
   static constexpr int SOFTMAX = 128 * SW, THREADS = SOFTMAX + 3 * 128;
   static constexpr int K_WARP = 4 * SW, V_WARP = K_WARP + 4, QK_WARP = V_WARP + 4, PV_WARP = QK_WARP + 1, LOAD_WARP = QK_WARP + 2, WALK_WARP = QK_WARP + 3;
   // tensor memory, all 512 columns: K tiles (binary16, two to a column), V tiles, the scores of a step, values; two of a kind where they
