@@ -24,8 +24,8 @@
  *     `status_dev` array of 4 uint32 (zeroed by the caller): [0] bit mask of IQ_STATUS_* flags,
  *     [1] rows whose codes were re-decided in fp64 (see iq_quantize_append), [2] rows skipped because they fell outside the
  *     cache (the page pool's calls: entries or forks that they could not serve), [3] reserved. Nothing on the device traps or spins without a bound: the waits of the
- *     decode, bulk append and reconstruction kernels on asynchronous copies and tensor-core results give up after 65536 polls
- *     of at most 20 us each (about a second at worst; a wait that works lasts microseconds). Decode and append then flag
+ *     decode, tree attention, bulk append and reconstruction kernels on asynchronous copies and tensor-core results give up after 65536 polls
+ *     of at most 20 us each (about a second at worst; a wait that works lasts microseconds). Decode, tree attention and append then flag
  *     IQ_STATUS_WAIT_TIMEOUT and return with invalid results; iq_reconstruct_rows, which has no status array, writes NaN
  *     to the rows concerned.
  *
@@ -94,7 +94,7 @@ enum {
 
 enum {
   IQ_STATUS_ROW_OUT_OF_RANGE = 1u, /* quantize-append: append_pos + i >= t_cap, row skipped */
-  IQ_STATUS_WAIT_TIMEOUT = 2u,     /* decode, bulk append: a bounded wait on an asynchronous copy or tensor-core result ran out; results invalid */
+  IQ_STATUS_WAIT_TIMEOUT = 2u,     /* decode, tree attention, bulk append: a bounded wait on an asynchronous copy or tensor-core result ran out; results invalid */
   IQ_STATUS_SCALE_OVERFLOW = 8u,   /* binary16 scales: a row norm above 65504 was stored as 65504 */
   IQ_STATUS_BAD_PAGE = 4u,         /* paged cache: a block-table entry outside [0, num_pages) was met: read as page 0 by
                                       decode / tree attention / reconstruct, the rows skipped (and counted in [2]) by quantize-append
@@ -472,18 +472,26 @@ int iq_selftest_bounded_wait(uint32_t* status_dev, uint32_t polls, void* stream)
  *   lse_out        device fp32 [batch][n_tokens_max][n_q_heads] or NULL.
  *   status_dev     optional (see top).
  * Codebooks as for iq_decode_attention. Blocks of 128 rows that no token sees are not read, and their pages need not be in the
- * block table. The cache is read once for up to IQ_TREE_TILE (token, query head) pairs of a KV head, in the order of tokens.
+ * block table. The cache is read once for every 64 (token, query head) pairs of a KV head.
  * The same inputs give the same bits in every call on the same kind of device.
- * Limits: batch * n_kv_heads * ceil(n_tokens_max * heads per KV head / 16) and batch * n_tokens_max * n_q_heads below 2^31
- * (IQ_ERR_LIMIT).
+ * Limits: batch * n_kv_heads * ceil(n_tokens_max * heads per KV head / 16) below 2^31 - 2^20, batch * n_tokens_max * n_q_heads below 2^31,
+ * t_cap at most 2^31 - 513 (IQ_ERR_LIMIT).
  */
 #define IQ_TREE_MAX_TOKENS 256
-size_t iq_tree_workspace_bytes(const iq_shape* shape, int32_t n_tokens_max);
+size_t iq_tree_workspace_bytes(const iq_shape* shape, int32_t n_tokens_max); /* 0: a shape or count that the call refuses */
 int iq_tree_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
                       int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
                       const uint32_t* tree_mask_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int32_t window,
                       int32_t sinks, void* workspace_dev, void* out, int32_t out_is_fp16, float* lse_out, uint32_t* status_dev,
                       void* stream);
+
+/* Diagnostic: the same call with `polls` (0 .. 65536) as the limit of its waits. 0: a wait that does not find what it waits for gives
+ * up at once, IQ_STATUS_WAIT_TIMEOUT is set, copies and MMAs in flight are waited for before the kernel returns; the outputs are invalid. */
+int iq_selftest_tree_wait(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                          int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                          const uint32_t* tree_mask_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int32_t window,
+                          int32_t sinks, void* workspace_dev, void* out, int32_t out_is_fp16, float* lse_out, uint32_t* status_dev,
+                          uint32_t polls, void* stream);
 
 /*
  * Accepting drafted tokens: row base_pos[b] + i of every KV head receives what row base_pos[b] + keep[b][i] held when the call

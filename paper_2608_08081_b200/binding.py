@@ -98,6 +98,7 @@ def _load():
     lib.iq_tree_workspace_bytes.restype = ctypes.c_size_t
     lib.iq_tree_attention.argtypes = [ctypes.POINTER(_IqShape), _vp, ctypes.POINTER(_IqCodebook), _vp, _i64, _i64, _i64,
                                       ctypes.POINTER(_IqCache), _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp]
+    lib.iq_selftest_tree_wait.argtypes = lib.iq_tree_attention.argtypes[:-1] + [ctypes.c_uint32, _vp]
     lib.iq_keep_rows.argtypes = [ctypes.POINTER(_IqShape), ctypes.POINTER(_IqCache), _vp, _vp, _vp, _i32, _vp, _vp]
     lib.iq_page_pool_state_ints.argtypes = [_i32]
     lib.iq_page_pool_state_ints.restype = ctypes.c_size_t
@@ -465,6 +466,15 @@ def iq_selftest_reconstruct_wait(shape: Shape, rot_dev, codebook: Codebook, cach
     _check(_lib.iq_selftest_reconstruct_wait(ctypes.byref(cs), _ptr(rot_dev), ctypes.byref(cb), ctypes.byref(cc), _ptr(seq_lens_dev),
                                              _ptr(k_out), _ptr(v_out), k_out.shape[1], k_out.stride(0), k_out.stride(1), k_out.stride(2),
                                              int(polls), _stream(stream)), "iq_selftest_reconstruct_wait")
+
+
+def iq_selftest_tree_wait(shape: Shape, rot_dev, codebook: Codebook, q, cache: Cache, ctx_lens_dev, tree_mask_dev, n_tokens_dev, workspace, out,
+                          status_dev, polls: int, stream=None) -> None:
+    cs, cb, cc = shape.c(), codebook.c(), cache.c()
+    _check(_lib.iq_selftest_tree_wait(ctypes.byref(cs), _ptr(rot_dev), ctypes.byref(cb), _ptr(q), q.stride(0), q.stride(1), q.stride(2),
+                                      ctypes.byref(cc), _ptr(ctx_lens_dev), _ptr(tree_mask_dev), _ptr(n_tokens_dev), q.shape[1], 0, 0,
+                                      _ptr(workspace), _ptr(out), 1 if out.dtype == torch.float16 else 0, None, _ptr(status_dev), int(polls),
+                                      _stream(stream)), "iq_selftest_tree_wait")
 
 
 def iq_selftest_bounded_wait(status, polls: int, stream=None) -> None:

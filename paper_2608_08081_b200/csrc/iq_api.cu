@@ -854,7 +854,7 @@ int tree_plan(const iq_shape* s, int32_t n_tokens_max, TreePlan& w) {
   const int rc = check_shape(s);
   if (rc) return rc;
   if (n_tokens_max < 0) return IQ_ERR_SHAPE;
-  if (n_tokens_max > IQ_TREE_MAX_TOKENS) return IQ_ERR_LIMIT;
+  if (n_tokens_max > IQ_TREE_MAX_TOKENS || s->t_cap > INT32_MAX - 512) return IQ_ERR_LIMIT;
   const long long queries = (long long)n_tokens_max * (s->n_q_heads / s->n_kv_heads);
   if ((long long)s->batch * s->n_kv_heads * ((queries + 15) / 16) >= (1ll << 31) - (1 << 20) || (long long)s->batch * n_tokens_max * s->n_q_heads >= (1ll << 31))
     return IQ_ERR_LIMIT;
@@ -890,11 +890,11 @@ size_t iq_tree_workspace_bytes(const iq_shape* shape, int32_t n_tokens_max) {
   return tree_plan(shape, n_tokens_max, w) == IQ_OK ? w.total : 0;
 }
 
-int iq_tree_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+static int tree_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
                       int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
                       const uint32_t* tree_mask_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int32_t window,
                       int32_t sinks, void* workspace_dev, void* out, int32_t out_is_fp16, float* lse_out, uint32_t* status_dev,
-                      void* stream) {
+                      uint32_t wait_polls, void* stream) {
   TreePlan w;
   int rc = tree_plan(shape, n_tokens_max, w);
   if (rc) return rc;
@@ -960,7 +960,27 @@ int iq_tree_attention(const iq_shape* shape, const float* rot_dev, const iq_code
   p.out_is_fp16 = out_is_fp16;
   p.lse = lse_out;
   p.status = status_dev;
+  p.wait_polls = wait_polls;
   return iq::launch_tree_attention(p, shape->head_dim, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+int iq_tree_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                      int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                      const uint32_t* tree_mask_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int32_t window,
+                      int32_t sinks, void* workspace_dev, void* out, int32_t out_is_fp16, float* lse_out, uint32_t* status_dev,
+                      void* stream) {
+  return tree_attention(shape, rot_dev, codebook, q, stride_b, stride_t, stride_h, cache, ctx_lens_dev, tree_mask_dev, n_tokens_dev, n_tokens_max,
+                        window, sinks, workspace_dev, out, out_is_fp16, lse_out, status_dev, iq::DEC_WAIT_LIMIT, stream);
+}
+
+int iq_selftest_tree_wait(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                      int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                      const uint32_t* tree_mask_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int32_t window,
+                      int32_t sinks, void* workspace_dev, void* out, int32_t out_is_fp16, float* lse_out, uint32_t* status_dev,
+                      uint32_t polls, void* stream) {
+  if (polls > iq::DEC_WAIT_LIMIT) return IQ_ERR_LIMIT;
+  return tree_attention(shape, rot_dev, codebook, q, stride_b, stride_t, stride_h, cache, ctx_lens_dev, tree_mask_dev, n_tokens_dev, n_tokens_max,
+                        window, sinks, workspace_dev, out, out_is_fp16, lse_out, status_dev, polls, stream);
 }
 
 int iq_keep_rows(const iq_shape* shape, const iq_cache* cache, const int32_t* base_pos_dev, const int32_t* keep_dev,

@@ -204,6 +204,7 @@ struct TreeParams {
   int out_is_fp16;
   float* lse;
   uint32_t* status;
+  uint32_t wait_polls;       // limit of the waits: DEC_WAIT_LIMIT, or what the self-test asks for
 };
 cudaError_t launch_tree_attention(const TreeParams& p, int head_dim, cudaStream_t stream);
 int tree_tile(int head_dim, int queries);  // tile for that many (token, head) pairs of a KV head

@@ -17,7 +17,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
   TreeSeq s;
   s.ctx = max(0, min(p.ctx_lens[b], p.t_cap));
   s.tokens = p.n_tokens ? max(0, min(p.n_tokens[b], p.n_tokens_max)) : p.n_tokens_max;
-  s.rows = min(s.ctx + s.tokens, p.t_cap);
+  s.rows = min(s.ctx + s.tokens, p.t_cap);  // (t_cap + IQ_TREE_MAX_TOKENS fits 31 bits: the host's limit)
   const int total = (s.rows + 127) >> 7;
   s.sink_blocks = total;
   s.skipped = 0;

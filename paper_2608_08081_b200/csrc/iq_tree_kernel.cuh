@@ -91,12 +91,12 @@ struct TreeLayout {
 
 // Bounded wait of a converged warp. A wait that gives up is noted in `failed`, and from then on no wait of the CTA lasts: every thread
 // goes on through the same loops and barriers over whatever is there, so that the CTA ends together.
-__device__ __forceinline__ void tree_wait(uint64_t* bar, uint32_t parity, uint32_t* failed);
+__device__ __forceinline__ void tree_wait(uint64_t* bar, uint32_t parity, uint32_t limit, uint32_t* failed);
 // The wait for tile n on a pair of barriers, one for even and one for odd tiles.
-__device__ __forceinline__ void tree_wait2(uint64_t* bars, uint32_t n, uint32_t* failed) { tree_wait(bars + (n & 1), (n >> 1) & 1, failed); }
-__device__ __forceinline__ void tree_wait(uint64_t* bar, uint32_t parity, uint32_t* failed) {
+__device__ __forceinline__ void tree_wait2(uint64_t* bars, uint32_t n, uint32_t limit, uint32_t* failed) { tree_wait(bars + (n & 1), (n >> 1) & 1, limit, failed); }
+__device__ __forceinline__ void tree_wait(uint64_t* bar, uint32_t parity, uint32_t limit, uint32_t* failed) {
   for (uint32_t i = 0; !mbar_try_wait(bar, parity); i++)
-    if (i >= DEC_WAIT_LIMIT || *(volatile uint32_t*)failed) { *(volatile uint32_t*)failed = 1; break; }
+    if (i >= limit || *(volatile uint32_t*)failed) { *(volatile uint32_t*)failed = 1; break; }
   __syncwarp();
 }
 
@@ -307,7 +307,8 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
           size_t row0[BPS];
 #pragma unroll
           for (int h = 0; h < BPS; h++) row0[h] = h < blocks ? cache_row(p.pm, c.b, c.g, (long long)c.sq.block(v + h) * 128, lane == 0 ? p.status : nullptr) : 0;
-          if (i >= NST) tree_wait(&s.taken[st], (i / NST - 1) & 1, &s.failed);
+          if (i >= NST) tree_wait(&s.taken[st], (i / NST - 1) & 1, p.wait_polls, &s.failed);
+          if (tree_failed(&s.failed)) break;  // (a second load on a barrier that still expects the first is no use to anybody)
           if (elect_one()) {
             mbar_expect_tx(&s.full[st], blocks * (2 * L::TILE_BYTES + 2 * sc_bytes));
             for (int h = 0; h < blocks; h++) {
@@ -328,16 +329,16 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
       const uint64_t desc = smem_desc_mn(smem_u32(bq), L::BQ_LBO, 128);
       uint32_t pieces = 0;
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
-        tree_wait(&s.q_ready, pieces & 1, &s.failed);
+        tree_wait(&s.q_ready, pieces & 1, p.wait_polls, &s.failed);
         pieces++;
         const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
         for (int v = 0; v < total; v += BPS, i++) {
-          if (i >= L::S_BUFS) tree_wait2(s.s_read, i - L::S_BUFS, &s.failed);  // the scores before have been read
+          if (i >= L::S_BUFS) tree_wait2(s.s_read, i - L::S_BUFS, p.wait_polls, &s.failed);  // the scores before have been read
           // and the probabilities of the step before last: the softmax, which waits for the scores, need not ask
-          if (i > 1) tree_wait2(s.o_done, i - 2, &s.failed);
+          if (i > 1) tree_wait2(s.o_done, i - 2, p.wait_polls, &s.failed);
 #pragma unroll 1
           for (int h = 0; h < min(BPS, total - v); h++, n++) {
-            tree_wait2(s.k_ready, n, &s.failed);
+            tree_wait2(s.k_ready, n, p.wait_polls, &s.failed);
             tc_fence_after();
             if (elect_one()) {
               const uint32_t d = tmem + L::S_COL + (L::S_BUFS == 2 ? (i & 1) * L::S_COLS : 0) + h * N, a = tmem + L::K_COL + (L::K_BUFS == 2 ? (n & 1) * L::TILE_COLS : 0);
@@ -361,10 +362,10 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
         const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
         for (int v = 0; v < total; v += BPS, i++) {
-          tree_wait(&s.p_ready, i & 1, &s.failed);
+          tree_wait(&s.p_ready, i & 1, p.wait_polls, &s.failed);
 #pragma unroll 1
           for (int h = 0; h < min(BPS, total - v); h++, n++) {
-            tree_wait2(s.v_ready, n, &s.failed);
+            tree_wait2(s.v_ready, n, p.wait_polls, &s.failed);
             tc_fence_after();
             if (elect_one()) {
               const bool last = h + 1 == min(BPS, total - v);
@@ -447,10 +448,10 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
         const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
         for (int v = 0; v < total; v += BPS, i++) {
           const uint32_t st = i % NST;
-          tree_wait(&s.full[st], (i / NST) & 1, &s.failed);
+          tree_wait(&s.full[st], (i / NST) & 1, p.wait_polls, &s.failed);
 #pragma unroll 1
           for (int h = 0; h < min(BPS, total - v); h++, n++) {
-            if (n >= bufs) tree_wait2(free_tile, n - bufs, &s.failed);  // the tile before is read no more
+            if (n >= bufs) tree_wait2(free_tile, n - bufs, p.wait_polls, &s.failed);  // the tile before is read no more
             tc_fence_after();
 #pragma unroll 1
             for (int x = 0; x < DJ; x++)
@@ -498,7 +499,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
         float ks[BPS], vs[BPS];
         uint32_t sees[BPS];  // bit n: column c0 + n sees the row of block h
         const bool masked = v < all_from || v + BPS > all_to || (BPS == 2 && !two);
-        tree_wait2(s.s_done, i, &s.failed);  // (and with it the step's copies and the room for its probabilities: see the score products)
+        tree_wait2(s.s_done, i, p.wait_polls, &s.failed);  // (and with it the step's copies and the room for its probabilities: see the score products)
         tc_fence_after();
 #pragma unroll
         for (int h = 0; h < BPS; h++) {
@@ -595,7 +596,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
             l[m] *= f.x; l[m + 1] *= f.y; l[m + 2] *= f.z; l[m + 3] *= f.w;
           }
           if (v > c.lo) {
-            tree_wait2(s.o_done, i - 1, &s.failed);
+            tree_wait2(s.o_done, i - 1, p.wait_polls, &s.failed);
             tc_fence_after();
 #pragma unroll 1
             for (int n0 = 0; n0 < DJ * NC; n0 += 8) {
@@ -665,7 +666,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
         *reinterpret_cast<float2*>(p.part_ml + 2 * (part + tid)) = make_float2(-s.neg_ref[tid], sum);
       }
       const float unit = p.value_unit * (v_ref / TREE_P_UNIT);
-      tree_wait2(s.o_done, i - 1, &s.failed);
+      tree_wait2(s.o_done, i - 1, p.wait_polls, &s.failed);
       tc_fence_after();
 #pragma unroll 1
       for (int h = 0; h < DJ; h++)

@@ -35,7 +35,7 @@ def tree(iq, lib, batch=2, heads=8, kv=2, d=128, cap=256, bits=3, cb=None, q=A, 
 
 @pytest.mark.parametrize("kw,code", [
     (dict(d=96), SHAPE), (dict(bits=5), SHAPE), (dict(heads=7), SHAPE), (dict(cap=100), SHAPE), (dict(T=-1), SHAPE), (dict(window=-1), SHAPE),
-    (dict(sinks=-1), SHAPE), (dict(sb=-8), SHAPE), (dict(T=257), LIMIT), (dict(batch=65535, heads=4096, kv=128, T=256), LIMIT),
+    (dict(sinks=-1), SHAPE), (dict(sb=-8), SHAPE), (dict(T=257), LIMIT), (dict(cap=(1 << 31) - 128), LIMIT), (dict(batch=65535, heads=4096, kv=128, T=256), LIMIT),
     (dict(q=None), NULL), (dict(ctx=None), NULL), (dict(ws=None), NULL), (dict(out=None), NULL), (dict(rot=None), NULL),
     (dict(q=A + 2), ALIGN), (dict(ws=A + 8), ALIGN), (dict(out=A + 4), ALIGN), (dict(sh=4), ALIGN), (dict(st=3), ALIGN)])
 def test_tree_refusals(iq, lib, kw, code):

@@ -167,6 +167,8 @@ CASES = [
     dict(T=6, ctx=250, t_cap=256),                       # the last tokens' rows lie outside the cache
     dict(T=4, ctx=400, t_cap=256),
     dict(T=4, ctx=300, sm_scale=0.3),
+    dict(T=1, ctx=200, H=130, hk=1),                     # a token's heads over three passes
+    dict(T=3, ctx=1000, H=22, hk=1),                     # 66 pairs: two left for a second pass
 ]
 WINDOWS = [
     dict(T=1, ctx=3000, window=1000, sinks=4, H=8, hk=2),
@@ -355,6 +357,22 @@ def test_rows_beyond_two_to_the_32_bytes(iq):
     small.call(out)
     torch.cuda.synchronize()
     small.check(out, want=want)
+
+
+@pytest.mark.parametrize("kw", [dict(T=1), dict(T=20, H=8, hk=1), dict(T=40, H=8, hk=2, d=256, bits=4)], ids=["16", "64", "d256"])
+def test_a_wait_that_gives_up_ends_the_call_and_says_so(iq, kw):
+    """With a limit of 0 the first wait whose copy or product is not there yet gives up; the kernel still ends, flags it, and frees what it
+    holds: the next call is right."""
+    c = Case(iq, 18, ctx=3000, **kw).upload()
+    out = torch.zeros((1, c.T, c.H, c.d), device="cuda")
+    iq.iq_selftest_tree_wait(c.shape, c.rot, c.cb, dev(c.q), c.cache, c.ctx_dev, c.mask, c.n_tokens, c.workspace, out, c.status, 0)
+    torch.cuda.synchronize()
+    assert c.status.tolist() == [2, 0, 0, 0]
+    c.status.zero_()
+    c.call(out)
+    torch.cuda.synchronize()
+    assert c.status.tolist() == [0, 0, 0, 0]
+    c.check(out)
 
 
 def test_more_sequences_than_threads(iq):
