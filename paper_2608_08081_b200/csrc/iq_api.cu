@@ -860,7 +860,7 @@ int tree_plan(const iq_shape* s, int32_t n_tokens_max, TreePlan& w) {
     return IQ_ERR_LIMIT;
   w.tile = iq::tree_tile(s->head_dim, (int)queries);
   w.tiles = (int)((queries + w.tile - 1) / w.tile);
-  w.ctas = sm_count();
+  w.ctas = sm_count() * iq::tree_ctas_per_sm(s->head_dim, w.tile);
   w.items = (long long)s->batch * s->n_kv_heads * w.tiles;
   auto up = [](size_t x) { return (x + 15) & ~(size_t)15; };
   const size_t parts = (size_t)(w.items + w.ctas) * w.tile;

@@ -57,7 +57,8 @@ struct TreeLayout {
   static constexpr int BLOCK_BYTES = 2 * TILE_BYTES + 2 * 512; // with the scales
   // Blocks of a step, what is waited for once. Two where a block is little work: 16 columns, 16 x 16 K rows, 8 KV heads: 118 us
   // instead of 146. With 64 columns one is faster (a sequence of 32 K rows and 240 columns: 120 us, with two 132).
-  static constexpr int BPS = D == 128 && N <= 32 ? 2 : 1;
+  static constexpr int CTAS = tree_ctas_per_sm(D, N);
+  static constexpr int BPS = D == 128 && N <= 32 && CTAS == 1 ? 2 : 1;
   static constexpr int STAGE_BYTES = BPS * BLOCK_BYTES;
   static constexpr int BQ_LBO = N * 16 + 16;                   // bytes between the 8-coordinate groups of B_Q (16 more than they take: no bank conflicts)
   static constexpr int BQ_TERM = D / 8 * BQ_LBO;
@@ -66,23 +67,25 @@ struct TreeLayout {
   static constexpr int SHARED = (sizeof(TreeShared<N>) + 127) / 128 * 128;
   static constexpr int BP_STEP = BPS * 2 * BP_TERM;            // probabilities of a step; two steps' are kept
   static constexpr int FIXED = SHARED + 2 * BP_STEP + 2 * BQ_TERM;
-  static constexpr int ROOM = 227 * 1024;
+  static constexpr int ROOM = (228 / CTAS - 1) * 1024;         // shared memory of a CTA
   static constexpr int FIT = (ROOM - FIXED) / STAGE_BYTES;
   static constexpr int STAGES = FIT < TREE_STAGES ? FIT : TREE_STAGES;
   static constexpr int SMEM = FIXED + STAGES * STAGE_BYTES;
   // Warpgroups of the softmax, columns of a thread. Every thread has some 150 instructions a block beside those of its columns; a single
   // group is slower all the same (32 columns: 165 us instead of 144), four are too (64 columns: 132 instead of 120).
-  static constexpr int SW = 2, NC = N / SW;
+  static constexpr int SW = CTAS == 2 ? 1 : 2, NC = N / SW;
   static constexpr int SOFTMAX = 128 * SW, THREADS = SOFTMAX + 3 * 128;
   static constexpr int K_WARP = 4 * SW, V_WARP = K_WARP + 4, QK_WARP = V_WARP + 4, PV_WARP = QK_WARP + 1, LOAD_WARP = QK_WARP + 2, WALK_WARP = QK_WARP + 3;
-  // tensor memory, all 512 columns: K tiles (binary16, two to a column), V tiles, the scores of a step, values; two of a kind where they
+  // Registers of a thread where two CTAs share an SM: 64 at launch, 256 over the four groups.
+  static constexpr int SOFTMAX_REGS = 88, OTHER_REGS = 56;
+  // tensor memory: K tiles (binary16, two to a column), V tiles, the scores of a step, values; two of a kind where they
   // fit, so that the next one is made while this one is used
-  static constexpr int TILE_COLS = 64 * DJ, S_COLS = BPS * N;
-  static constexpr int V_BUFS = 3 * TILE_COLS + S_COLS + DJ * N <= 512 ? 2 : 1;
-  static constexpr int K_BUFS = (2 + V_BUFS) * TILE_COLS + S_COLS + DJ * N <= 512 ? 2 : 1;
-  static constexpr int S_BUFS = (K_BUFS + V_BUFS) * TILE_COLS + 2 * S_COLS + DJ * N <= 512 ? 2 : 1;
+  static constexpr int COLS = 512 / CTAS, TILE_COLS = 64 * DJ, S_COLS = BPS * N;
+  static constexpr int V_BUFS = 3 * TILE_COLS + S_COLS + DJ * N <= COLS ? 2 : 1;
+  static constexpr int K_BUFS = (2 + V_BUFS) * TILE_COLS + S_COLS + DJ * N <= COLS ? 2 : 1;
+  static constexpr int S_BUFS = (K_BUFS + V_BUFS) * TILE_COLS + 2 * S_COLS + DJ * N <= COLS ? 2 : 1;
   static constexpr int K_COL = 0, V_COL = K_BUFS * TILE_COLS, S_COL = V_COL + V_BUFS * TILE_COLS, O_COL = S_COL + S_BUFS * S_COLS;
-  static_assert(O_COL + DJ * N <= 512, "tensor memory");
+  static_assert(O_COL + DJ * N <= COLS, "tensor memory");
   static_assert(STAGES >= 2 && SMEM <= ROOM, "shared memory");
   // fp32 result, binary16 operands, M = 128; B_Q K-major, B_P MN-major
   static constexpr uint32_t IDESC_Q = (1u << 4) | (((uint32_t)N >> 3) << 17) | ((128u >> 4) << 24);
@@ -247,7 +250,7 @@ __device__ __forceinline__ int tree_queries(const TreeParams& p, TreeShared<N>& 
 }
 
 template <int D, int BITS, int N>
-__global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_kernel(const __grid_constant__ TreeParams p) {
+__global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout<D, BITS, N>::CTAS)) tree_kernel(const __grid_constant__ TreeParams p) {
   using L = TreeLayout<D, BITS, N>;
   constexpr int DJ = L::DJ, NST = L::STAGES, NC = L::NC, BPS = L::BPS;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -279,7 +282,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
     fence_proxy_async();
   }
   if (warp == L::QK_WARP) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "r"(512));
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s.tmem)), "r"(L::COLS));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
   }
   grid_dependency_wait();
@@ -296,6 +299,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
   };
 
   if (warp >= L::QK_WARP) {
+    if constexpr (L::CTAS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
     if (warp == L::LOAD_WARP) {
       // ---- loads: step i into stage i % NST, when step i - NST has been taken
       const uint32_t sc_bytes = p.scale_f16 ? 256u : 512u;
@@ -423,6 +427,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
       }
     }
   } else if (warp >= L::K_WARP) {
+    if constexpr (L::CTAS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
     // ---- dequantisation. One loop for both sides, and its parts rolled up where they repeat: the code that the SM's warps run side by
     // side has to fit its instruction cache.
     const int r = tid & 127;
@@ -467,6 +472,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
     }
   } else {
     // ---- softmax
+    if constexpr (L::CTAS == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
     const int r = tid & 127, c0 = (warp >> 2) * NC;  // the thread's row, its first column
     const uint32_t o_col = tmem + lanes + L::O_COL + c0;
     uint8_t* const bp_row = bp + c0 / 8 * L::BP_SBO + (r & 7) * 16 + (r >> 3) * L::BP_LBO;
@@ -696,7 +702,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), 1) tree_ker
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == L::QK_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+  if (warp == L::QK_WARP) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L::COLS));
 }
 
 template <int D, int BITS, int N>
