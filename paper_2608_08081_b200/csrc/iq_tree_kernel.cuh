@@ -27,16 +27,15 @@ struct TreePiece {
 };
 constexpr int TREE_BATCH = 16;
 struct TreeBatch {
-  int pieces;
+  int pieces, blocks;
   TreePiece piece[TREE_BATCH];
 };
 
 constexpr int TREE_STAGES = 6;  // at most
 template <int N>
 struct TreeShared {
-  uint64_t full[TREE_STAGES], taken[TREE_STAGES], q_ready, p_ready, drain;
-  uint64_t k_ready[2], k_free[2], v_ready[2], v_free[2];  // of even and odd tiles
-  uint64_t s_done[2], s_read[2], o_done[2];               // of even and odd steps
+  uint64_t full[TREE_STAGES], taken[TREE_STAGES], q_ready, drain;
+  uint64_t k_ready[2], s_done[2], s_read[2], v_ready[2], p_ready[2], o_done[2];  // of even and odd blocks
   uint32_t tmem, failed;
   alignas(16) float neg_ref[N];     // minus the reference of each column, log2 units
   alignas(16) float l_factor[N];    // of the last raise
@@ -55,36 +54,31 @@ struct TreeLayout {
   static constexpr int P = PackedFormat<BITS>::row_bytes(D);
   static constexpr int TILE_BYTES = 128 * P;                   // K rows of a block, or V records
   static constexpr int BLOCK_BYTES = 2 * TILE_BYTES + 2 * 512; // with the scales
-  // Blocks of a step, what is waited for once. Two where a block is little work: 16 columns, 16 x 16 K rows, 8 KV heads: 118 us
-  // instead of 146. With 64 columns one is faster (a sequence of 32 K rows and 240 columns: 120 us, with two 132).
   static constexpr int CTAS = tree_ctas_per_sm(D, N);
-  static constexpr int BPS = D == 128 && N <= 32 && CTAS == 1 ? 2 : 1;
-  static constexpr int STAGE_BYTES = BPS * BLOCK_BYTES;
   static constexpr int BQ_LBO = N * 16 + 16;                   // bytes between the 8-coordinate groups of B_Q (16 more than they take: no bank conflicts)
   static constexpr int BQ_TERM = D / 8 * BQ_LBO;
   static constexpr int BP_LBO = 128, BP_SBO = 2048;
   static constexpr int BP_TERM = N / 8 * BP_SBO;
   static constexpr int SHARED = (sizeof(TreeShared<N>) + 127) / 128 * 128;
-  static constexpr int BP_STEP = BPS * 2 * BP_TERM;            // probabilities of a step; two steps' are kept
-  static constexpr int FIXED = SHARED + 2 * BP_STEP + 2 * BQ_TERM;
+  static constexpr int FIXED = SHARED + 2 * 2 * BP_TERM + 2 * BQ_TERM;  // the probabilities of two blocks, the queries; two terms each
   static constexpr int ROOM = (228 / CTAS - 1) * 1024;         // shared memory of a CTA
-  static constexpr int FIT = (ROOM - FIXED) / STAGE_BYTES;
+  static constexpr int FIT = (ROOM - FIXED) / BLOCK_BYTES;
   static constexpr int STAGES = FIT < TREE_STAGES ? FIT : TREE_STAGES;
-  static constexpr int SMEM = FIXED + STAGES * STAGE_BYTES;
-  // Warpgroups of the softmax, columns of a thread. Every thread has some 150 instructions a block beside those of its columns; a single
-  // group is slower all the same (32 columns: 165 us instead of 144), four are too (64 columns: 132 instead of 120).
+  static constexpr int SMEM = FIXED + STAGES * BLOCK_BYTES;
+  // Warpgroups of the softmax, columns of a thread. Every thread has some 150 instructions a block beside those of its columns, so four
+  // groups are slower than two (64 columns, a sequence of 32 K rows: 132 us instead of 120).
   static constexpr int SW = CTAS == 2 ? 1 : 2, NC = N / SW;
   static constexpr int SOFTMAX = 128 * SW, THREADS = SOFTMAX + 3 * 128;
   static constexpr int K_WARP = 4 * SW, V_WARP = K_WARP + 4, QK_WARP = V_WARP + 4, PV_WARP = QK_WARP + 1, LOAD_WARP = QK_WARP + 2, WALK_WARP = QK_WARP + 3;
   // Registers of a thread where two CTAs share an SM: 64 at launch, 256 over the four groups.
-  static constexpr int SOFTMAX_REGS = 88, OTHER_REGS = 56;
-  // tensor memory: K tiles (binary16, two to a column), V tiles, the scores of a step, values; two of a kind where they
+  static constexpr int SOFTMAX_REGS = N == 16 ? 88 : 112, OTHER_REGS = N == 16 ? 56 : 48;
+  // tensor memory: K tiles (binary16, two to a column), V tiles, scores, values; two of a kind where they
   // fit, so that the next one is made while this one is used
-  static constexpr int COLS = 512 / CTAS, TILE_COLS = 64 * DJ, S_COLS = BPS * N;
-  static constexpr int V_BUFS = 3 * TILE_COLS + S_COLS + DJ * N <= COLS ? 2 : 1;
-  static constexpr int K_BUFS = (2 + V_BUFS) * TILE_COLS + S_COLS + DJ * N <= COLS ? 2 : 1;
-  static constexpr int S_BUFS = (K_BUFS + V_BUFS) * TILE_COLS + 2 * S_COLS + DJ * N <= COLS ? 2 : 1;
-  static constexpr int K_COL = 0, V_COL = K_BUFS * TILE_COLS, S_COL = V_COL + V_BUFS * TILE_COLS, O_COL = S_COL + S_BUFS * S_COLS;
+  static constexpr int COLS = 512 / CTAS, TILE_COLS = 64 * DJ;
+  static constexpr int V_BUFS = 3 * TILE_COLS + N + DJ * N <= COLS ? 2 : 1;
+  static constexpr int K_BUFS = (2 + V_BUFS) * TILE_COLS + N + DJ * N <= COLS ? 2 : 1;
+  static constexpr int S_BUFS = (K_BUFS + V_BUFS) * TILE_COLS + 2 * N + DJ * N <= COLS ? 2 : 1;
+  static constexpr int K_COL = 0, V_COL = K_BUFS * TILE_COLS, S_COL = V_COL + V_BUFS * TILE_COLS, O_COL = S_COL + S_BUFS * N;
   static_assert(O_COL + DJ * N <= COLS, "tensor memory");
   static_assert(STAGES >= 2 && SMEM <= ROOM, "shared memory");
   // fp32 result, binary16 operands, M = 128; B_Q K-major, B_P MN-major
@@ -95,7 +89,7 @@ struct TreeLayout {
 // Bounded wait of a converged warp. A wait that gives up is noted in `failed`, and from then on no wait of the CTA lasts: every thread
 // goes on through the same loops and barriers over whatever is there, so that the CTA ends together.
 __device__ __forceinline__ void tree_wait(uint64_t* bar, uint32_t parity, uint32_t limit, uint32_t* failed);
-// The wait for tile n on a pair of barriers, one for even and one for odd tiles.
+// The wait for block n on a pair of barriers, one for even and one for odd blocks.
 __device__ __forceinline__ void tree_wait2(uint64_t* bars, uint32_t n, uint32_t limit, uint32_t* failed) { tree_wait(bars + (n & 1), (n >> 1) & 1, limit, failed); }
 __device__ __forceinline__ void tree_wait(uint64_t* bar, uint32_t parity, uint32_t limit, uint32_t* failed) {
   for (uint32_t i = 0; !mbar_try_wait(bar, parity); i++)
@@ -252,11 +246,11 @@ __device__ __forceinline__ int tree_queries(const TreeParams& p, TreeShared<N>& 
 template <int D, int BITS, int N>
 __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout<D, BITS, N>::CTAS)) tree_kernel(const __grid_constant__ TreeParams p) {
   using L = TreeLayout<D, BITS, N>;
-  constexpr int DJ = L::DJ, NST = L::STAGES, NC = L::NC, BPS = L::BPS;
+  constexpr int DJ = L::DJ, NST = L::STAGES, NC = L::NC;
   extern __shared__ __align__(1024) uint8_t smem[];
   TreeShared<N>& s = *reinterpret_cast<TreeShared<N>*>(smem);
   uint8_t* const bp = smem + L::SHARED;
-  uint8_t* const bq = bp + 2 * L::BP_STEP;
+  uint8_t* const bq = bp + 2 * 2 * L::BP_TERM;
   uint8_t* const stages = bq + 2 * L::BQ_TERM;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(FULL, tid >> 5, 0);
 
@@ -266,13 +260,11 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
       mbar_init(&s.taken[i], 1);
     }
     mbar_init(&s.q_ready, 4 * L::SW);
-    mbar_init(&s.p_ready, 4 * L::SW);
     for (int i = 0; i < 2; i++) {
       mbar_init(&s.k_ready[i], 4);
-      mbar_init(&s.k_free[i], 1);
       mbar_init(&s.v_ready[i], 4);
-      mbar_init(&s.v_free[i], 1);
       mbar_init(&s.o_done[i], 1);
+      mbar_init(&s.p_ready[i], 4 * L::SW);
       mbar_init(&s.s_done[i], 1);
       mbar_init(&s.s_read[i], 4 * L::SW);
     }
@@ -291,7 +283,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(FULL, s.tmem, 0);
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the tensor-memory lanes
-  uint32_t i = 0, n = 0;  // steps and tiles (blocks) of the CTA so far
+  uint32_t i = 0;  // blocks of the CTA so far
   // Batch k of pieces is there (false: an empty one, the range is done), and the one before it has been worked off by everybody.
   auto batch = [&](int k) {
     cta_bar_sync_n(3, L::THREADS);
@@ -301,27 +293,23 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
   if (warp >= L::QK_WARP) {
     if constexpr (L::CTAS == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
     if (warp == L::LOAD_WARP) {
-      // ---- loads: step i into stage i % NST, when step i - NST has been taken
+      // ---- loads: block i into stage i % NST, when block i - NST has been taken
       const uint32_t sc_bytes = p.scale_f16 ? 256u : 512u;
       const size_t sc_size = p.scale_f16 ? 2 : 4;
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
         const TreePiece c = s.batch[k & 1].piece[j];
-        for (int v = c.lo; v < c.hi && !tree_failed(&s.failed); v += BPS, i++) {
-          const int st = i % NST, blocks = min(BPS, c.hi - v);
-          size_t row0[BPS];
-#pragma unroll
-          for (int h = 0; h < BPS; h++) row0[h] = h < blocks ? cache_row(p.pm, c.b, c.g, (long long)c.sq.block(v + h) * 128, lane == 0 ? p.status : nullptr) : 0;
+        for (int v = c.lo; v < c.hi && !tree_failed(&s.failed); v++, i++) {
+          const int st = i % NST;
+          const size_t row0 = cache_row(p.pm, c.b, c.g, (long long)c.sq.block(v) * 128, lane == 0 ? p.status : nullptr);
           if (i >= NST) tree_wait(&s.taken[st], (i / NST - 1) & 1, p.wait_polls, &s.failed);
           if (tree_failed(&s.failed)) break;  // (a second load on a barrier that still expects the first is no use to anybody)
           if (elect_one()) {
-            mbar_expect_tx(&s.full[st], blocks * (2 * L::TILE_BYTES + 2 * sc_bytes));
-            for (int h = 0; h < blocks; h++) {
-              uint8_t* const dst = stages + st * L::STAGE_BYTES + h * L::BLOCK_BYTES;
-              bulk_g2s(dst, p.k_codes + row0[h] * L::P, L::TILE_BYTES, &s.full[st]);
-              bulk_g2s(dst + 2 * L::TILE_BYTES, reinterpret_cast<const uint8_t*>(p.k_scales) + row0[h] * sc_size, sc_bytes, &s.full[st]);
-              bulk_g2s(dst + L::TILE_BYTES, p.v_codes + row0[h] * L::P, L::TILE_BYTES, &s.full[st]);
-              bulk_g2s(dst + 2 * L::TILE_BYTES + 512, reinterpret_cast<const uint8_t*>(p.v_scales) + row0[h] * sc_size, sc_bytes, &s.full[st]);
-            }
+            uint8_t* const dst = stages + st * L::BLOCK_BYTES;
+            mbar_expect_tx(&s.full[st], 2 * L::TILE_BYTES + 2 * sc_bytes);
+            bulk_g2s(dst, p.k_codes + row0 * L::P, L::TILE_BYTES, &s.full[st]);
+            bulk_g2s(dst + 2 * L::TILE_BYTES, reinterpret_cast<const uint8_t*>(p.k_scales) + row0 * sc_size, sc_bytes, &s.full[st]);
+            bulk_g2s(dst + L::TILE_BYTES, p.v_codes + row0 * L::P, L::TILE_BYTES, &s.full[st]);
+            bulk_g2s(dst + 2 * L::TILE_BYTES + 512, reinterpret_cast<const uint8_t*>(p.v_scales) + row0 * sc_size, sc_bytes, &s.full[st]);
           }
           __syncwarp();
         }
@@ -329,64 +317,54 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
       // every copy that was asked for has landed (where no wait gave up: at once)
       for (uint32_t m = i > NST ? i - NST : 0; m < i; m++) mbar_wait_bounded(&s.full[m % NST], (m / NST) & 1, DEC_WAIT_LIMIT);
     } else if (warp == L::QK_WARP) {
-      // ---- score products. (Those of a piece's first step wait for its queries, which wait for the piece before.)
+      // ---- score products. (Those of a piece's first block wait for its queries, which wait for the piece before.)
       const uint64_t desc = smem_desc_mn(smem_u32(bq), L::BQ_LBO, 128);
       uint32_t pieces = 0;
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
         tree_wait(&s.q_ready, pieces & 1, p.wait_polls, &s.failed);
         pieces++;
-        const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
-        for (int v = 0; v < total; v += BPS, i++) {
+        for (const uint32_t end = i + s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo; i < end; i++) {
           if (i >= L::S_BUFS) tree_wait2(s.s_read, i - L::S_BUFS, p.wait_polls, &s.failed);  // the scores before have been read
-          // and the probabilities of the step before last: the softmax, which waits for the scores, need not ask
+          // and the probabilities of the block before last: the softmax, which waits for the scores, need not ask
           if (i > 1) tree_wait2(s.o_done, i - 2, p.wait_polls, &s.failed);
+          tree_wait2(s.k_ready, i, p.wait_polls, &s.failed);
+          tc_fence_after();
+          if (elect_one()) {
+            const uint32_t d = tmem + L::S_COL + (L::S_BUFS == 2 ? (i & 1) * N : 0), a = tmem + L::K_COL + (L::K_BUFS == 2 ? (i & 1) * L::TILE_COLS : 0);
 #pragma unroll 1
-          for (int h = 0; h < min(BPS, total - v); h++, n++) {
-            tree_wait2(s.k_ready, n, p.wait_polls, &s.failed);
-            tc_fence_after();
-            if (elect_one()) {
-              const uint32_t d = tmem + L::S_COL + (L::S_BUFS == 2 ? (i & 1) * L::S_COLS : 0) + h * N, a = tmem + L::K_COL + (L::K_BUFS == 2 ? (n & 1) * L::TILE_COLS : 0);
-#pragma unroll 1
-              for (int t = 0; t < 2 * DJ; t++) {  // halves of the coordinates, terms of q~
-                const uint32_t at = (t & (DJ - 1)) * 16 * L::BQ_LBO + t / DJ * L::BQ_TERM;
+            for (int t = 0; t < 2 * DJ; t++) {  // halves of the coordinates, terms of q~
+              const uint32_t at = (t & (DJ - 1)) * 16 * L::BQ_LBO + t / DJ * L::BQ_TERM;
 #pragma unroll
-                for (int m = 0; m < 8; m++)
-                  tc_mma_f16(d, a + (t & (DJ - 1)) * 64 + 8 * m, desc + ((at + 2 * m * L::BQ_LBO) >> 4), L::IDESC_Q, t || m);
-              }
-              tc_commit(&s.k_free[n & 1]);
-              if (h + 1 == min(BPS, total - v)) tc_commit(&s.s_done[i & 1]);
+              for (int m = 0; m < 8; m++)
+                tc_mma_f16(d, a + (t & (DJ - 1)) * 64 + 8 * m, desc + ((at + 2 * m * L::BQ_LBO) >> 4), L::IDESC_Q, t || m);
             }
-            __syncwarp();
+            tc_commit(&s.s_done[i & 1]);
           }
+          __syncwarp();
         }
       }
     } else if (warp == L::PV_WARP) {
       // ---- value products
       const uint64_t desc = smem_desc_mn(smem_u32(bp), L::BP_LBO, L::BP_SBO);
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
-        const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
-        for (int v = 0; v < total; v += BPS, i++) {
-          tree_wait(&s.p_ready, i & 1, p.wait_polls, &s.failed);
+        const uint32_t first = i;
+        for (const uint32_t end = i + s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo; i < end; i++) {
+          tree_wait2(s.p_ready, i, p.wait_polls, &s.failed);
+          tree_wait2(s.v_ready, i, p.wait_polls, &s.failed);
+          tc_fence_after();
+          if (elect_one()) {
+            mbar_arrive(&s.taken[i % NST]);
+            const uint32_t a = tmem + L::V_COL + (L::V_BUFS == 2 ? (i & 1) * L::TILE_COLS : 0);
 #pragma unroll 1
-          for (int h = 0; h < min(BPS, total - v); h++, n++) {
-            tree_wait2(s.v_ready, n, p.wait_polls, &s.failed);
-            tc_fence_after();
-            if (elect_one()) {
-              const bool last = h + 1 == min(BPS, total - v);
-              if (last) mbar_arrive(&s.taken[i % NST]);
-              const uint32_t a = tmem + L::V_COL + (L::V_BUFS == 2 ? (n & 1) * L::TILE_COLS : 0);
-#pragma unroll 1
-              for (int t = 0; t < 2 * DJ; t++) {  // terms of the probabilities, halves of the coordinates
-                const uint32_t x = t >> 1, at = (t & 1) * L::BP_TERM + h * 2 * L::BP_TERM + (i & 1) * L::BP_STEP;
+            for (int t = 0; t < 2 * DJ; t++) {  // terms of the probabilities, halves of the coordinates
+              const uint32_t x = t >> 1, at = ((t & 1) + 2 * (i & 1)) * L::BP_TERM;
 #pragma unroll
-                for (int m = 0; m < 8; m++)
-                  tc_mma_f16(tmem + L::O_COL + x * N, a + 64 * x + 8 * m, desc + ((at + 2 * m * L::BP_LBO) >> 4), L::IDESC_P, v + h > 0 || (t & 1) || m);
-              }
-              tc_commit(&s.v_free[n & 1]);
-              if (last) tc_commit(&s.o_done[i & 1]);
+              for (int m = 0; m < 8; m++)
+                tc_mma_f16(tmem + L::O_COL + x * N, a + 64 * x + 8 * m, desc + ((at + 2 * m * L::BP_LBO) >> 4), L::IDESC_P, i > first || (t & 1) || m);
             }
-            __syncwarp();
+            tc_commit(&s.o_done[i & 1]);
           }
+          __syncwarp();
         }
       }
     }
@@ -398,7 +376,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
       if (at < range.end) sq = tree_seq(p, b);
       for (int k = 0;; k++) {
         TreeBatch& out = s.batch[k & 1];
-        int count = 0;
+        int count = 0, blocks = 0;
         while (count < TREE_BATCH && at < range.end) {
           if (at >= seq_at + sq.weight) { seq_at += sq.weight; sq = tree_seq(p, ++b); continue; }
           const int len = sq.blocks + TREE_SEG_COST;
@@ -419,9 +397,10 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
           if (lo < hi) {
             if (lane == 0) out.piece[count] = {sq, b, g, tile, lo, hi, item};
             count++;
+            blocks += hi - lo;
           }
         }
-        if (lane == 0) out.pieces = count;
+        if (lane == 0) { out.pieces = count; out.blocks = blocks; }
         cta_bar_sync_n(3, L::THREADS);
         if (count == 0) break;
       }
@@ -442,32 +421,25 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
     const int next = k_side ? 16 * BITS : 128 * 16 * BITS;
     const uint32_t col = tmem + lanes + (k_side ? L::K_COL : L::V_COL), bufs = k_side ? L::K_BUFS : L::V_BUFS;
     uint64_t* const ready = k_side ? s.k_ready : s.v_ready;
-    uint64_t* const free_tile = k_side ? s.k_free : s.v_free;
+    uint64_t* const used = k_side ? s.s_done : s.o_done;
     for (int k = 0; batch(k); k++) {
       if (k == 0 && !k_side) {  // a hand with the first piece's queries
         const TreePiece c = s.batch[0].piece[0];
         const int q0 = c.tile * N;
         tree_queries<D, BITS, N>(p, s, bq, c, q0, min(N, c.sq.tokens * p.group - q0), warp - 4, 4 * L::SW + 4, 2, L::SOFTMAX + 128, lane);
       }
-      for (int j = 0; j < s.batch[k & 1].pieces; j++) {
-        const int total = s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo;
-        for (int v = 0; v < total; v += BPS, i++) {
-          const uint32_t st = i % NST;
-          tree_wait(&s.full[st], (i / NST) & 1, p.wait_polls, &s.failed);
+      for (const uint32_t end = i + s.batch[k & 1].blocks; i < end; i++) {
+        const uint32_t st = i % NST;
+        tree_wait(&s.full[st], (i / NST) & 1, p.wait_polls, &s.failed);
+        if (i >= bufs) tree_wait2(used, i - bufs, p.wait_polls, &s.failed);  // the tile before is read no more
+        tc_fence_after();
 #pragma unroll 1
-          for (int h = 0; h < min(BPS, total - v); h++, n++) {
-            if (n >= bufs) tree_wait2(free_tile, n - bufs, p.wait_polls, &s.failed);  // the tile before is read no more
-            tc_fence_after();
-#pragma unroll 1
-            for (int x = 0; x < DJ; x++)
-              tree_dequant<BITS>(run + st * L::STAGE_BYTES + h * L::BLOCK_BYTES + x * next, lo, hi, p.lookup,
-                                 col + (bufs == 2 ? (n & 1) * L::TILE_COLS : 0) + 64 * x);
-            tc_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ready + (n & 1));
-          }
-        }
+        for (int x = 0; x < DJ; x++)
+          tree_dequant<BITS>(run + st * L::BLOCK_BYTES + x * next, lo, hi, p.lookup, col + (bufs == 2 ? (i & 1) * L::TILE_COLS : 0) + 64 * x);
+        tc_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ready + (i & 1));
       }
     }
   } else {
@@ -498,80 +470,56 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
       // blocks that every token of the tile sees in full (those of the sinks are looked at row by row)
       const int from_max = s.masks.from_max, all_from = from_max ? max(c.sq.sink_blocks, ((from_max + 127) >> 7) - c.sq.skipped) : 0;
       const int all_to = (c.sq.ctx >> 7) - c.sq.skipped;
-      for (int v = c.lo; v < c.hi; v += BPS, i++) {
-        const uint8_t* const st = stages + (i % NST) * L::STAGE_BYTES + 2 * L::TILE_BYTES;
-        const uint32_t s_col = tmem + lanes + L::S_COL + (L::S_BUFS == 2 ? (i & 1) * L::S_COLS : 0) + c0;
-        const bool two = BPS == 2 && v + 1 < c.hi;
-        float ks[BPS], vs[BPS];
-        uint32_t sees[BPS];  // bit n: column c0 + n sees the row of block h
-        const bool masked = v < all_from || v + BPS > all_to || (BPS == 2 && !two);
-        tree_wait2(s.s_done, i, p.wait_polls, &s.failed);  // (and with it the step's copies and the room for its probabilities: see the score products)
+      for (int v = c.lo; v < c.hi; v++, i++) {
+        const uint8_t* const st = stages + (i % NST) * L::BLOCK_BYTES + 2 * L::TILE_BYTES;
+        const uint32_t s_col = tmem + lanes + L::S_COL + (L::S_BUFS == 2 ? (i & 1) * N : 0) + c0;
+        const bool masked = v < all_from || v >= all_to;
+        tree_wait2(s.s_done, i, p.wait_polls, &s.failed);  // (and with it the block's copies and the room for its probabilities: see the score products)
         tc_fence_after();
-#pragma unroll
-        for (int h = 0; h < BPS; h++) {
-          ks[h] = load_scale(st + h * L::BLOCK_BYTES, r, p.scale_f16) * score_unit;
-          vs[h] = load_scale(st + h * L::BLOCK_BYTES + 512, r, p.scale_f16);
-          sees[h] = 0xFFFFFFFFu;
-        }
+        const float ks = load_scale(st, r, p.scale_f16) * score_unit;
+        float vs = load_scale(st + 512, r, p.scale_f16);
+        uint32_t sees = 0xFFFFFFFFu;  // bit n: column c0 + n sees the row
         if (__builtin_expect(masked, 0)) {
-#pragma unroll
-          for (int h = 0; h < BPS; h++) {
-            const int row0 = c.sq.block(v + h) * 128;
-            uint32_t bits = 0;
-            if (h == 0 || two) {  // (a step of one block: nobody sees the other)
+          const int row = c.sq.block(v) * 128 + r;
+          sees = 0;
 #pragma unroll 1
-              for (int m = 0; m < NC && c0 + m < nq; m++)
-                if (tree_sees(s.masks, s.token[c0 + m], row0 + r, c.sq.ctx, c.sq.rows, p.sinks)) bits |= 1u << m;
-            }
-            sees[h] = bits;
-            if (!bits) vs[h] = 0.f;
-          }
+          for (int m = 0; m < NC && c0 + m < nq; m++)
+            if (tree_sees(s.masks, s.token[c0 + m], row, c.sq.ctx, c.sq.rows, p.sinks)) sees |= 1u << m;
+          if (!sees) vs = 0.f;
         }
-        float vs_fin = vs[0] < INFINITY ? vs[0] : 0.f;  // (an infinite or undefined scale is its own row's affair)
-        if constexpr (BPS == 2) vs_fin = fmaxf(vs_fin, vs[BPS - 1] < INFINITY ? vs[BPS - 1] : 0.f);
+        const float vs_fin = vs < INFINITY ? vs : 0.f;  // (an infinite or undefined scale is its own row's affair)
 
         // scores relative to the references; -inf where the token does not see the row
-        float t[BPS][NC];
+        float t[NC];
         auto relative = [&]() {
+          tree_ld<NC>(s_col, t);
+          const float4* ref = reinterpret_cast<const float4*>(s.neg_ref + c0);
 #pragma unroll
-          for (int h = 0; h < BPS; h++) {
-            tree_ld<NC>(s_col + h * N, t[h]);
-            const float4* ref = reinterpret_cast<const float4*>(s.neg_ref + c0);
+          for (int m = 0; m < NC; m += 4) {
+            const float4 f = ref[m / 4];
+            const F32x2 a = fma2(f32x2(t[m], t[m + 1]), f32x2(ks, ks), f32x2(f.x, f.y)), b = fma2(f32x2(t[m + 2], t[m + 3]), f32x2(ks, ks), f32x2(f.z, f.w));
+            t[m] = a.lo(); t[m + 1] = a.hi(); t[m + 2] = b.lo(); t[m + 3] = b.hi();
+          }
+          if (__builtin_expect(masked, 0)) {
 #pragma unroll
-            for (int m = 0; m < NC; m += 4) {
-              const float4 f = ref[m / 4];
-              const F32x2 a = fma2(f32x2(t[h][m], t[h][m + 1]), f32x2(ks[h], ks[h]), f32x2(f.x, f.y));
-              const F32x2 b = fma2(f32x2(t[h][m + 2], t[h][m + 3]), f32x2(ks[h], ks[h]), f32x2(f.z, f.w));
-              t[h][m] = a.lo(); t[h][m + 1] = a.hi(); t[h][m + 2] = b.lo(); t[h][m + 3] = b.hi();
-            }
-            if (__builtin_expect(masked, 0)) {
-#pragma unroll
-              for (int m = 0; m < NC; m++)
-                if (!(sees[h] >> m & 1u)) t[h][m] = -INFINITY;
-            }
+            for (int m = 0; m < NC; m++)
+              if (!(sees >> m & 1u)) t[m] = -INFINITY;
           }
         };
         relative();
-        float top = fmaxf(t[0][0], t[0][1]);
+        float top = fmaxf(t[0], t[1]);
 #pragma unroll
-        for (int h = 0; h < BPS; h++)
-#pragma unroll
-          for (int m = h ? 0 : 2; m < NC; m += 2) top = max3f(top, t[h][m], t[h][m + 1]);
+        for (int m = 2; m < NC; m += 2) top = max3f(top, t[m], t[m + 1]);
         if (__builtin_expect(cta_bar_or_n(1, L::SOFTMAX, top > TREE_RAISE || vs_fin > v_ref), 0)) {
-          // ---- new references: the maximum of each column over the step, and of the V scales
+          // ---- new references: the maximum of each column over the block, and of the V scales
           const float vm = tree_warp_max(vs_fin);
           if (lane == 0) s.warp_v[warp] = vm;
 #pragma unroll 1
           for (int n0 = 0; n0 < NC; n0 += 8) {
-            float z[BPS][8], m[8];
+            float z[8], m[8];
+            tree_ld<8>(s_col + n0, z);
 #pragma unroll
-            for (int h = 0; h < BPS; h++) tree_ld<8>(s_col + h * N + n0, z[h]);
-#pragma unroll
-            for (int x = 0; x < 8; x++) {
-              float y = (sees[0] >> (n0 + x) & 1u) ? z[0][x] * ks[0] : -3e38f;
-              if constexpr (BPS == 2) y = fmaxf(y, (sees[BPS - 1] >> (n0 + x) & 1u) ? z[BPS - 1][x] * ks[BPS - 1] : -3e38f);
-              m[x] = tree_warp_max(y);
-            }
+            for (int x = 0; x < 8; x++) m[x] = tree_warp_max((sees >> (n0 + x) & 1u) ? z[x] * ks : -3e38f);
             if (lane == 0) {
               *reinterpret_cast<float4*>(&s.warp_max[warp & 3][c0 + n0]) = make_float4(m[0], m[1], m[2], m[3]);
               *reinterpret_cast<float4*>(&s.warp_max[warp & 3][c0 + n0 + 4]) = make_float4(m[4], m[5], m[6], m[7]);
@@ -621,43 +569,39 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.s_read[i & 1]);
         // ---- probabilities, and times the V scale as two binary16 terms of the operand B_P
-        uint8_t* const bp_step = bp_row + (i & 1) * L::BP_STEP;
+        uint8_t* const bp_block = bp_row + (i & 1) * 2 * L::BP_TERM;
+        const float vn = vs * v_unit;
 #pragma unroll
-        for (int h = 0; h < BPS; h++) {
-          if (h == 1 && !two) break;
-          const float vn = vs[h] * v_unit;
+        for (int n0 = 0; n0 < NC; n0 += 8) {
+          uint32_t hi[4], lo[4];
 #pragma unroll
-          for (int n0 = 0; n0 < NC; n0 += 8) {
-            uint32_t hi[4], lo[4];
-#pragma unroll
-            for (int x = 0; x < 4; x++) {
-              const int m = n0 + 2 * x;
-              const float p0 = ex2f(t[h][m]), p1 = ex2f(t[h][m + 1]);
-              const F32x2 ls = add2(f32x2(l[m], l[m + 1]), f32x2(p0, p1)), y = mul2(f32x2(p0, p1), f32x2(vn, vn));
-              l[m] = ls.lo();
-              l[m + 1] = ls.hi();
-              hi[x] = pack_half2(y.lo(), y.hi());
-              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[x]));
-              lo[x] = pack_half2(y.lo() - f.x, y.hi() - f.y);
-            }
-            uint8_t* const dst = bp_step + h * 2 * L::BP_TERM + (n0 / 8) * L::BP_SBO;
-            *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4*>(dst + L::BP_TERM) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          for (int x = 0; x < 4; x++) {
+            const int m = n0 + 2 * x;
+            const float p0 = ex2f(t[m]), p1 = ex2f(t[m + 1]);
+            const F32x2 ls = add2(f32x2(l[m], l[m + 1]), f32x2(p0, p1)), y = mul2(f32x2(p0, p1), f32x2(vn, vn));
+            l[m] = ls.lo();
+            l[m + 1] = ls.hi();
+            hi[x] = pack_half2(y.lo(), y.hi());
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[x]));
+            lo[x] = pack_half2(y.lo() - f.x, y.hi() - f.y);
           }
-          if (__builtin_expect(masked && !(vs[h] < INFINITY), 0)) {  // an infinite scale, and tokens that do not see its row: 0 instead of 0 times infinity
+          uint8_t* const dst = bp_block + (n0 / 8) * L::BP_SBO;
+          *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(dst + L::BP_TERM) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        }
+        if (__builtin_expect(masked && !(vs < INFINITY), 0)) {  // an infinite scale, and tokens that do not see its row: 0 instead of 0 times infinity
 #pragma unroll 1
-            for (int m = 0; m < NC; m++)
-              if (!(sees[h] >> m & 1u)) {
-                uint8_t* const dst = bp_step + h * 2 * L::BP_TERM + (m / 8) * L::BP_SBO + (m & 7) * 2;
-                *reinterpret_cast<uint16_t*>(dst) = 0;
-                *reinterpret_cast<uint16_t*>(dst + L::BP_TERM) = 0;
-              }
-          }
+          for (int m = 0; m < NC; m++)
+            if (!(sees >> m & 1u)) {
+              uint8_t* const dst = bp_block + (m / 8) * L::BP_SBO + (m & 7) * 2;
+              *reinterpret_cast<uint16_t*>(dst) = 0;
+              *reinterpret_cast<uint16_t*>(dst + L::BP_TERM) = 0;
+            }
         }
         fence_proxy_async();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s.p_ready);
+        if (lane == 0) mbar_arrive(&s.p_ready[i & 1]);
       }
       // ---- the piece's partial. Sums over the rows: in the warp, then over the four warps, in a fixed order.
       const size_t part = (c.item + blockIdx.x) * N;
