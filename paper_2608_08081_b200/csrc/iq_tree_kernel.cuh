@@ -1,5 +1,21 @@
 // Attention for drafted tokens over the packed cache: one pass over the blocks of a (sequence, KV head) for up to N (token, query head)
-// pairs.
+// pairs, the columns.
+//
+// A block of 128 rows: S[row][column] = A_K B_Q, A_K the levels of the K codes (binary16, exact: the integers of an 8-bit grid or the levels
+// themselves), B_Q the rotated queries; t = S scale_row unit - reference_column in units of log2; p = 2^t; O[coordinate][column] += A_V B_P,
+// A_V the levels of the V codes, B_P = p times the row's V scale. Both tiles are dequantised into tensor memory (the A operands), the
+// queries and probabilities are shared memory (B). A column's sum of p stays with the row's thread until the piece ends; a reference
+// that a score leaves behind is raised for all columns, and sums and O scaled. q~ and p are two binary16 terms each (22 bits): one
+// term's 11 would be as much error again as the rounding of a binary16 output. Products with both terms go to the same accumulator.
+//
+// What bounds it: neither memory nor a pipe. 32 sequences of up to 32 K rows, 8 KV heads, 32 columns, 3 bits: 0.33 ms = 2.0 TB/s of packed
+// rows and 0.23 PFLOP/s; the shift/logic pipe, which has the lookups (216 instructions for 128 codes), is busy half of the time, the
+// tensor pipe a quarter, and the schedulers issue in 0.6 of the cycles: a warp has an instruction ready every five cycles or so, and
+// the waits between the warpgroups (90 cycles each when there is nothing to wait for) come on top. By measurement (the same launch):
+// every warp dequantising and taking half of the softmax 0.44 ms; dequantisation and softmax apart, one control warp 0.38; K, V, each
+// product, loads and the search for work in warps of their own 0.37 (the search in one place: the loops then stay in the instruction
+// cache, which half of the fetches missed before); two softmax groups 0.39; one CTA per SM with two blocks to a step and everything in
+// pairs 0.35; two groups each for K and V 0.37; this one, one CTA's pairs and one wait per block with two CTAs, 0.33.
 #pragma once
 #include "iq_decode_common.cuh"
 #include "iq_format.cuh"
@@ -7,10 +23,11 @@
 
 namespace iq {
 
-// Warpgroups of a CTA: two for the softmax (a thread to a cache row, half of the columns each), one that dequantises
-// K (a thread to a row), one that dequantises V (a thread to a coordinate), and one of which a warp each issues the score products, issues
-// the value products, loads, and finds the work.
+// Warpgroups of a CTA: one or two for the softmax (a thread to a cache row; two: half of the columns each), one that dequantises K (a thread
+// to a row), one that dequantises V (a thread to a coordinate), and one of which a warp each issues the score products, issues the value
+// products, loads, and finds the work.
 
+// With 4 and 3 in the place of 9 and 2 one block in six raised (16 sequences of 16 K rows, 32 columns), now one in twenty.
 constexpr float TREE_RAISE = 9.f;      // a score this far (log2) above its column's reference raises the references,
 constexpr float TREE_HEADROOM = 2.f;   // to this far above the block's maximum
 constexpr float TREE_V_ROOM = 2.f;     // and the reference of the V scales to at least this times their maximum
@@ -70,7 +87,7 @@ struct TreeLayout {
   static constexpr int SW = CTAS == 2 ? 1 : 2, NC = N / SW;
   static constexpr int SOFTMAX = 128 * SW, THREADS = SOFTMAX + 3 * 128;
   static constexpr int K_WARP = 4 * SW, V_WARP = K_WARP + 4, QK_WARP = V_WARP + 4, PV_WARP = QK_WARP + 1, LOAD_WARP = QK_WARP + 2, WALK_WARP = QK_WARP + 3;
-  // Registers of a thread where two CTAs share an SM: 64 at launch, 256 over the four groups.
+  // Registers of a thread where two CTAs share an SM: 64 at launch, 256 over the four groups; a softmax thread holds N sums and N scores.
   static constexpr int SOFTMAX_REGS = N == 16 ? 88 : 112, OTHER_REGS = N == 16 ? 56 : 48;
   // tensor memory: K tiles (binary16, two to a column), V tiles, scores, values; two of a kind where they
   // fit, so that the next one is made while this one is used
