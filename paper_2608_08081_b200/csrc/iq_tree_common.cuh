@@ -13,6 +13,7 @@ struct TreeSeq {
   long long weight;        // blocks of all its items, each item counting TREE_SEG_COST more
   __device__ __forceinline__ int block(int v) const { return v < sink_blocks ? v : v + skipped; }
 };
+template <int TILE>
 __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
   TreeSeq s;
   s.ctx = max(0, min(p.ctx_lens[b], p.t_cap));
@@ -27,7 +28,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
     s.skipped = max(0, (max(0, s.ctx - p.window) >> 7) - s.sink_blocks);
   }
   s.blocks = total - s.skipped;
-  s.tiles = (s.tokens * p.group + p.tile - 1) / p.tile;
+  s.tiles = (s.tokens * p.group + TILE - 1) / TILE;
   s.weight = (long long)p.n_kv_heads * s.tiles * (s.blocks + TREE_SEG_COST);
   return s;
 }
@@ -48,51 +49,41 @@ __device__ __forceinline__ long long tree_div(long long a, long long b) {
 __device__ __forceinline__ long long tree_cut(long long total, int cta, int ctas) { return tree_div(total * cta, ctas); }
 __device__ __forceinline__ int tree_cta_of(long long unit, long long total, int ctas) { return (int)tree_div((unit + 1) * ctas - 1, total); }
 
-// All threads; scratch: THREADS / 32 + 4 words of 8 bytes. Ends with a barrier.
-template <int THREADS>
-__device__ __forceinline__ TreeRange tree_range(const TreeParams& p, long long* scratch) {
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int per = (p.batch + THREADS - 1) / THREADS;
-  const int b0 = min(p.batch, tid * per), b1 = min(p.batch, b0 + per);
-  long long sum = 0;
-  for (int b = b0; b < b1; b++) sum += tree_seq(p, b).weight;
-  long long x = sum;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(FULL, x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 31) scratch[warp] = x;
-  __syncthreads();
-  long long before = x - sum, total = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 32; w++) {
-    const long long t = scratch[w];
-    if (w < warp) before += t;
-    total += t;
-  }
+// By one converged warp, 32 sequences at a time: first the launch's units, then the sequence that this CTA's range starts in. (The other
+// warps need neither; with all of them at it, each fetching the code, a launch over one short sequence took 2 us longer.)
+template <int TILE>
+__device__ __forceinline__ TreeRange tree_range(const TreeParams& p, int lane) {
   TreeRange r;
+  long long total = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += 32)
+    if (b0 + lane < p.batch) total += tree_seq<TILE>(p, b0 + lane).weight;
+#pragma unroll 1
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(FULL, total, o);
   r.total = total;
   r.ctas = (int)min((long long)p.ctas, total);
   r.at = r.end = total;
-  if (blockIdx.x < r.ctas) {
-    r.at = tree_cut(total, blockIdx.x, r.ctas);
-    r.end = tree_cut(total, blockIdx.x + 1, r.ctas);
-  }
-  if (r.at < r.end && before <= r.at && r.at < before + sum) {
-    int b = b0;
-    for (;; b++) {
-      const long long w = tree_seq(p, b).weight;
-      if (r.at < before + w) break;
-      before += w;
+  r.b = 0;
+  r.seq_at = 0;
+  if (blockIdx.x >= r.ctas) return r;
+  r.at = tree_cut(total, blockIdx.x, r.ctas);
+  r.end = tree_cut(total, blockIdx.x + 1, r.ctas);
+  for (int b0 = 0;; b0 += 32) {
+    const long long w = b0 + lane < p.batch ? tree_seq<TILE>(p, b0 + lane).weight : 0;
+    long long x = w;
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(FULL, x, o);
+      if (lane >= o) x += y;
     }
-    scratch[THREADS / 32] = b;
-    scratch[THREADS / 32 + 1] = before;
+    const uint32_t behind = __ballot_sync(FULL, r.at < r.seq_at + x);  // lanes whose sequence ends behind the start
+    if (behind) {
+      const int at = __ffs(behind) - 1;
+      r.b = b0 + at;
+      r.seq_at += __shfl_sync(FULL, x - w, at);
+      return r;
+    }
+    r.seq_at += __shfl_sync(FULL, x, 31);
   }
-  __syncthreads();
-  r.b = (int)scratch[THREADS / 32];
-  r.seq_at = scratch[THREADS / 32 + 1];
-  return r;
 }
 
 // What the tokens of a tile see: per token its mask (without drafted tokens before its window) and the first context row of its window.

@@ -58,11 +58,10 @@ struct TreeShared {
   alignas(16) float l_factor[N];    // of the last raise
   alignas(16) float o_factor[N];
   alignas(16) float warp_max[4][N];             // per quarter of the rows; at the end of a piece: sums
-  float warp_v[8], warp_q[12];
+  float warp_v[8], warp_q[16];
   int token[N];                     // the token of a column, counted from the tile's first
   TreeMasks<N> masks;
   TreeBatch batch[2];
-  long long scratch[32 + 2];
 };
 
 template <int D, int BITS, int N>
@@ -192,19 +191,14 @@ __device__ __forceinline__ int tree_queries(const TreeParams& p, TreeShared<N>& 
   using L = TreeLayout<D, BITS, N>;
   constexpr int E = D / 32;
   auto load = [&](int n, uint32_t (&raw)[E / 2]) {
-    if (n < nq) {
-      const int t = (q0 + n) / p.group, h = c.g * p.group + (q0 + n) - t * p.group;
-      const __half* q = p.q + c.b * p.qs_b + t * p.qs_t + h * p.qs_h + lane * E;
-      if constexpr (E == 4) {
-        const uint2 x = *reinterpret_cast<const uint2*>(q);
-        raw[0] = x.x; raw[1] = x.y;
-      } else {
-        const uint4 x = *reinterpret_cast<const uint4*>(q);
-        raw[0] = x.x; raw[1] = x.y; raw[E / 2 - 2] = x.z; raw[E / 2 - 1] = x.w;
-      }
+    const int t = (q0 + n) / p.group, h = c.g * p.group + (q0 + n) - t * p.group;
+    const __half* q = p.q + c.b * p.qs_b + t * p.qs_t + h * p.qs_h + lane * E;
+    if constexpr (E == 4) {
+      const uint2 x = *reinterpret_cast<const uint2*>(q);
+      raw[0] = x.x; raw[1] = x.y;
     } else {
-#pragma unroll
-      for (int e = 0; e < E / 2; e++) raw[e] = 0u;
+      const uint4 x = *reinterpret_cast<const uint4*>(q);
+      raw[0] = x.x; raw[1] = x.y; raw[E / 2 - 2] = x.z; raw[E / 2 - 1] = x.w;
     }
   };
   float qmax = 0.f;
@@ -228,6 +222,12 @@ __device__ __forceinline__ int tree_queries(const TreeParams& p, TreeShared<N>& 
   const float scale = rsqrtf((float)D) * __uint_as_float((uint32_t)(127 + e2) << 23);
 #pragma unroll 2
   for (int n = w; n < N; n += W) {
+    uint8_t* const dst = bq + (n >> 3) * 128 + (n & 7) * 16 + (E == 4 ? (lane >> 1) * L::BQ_LBO + (lane & 1) * 8 : lane * L::BQ_LBO);
+    if (n >= nq) {
+      if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<uint2*>(dst + L::BQ_TERM) = make_uint2(0u, 0u);
+      else *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<uint4*>(dst + L::BQ_TERM) = make_uint4(0u, 0u, 0u, 0u);
+      continue;
+    }
     uint32_t raw[E / 2];
     load(n, raw);
     float x[E];
@@ -246,7 +246,6 @@ __device__ __forceinline__ int tree_queries(const TreeParams& p, TreeShared<N>& 
       const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[e]));
       lo[e] = pack_half2(a0 - f.x, a1 - f.y);
     }
-    uint8_t* const dst = bq + (n >> 3) * 128 + (n & 7) * 16 + (E == 4 ? (lane >> 1) * L::BQ_LBO + (lane & 1) * 8 : lane * L::BQ_LBO);
     if constexpr (E == 4) {
       *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0], hi[1]);
       *reinterpret_cast<uint2*>(dst + L::BQ_TERM) = make_uint2(lo[0], lo[1]);
@@ -296,7 +295,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
   }
   grid_dependency_wait();
   tc_fence_before();
-  const TreeRange range = tree_range<L::THREADS>(p, s.scratch);  // (its barriers also cover the set-up above)
+  __syncthreads();
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(FULL, s.tmem, 0);
   const uint32_t lanes = (uint32_t)(warp & 3) << 21;  // this warp's quarter of the tensor-memory lanes
@@ -387,15 +386,16 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
     }
     else if (warp == L::WALK_WARP) {
       // ---- the pieces
+      const TreeRange range = tree_range<N>(p, lane);
       long long at = range.at, seq_at = range.seq_at;
       int b = range.b;
       TreeSeq sq;
-      if (at < range.end) sq = tree_seq(p, b);
+      if (at < range.end) sq = tree_seq<N>(p, b);
       for (int k = 0;; k++) {
         TreeBatch& out = s.batch[k & 1];
         int count = 0, blocks = 0;
         while (count < TREE_BATCH && at < range.end) {
-          if (at >= seq_at + sq.weight) { seq_at += sq.weight; sq = tree_seq(p, ++b); continue; }
+          if (at >= seq_at + sq.weight) { seq_at += sq.weight; sq = tree_seq<N>(p, ++b); continue; }
           const int len = sq.blocks + TREE_SEG_COST;
           const int m = (int)tree_div(at - seq_at, len);  // item of the sequence
           const long long item_at = seq_at + (long long)m * len;
@@ -440,10 +440,10 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
     uint64_t* const ready = k_side ? s.k_ready : s.v_ready;
     uint64_t* const used = k_side ? s.s_done : s.o_done;
     for (int k = 0; batch(k); k++) {
-      if (k == 0 && !k_side) {  // a hand with the first piece's queries
+      if (k == 0) {  // a hand with the first piece's queries, while its first tiles come
         const TreePiece c = s.batch[0].piece[0];
         const int q0 = c.tile * N;
-        tree_queries<D, BITS, N>(p, s, bq, c, q0, min(N, c.sq.tokens * p.group - q0), warp - 4, 4 * L::SW + 4, 2, L::SOFTMAX + 128, lane);
+        tree_queries<D, BITS, N>(p, s, bq, c, q0, min(N, c.sq.tokens * p.group - q0), warp, 4 * L::SW + 8, 2, L::SOFTMAX + 256, lane);
       }
       for (const uint32_t end = i + s.batch[k & 1].blocks; i < end; i++) {
         const uint32_t st = i % NST;
@@ -470,14 +470,16 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
       const int q0 = c.tile * N, nq = min(N, c.sq.tokens * p.group - q0), t0 = q0 / p.group;
       if (tid == 0) s.masks.from_max = 0;
       cta_bar_sync_n(1, L::SOFTMAX);  // the last piece's references have been read
+      const bool first = i == 0;
+      const int e2 = tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, 4 * L::SW + (first ? 8 : 0), 2, L::SOFTMAX + (first ? 256 : 0), lane);
+      if (lane == 0) mbar_arrive(&s.q_ready);
+      // (the first score products run meanwhile)
       tree_masks(p, s.masks, c.b, c.sq, t0, (q0 + nq - 1) / p.group - t0 + 1, tid, L::SOFTMAX);
       if (tid < N) {
         s.neg_ref[tid] = 1e30f;
         s.token[tid] = (q0 + tid) / p.group - t0;
       }
-      const bool first = i == 0;
-      const int e2 = tree_queries<D, BITS, N>(p, s, bq, c, q0, nq, warp, 4 * L::SW + (first ? 4 : 0), 2, L::SOFTMAX + (first ? 128 : 0), lane);
-      if (lane == 0) mbar_arrive(&s.q_ready);
+      cta_bar_sync_n(1, L::SOFTMAX);
       const float score_unit = p.score_unit * __uint_as_float((uint32_t)(127 - e2) << 23);
 
       float l[NC];
