@@ -2,7 +2,7 @@
 // a pool. Integer work on a few kilobytes (the copies apart): what bounds these kernels is a launch and a few trips to memory one after
 // the other, so each is one launch, and what has to be agreed on between CTAs (the top of the stack of free pages) is worked out by
 // every CTA for itself and written by the one that arrives last. In a captured graph, one B200: three of five rows of one sequence kept
-// 1.7 us, up to a quarter of 60 in each of 64 sequences (8 KV heads) 10.2; pages of 8 sequences given back and reserved 7, of 512 13.8;
+// 1.7 us, up to a quarter of 60 in each of 64 sequences (8 KV heads) 10.2; pages of 8 sequences given back and reserved 6.8, of 512 12.1;
 // four branches given back and made anew 8.9, 64 with 24 MB copied 17.9.
 #include "iq_common.cuh"
 #include "iq_format.cuh"
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(RELEASE_THREADS) release_kernel(const PoolPara
     const long long first = max(0, p.first_row[b]), end = min((long long)p.end_row[b], cap);
     const int lo = (int)((first + p.page_rows - 1) / p.page_rows), hi = end > 0 ? (int)(end / p.page_rows) : 0;
     int32_t* const row = p.table + (size_t)b * p.pages_per_seq;
-    constexpr int U = 8;  // entries of a lane in flight: 512 tables of 252 entries and the reservation behind it 13.8 us, one by one 15.0
+    constexpr int U = 8;  // entries of a lane in flight (512 tables of 252 entries and the reservation behind it 13.8 us, one by one 15.0)
     for (int j0 = lo + lane; j0 < hi; j0 += 32 * U) {
       int pages[U];
 #pragma unroll
@@ -279,21 +279,29 @@ __global__ void __launch_bounds__(RELEASE_THREADS) release_kernel(const PoolPara
     }
   }
   if (!last_to_arrive(p.state, gridDim.x)) return;
-  const int words = (p.num_pages + 31) / 32, per = (words + RELEASE_THREADS - 1) / RELEASE_THREADS;
-  const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
-  int count = 0;
-  for (int w = w0; w < w1; w++) count += __popc(__ldcg(&marks[w]));
-  int total;
-  const int n_free = max(0, min(__ldcg(&p.state[0]), p.num_pages));
-  int at = n_free + block_prefix<RELEASE_THREADS>(count, s_warp, total);
-  if (count)
-    for (int w = w0; w < w1; w++) {
-      uint32_t m = __ldcg(&marks[w]);
-      if (m) marks[w] = 0;
-      for (; m; m &= m - 1, at++)
-        if (at < p.num_pages) p.free_list[at] = 32 * w + __ffs(m) - 1;
+  constexpr int U = 8;  // words of a thread in flight (the same 12.1 us, one by one 13.9)
+  const int words = (p.num_pages + 31) / 32;
+  int top = max(0, min(__ldcg(&p.state[0]), p.num_pages));
+  for (int c = 0; c < words; c += U * RELEASE_THREADS) {
+    const int w0 = c + tid * U;
+    uint32_t m[U];
+    int count = 0, total;
+#pragma unroll
+    for (int u = 0; u < U; u++) m[u] = w0 + u < words ? __ldcg(&marks[w0 + u]) : 0u;
+#pragma unroll
+    for (int u = 0; u < U; u++) count += __popc(m[u]);
+    int at = top + block_prefix<RELEASE_THREADS>(count, s_warp, total);
+    if (count) {
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        if (m[u]) marks[w0 + u] = 0;
+        for (uint32_t x = m[u]; x; x &= x - 1, at++)
+          if (at < p.num_pages) p.free_list[at] = 32 * (w0 + u) + __ffs(x) - 1;
+      }
     }
-  if (tid == 0) p.state[0] = min(n_free + total, p.num_pages);
+    top = min(top + total, p.num_pages);
+  }
+  if (tid == 0) p.state[0] = top;
 }
 
 // ------------------------------------------------------------------------------------------------ copies

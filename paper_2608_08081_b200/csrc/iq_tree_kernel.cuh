@@ -15,7 +15,7 @@
 // every warp dequantising and taking half of the softmax 0.44 ms; dequantisation and softmax apart, one control warp 0.38; K, V, each
 // product, loads and the search for work in warps of their own 0.37 (the search in one place: the loops then stay in the instruction
 // cache, which half of the fetches missed before); two softmax groups 0.39; one CTA per SM with two blocks to a step and everything in
-// pairs 0.35; two groups each for K and V 0.37; this one, one CTA's pairs and one wait per block with two CTAs, 0.33.
+// pairs 0.35; two groups each for K and V 0.37; this one, pairs of everything and one wait per block, with two CTAs, 0.33.
 #pragma once
 #include "iq_decode_common.cuh"
 #include "iq_format.cuh"
