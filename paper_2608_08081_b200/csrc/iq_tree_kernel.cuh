@@ -34,6 +34,10 @@ constexpr float TREE_V_ROOM = 2.f;     // and the reference of the V scales to a
 // A probability of 1 of a row with the longest V scale as a binary16 operand: the largest, 2^9, stays below 2^15, and of one of 2^-20
 // the second term still holds 9 bits.
 constexpr float TREE_P_UNIT = 32.f;
+// The tensor core cuts its sums off, always towards zero: 3e-7 of the sum a block in the values of a piece (160 blocks: 4.9e-5 of the
+// output). They are added up in fp32 after every so many blocks, in the piece's partial. (Every 8: 32 columns and 220 blocks to a CTA
+// 345 us, 16: 338, 32: 334, with shrinkage of 2e-6, 4e-6 and twice that.)
+constexpr int TREE_FOLD = 16;
 
 // The pieces of a CTA's range: runs of blocks of an item. One warp walks along the range and leaves the pieces in shared memory, up to
 // TREE_BATCH at a time, the next ones while the others work on these.
@@ -54,6 +58,7 @@ struct TreeShared {
   uint64_t full[TREE_STAGES], taken[TREE_STAGES], q_ready, drain;
   uint64_t k_ready[2], s_done[2], s_read[2], v_ready[2], p_ready[2], o_done[2];  // of even and odd blocks
   uint32_t tmem, failed;
+  uint32_t fresh[2];                // the values of an even or odd block start the accumulator anew
   alignas(16) float neg_ref[N];     // minus the reference of each column, log2 units
   alignas(16) float l_factor[N];    // of the last raise
   alignas(16) float o_factor[N];
@@ -137,12 +142,6 @@ __device__ __forceinline__ void tree_ld(uint32_t taddr, float (&o)[C]) {
 #pragma unroll
   for (int i = 0; i < C; i++) o[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tree_st8(uint32_t taddr, const float (&v)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])),
-               "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])),
-               "r"(__float_as_uint(v[7])) : "memory");
-}
-
 // 128 codes of a packed run in shared memory -> 64 columns of the thread's tensor-memory lane.
 template <int BITS>
 __device__ __forceinline__ void tree_dequant(const uint8_t* run, const uint32_t (&lo)[4], const uint32_t (&hi)[4], LookupConst c, uint32_t taddr) {
@@ -348,8 +347,8 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
           if (elect_one()) {
             const uint32_t d = tmem + L::S_COL + (L::S_BUFS == 2 ? (i & 1) * N : 0), a = tmem + L::K_COL + (L::K_BUFS == 2 ? (i & 1) * L::TILE_COLS : 0);
 #pragma unroll 1
-            for (int t = 0; t < 2 * DJ; t++) {  // halves of the coordinates, terms of q~
-              const uint32_t at = (t & (DJ - 1)) * 16 * L::BQ_LBO + t / DJ * L::BQ_TERM;
+            for (int t = 0; t < 2 * DJ; t++) {  // terms of q~, halves of the coordinates: the second terms first, while there is little to cut off
+              const uint32_t at = (t & (DJ - 1)) * 16 * L::BQ_LBO + (t < DJ ? L::BQ_TERM : 0);
 #pragma unroll
               for (int m = 0; m < 8; m++)
                 tc_mma_f16(d, a + (t & (DJ - 1)) * 64 + 8 * m, desc + ((at + 2 * m * L::BQ_LBO) >> 4), L::IDESC_Q, t || m);
@@ -363,11 +362,11 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
       // ---- value products
       const uint64_t desc = smem_desc_mn(smem_u32(bp), L::BP_LBO, L::BP_SBO);
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
-        const uint32_t first = i;
         for (const uint32_t end = i + s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo; i < end; i++) {
           tree_wait2(s.p_ready, i, p.wait_polls, &s.failed);
           tree_wait2(s.v_ready, i, p.wait_polls, &s.failed);
           tc_fence_after();
+          const uint32_t more = !*(volatile uint32_t*)&s.fresh[i & 1];
           if (elect_one()) {
             mbar_arrive(&s.taken[i % NST]);
             const uint32_t a = tmem + L::V_COL + (L::V_BUFS == 2 ? (i & 1) * L::TILE_COLS : 0);
@@ -376,7 +375,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
               const uint32_t x = t >> 1, at = ((t & 1) + 2 * (i & 1)) * L::BP_TERM;
 #pragma unroll
               for (int m = 0; m < 8; m++)
-                tc_mma_f16(tmem + L::O_COL + x * N, a + 64 * x + 8 * m, desc + ((at + 2 * m * L::BP_LBO) >> 4), L::IDESC_P, i > first || (t & 1) || m);
+                tc_mma_f16(tmem + L::O_COL + x * N, a + 64 * x + 8 * m, desc + ((at + 2 * m * L::BP_LBO) >> 4), L::IDESC_P, more || (t & 1) || m);
             }
             tc_commit(&s.o_done[i & 1]);
           }
@@ -485,6 +484,11 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
       float l[NC];
 #pragma unroll
       for (int n = 0; n < NC; n++) l[n] = 0.f;
+      // The values: those of the last `held` blocks in tensor memory, those before in the piece's partial (in units of v_ref, too).
+      const size_t part = (c.item + blockIdx.x) * N;
+      float* const part_row = p.part_acc + (part + c0) * D + r;
+      int held = 0;
+      bool kept = false;
       float v_ref = 0.f, v_unit = 0.f;  // a power of two at least as large as every V scale so far; TREE_P_UNIT over it
       // blocks that every token of the tile sees in full (those of the sinks are looked at row by row)
       const int from_max = s.masks.from_max, all_from = from_max ? max(c.sq.sink_blocks, ((from_max + 127) >> 7) - c.sq.skipped) : 0;
@@ -529,7 +533,8 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
         float top = fmaxf(t[0], t[1]);
 #pragma unroll
         for (int m = 2; m < NC; m += 2) top = max3f(top, t[m], t[m + 1]);
-        if (__builtin_expect(cta_bar_or_n(1, L::SOFTMAX, top > TREE_RAISE || vs_fin > v_ref), 0)) {
+        const bool raised = cta_bar_or_n(1, L::SOFTMAX, top > TREE_RAISE || vs_fin > v_ref);
+        if (__builtin_expect(raised, 0)) {
           // ---- new references: the maximum of each column over the block, and of the V scales
           const float vm = tree_warp_max(vs_fin);
           if (lane == 0) s.warp_v[warp] = vm;
@@ -568,20 +573,6 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
             const float4 f = *reinterpret_cast<const float4*>(s.l_factor + c0 + m);
             l[m] *= f.x; l[m + 1] *= f.y; l[m + 2] *= f.z; l[m + 3] *= f.w;
           }
-          if (v > c.lo) {
-            tree_wait2(s.o_done, i - 1, p.wait_polls, &s.failed);
-            tc_fence_after();
-#pragma unroll 1
-            for (int n0 = 0; n0 < DJ * NC; n0 += 8) {
-              const int n1 = n0 & (NC - 1), at = n1 + n0 / NC * N;
-              float o[8];
-              tree_ld<8>(o_col + at, o);
-#pragma unroll
-              for (int x = 0; x < 8; x++) o[x] *= s.o_factor[c0 + n1 + x];
-              tree_st8(o_col + at, o);
-            }
-            tc_wait_st();
-          }
           relative();
         }
         tc_fence_before();
@@ -618,12 +609,38 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
             }
         }
         fence_proxy_async();
+        // ---- the values so far into the partial, to the new references. (Sixteen columns at a time where a thread has the registers.)
+        constexpr int FC = L::CTAS == 2 ? 16 : 8;
+        if (held && (raised || held == TREE_FOLD)) {
+          tree_wait2(s.o_done, i - 1, p.wait_polls, &s.failed);
+          tc_fence_after();
+#pragma unroll 1
+          for (int n0 = 0; n0 < DJ * NC; n0 += FC) {
+            const int n1 = n0 & (NC - 1), h = n0 / NC;
+            float* const dst = part_row + (size_t)n1 * D + 128 * h;
+            float o[FC], old[FC];
+#pragma unroll
+            for (int x = 0; x < FC; x++) old[x] = kept ? dst[x * D] : 0.f;
+            tree_ld<FC>(o_col + h * N + n1, o);
+#pragma unroll
+            for (int x = 0; x < FC; x++) o[x] += old[x];
+            if (raised) {
+#pragma unroll
+              for (int x = 0; x < FC; x++) o[x] *= s.o_factor[c0 + n1 + x];
+            }
+#pragma unroll
+            for (int x = 0; x < FC; x++) dst[x * D] = o[x];
+          }
+          kept = true;
+          held = 0;
+        }
+        if (tid == 0) s.fresh[i & 1] = held == 0;
+        held++;
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.p_ready[i & 1]);
       }
       // ---- the piece's partial. Sums over the rows: in the warp, then over the four warps, in a fixed order.
-      const size_t part = (c.item + blockIdx.x) * N;
       cta_bar_sync_n(1, L::SOFTMAX);  // (warp_max of a raise has been read)
       {
         const float sum = tree_reduce<NC>(l, lane);
@@ -643,7 +660,11 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
         for (int n0 = 0; n0 < NC && c0 + n0 < nq; n0 += 8) {
           float o[8];
           tree_ld<8>(o_col + h * N + n0, o);
-          float* const dst = p.part_acc + (part + c0 + n0) * D + 128 * h + r;
+          float* const dst = part_row + (size_t)n0 * D + 128 * h;
+          if (kept) {
+#pragma unroll
+            for (int n = 0; n < 8; n++) o[n] += dst[n * D];
+          }
 #pragma unroll
           for (int n = 0; n < 8; n++)
             if (c0 + n0 + n < nq) dst[n * D] = o[n] * unit;

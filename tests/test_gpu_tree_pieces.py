@@ -1,0 +1,90 @@
+"""iq_tree_attention where a CTA works off long pieces, many pieces, or pieces whose rows differ much in weight and length. Many sequences
+share the pages of one context, so the cache stays small; a few sequences are compared with the definition in 64 bits."""
+import numpy as np
+import pytest
+
+import branching as br
+from test_gpu_tree import Case, dev
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def iq():
+    import paper_2608_08081_b200 as m
+    return m
+
+
+def tile_and_ctas(c):
+    """(token, query head) pairs of an item and CTAs of the launch."""
+    pairs = c.T * c.H // c.hk
+    tile = 16 if pairs <= 16 else 32 if pairs <= 32 else 64
+    return tile, torch.cuda.get_device_properties(0).multi_processor_count * (2 if c.d == 128 and tile <= 32 else 1)
+
+
+def blocks_per_cta(c):
+    """Blocks of 128 rows in a CTA's range (no window)."""
+    tile, ctas = tile_and_ctas(c)
+    items = [c.hk * -(-int(t) * (c.H // c.hk) // tile) * -(-(int(x) + int(t)) // 128) for x, t in zip(c.ctx, c.tokens)]
+    return sum(items) / ctas
+
+
+def shared(iq, seed, sequences=None, **kw):
+    """A Case of one sequence, its pages read by as many sequences as the launch has CTAs (or `sequences`), each with queries of its own.
+    The drafted tokens see the context only."""
+    c = Case(iq, seed, B=1, page_rows=128, tree="any", **kw)
+    B = sequences or tile_and_ctas(c)[1]
+    c.B = B
+    c.ctx, c.tokens, c.table = np.repeat(c.ctx, B), np.repeat(c.tokens, B), np.repeat(c.table, B, 0)
+    c.see = np.zeros((B, c.T, c.T), bool)
+    c.mask = dev(br.mask_words(c.see))
+    c.q = c.rng.standard_normal((B, c.T, c.H, c.d)).astype(np.float16)
+    c.shape = iq.Shape(B, c.H, c.hk, c.d, c.t_cap, c.bits, c.sm_scale)
+    return c
+
+
+def run(c):
+    c.upload()
+    out = torch.zeros((c.B, c.T, c.H, c.d), device="cuda")
+    lse = torch.zeros((c.B, c.T, c.H), device="cuda")
+    c.call(out, lse)
+    torch.cuda.synchronize()
+    assert c.status.tolist() == [0, 0, 0, 0]
+    return out, lse
+
+
+def expected(c, some):
+    return br.attention(c.rows, c.table[some], c.page_rows, c.quats, c.lk, c.lv, c.q[some], c.ctx[some], c.tokens[some], c.see[some], c.window, c.sinks,
+                        c.t_cap, c.sm_scale)
+
+
+def off(got, want):
+    """Error over all the outputs, relative to them."""
+    got = got.double().cpu().numpy()
+    return np.linalg.norm(got - want) / np.linalg.norm(want)
+
+
+# Head counts and tokens of the three tiles.
+TILES = [dict(T=2, H=8), dict(T=4, H=8), dict(T=8, H=8)]
+KINDS = [dict(d=128), dict(d=256, bits=4), dict(d=128, bits=2, grid="fp16"), dict(d=256, grid="fp16")]
+
+
+def ids(k):
+    return "-".join(f"{a}{v}" for a, v in k.items())
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=ids)
+@pytest.mark.parametrize("tile", TILES, ids=ids)
+def test_sums_over_long_pieces(iq, tile, kind):
+    """Over 150 blocks of one item to a CTA. A tensor core cuts its sums off where an fp32 addition rounds, 16 times a block, by half of
+    2^-24 .. 2^-23 of the sum in the mean, always towards zero: left there for 160 blocks the sums lose 160 * 16 * 2^-25 = 8e-5, over
+    the growing sum 4e-5. Taken over into fp32 sums every 16 blocks it is a tenth: with q~ and the weights (2^-18 and less of each, not
+    all one way) below 1e-5."""
+    c = shared(iq, 21, ctx=160 * 128, **tile, **kind)
+    assert blocks_per_cta(c) > 150
+    out, lse = run(c)
+    some = [0, c.B // 2, c.B - 1]
+    o, l, tol, tol_lse = expected(c, some)
+    assert off(out[some], o) <= 1e-5
+    assert np.all(np.abs(lse[some].double().cpu().numpy() - l) <= tol_lse)
