@@ -4,6 +4,8 @@
 #include <cstring>
 #include <vector>
 
+#include <cuda_bf16.h>
+
 #include "iq_common.cuh"
 #include "iq_kernels.h"
 
@@ -937,14 +939,22 @@ static int tree_attention(const iq_shape* shape, const float* rot_dev, const iq_
   p.pm = page_map(cache, shape);
   p.scale_f16 = cache->scales_fp16 ? 1 : 0;
   p.bits = shape->bits;
-  for (int v = 0; v < 2; v++)
-    for (int i = 0; i < 1 << shape->bits; i++) {
-      const __half hv = __float2half_rn(grid8 ? (float)n8[v][i] : side_levels(codebook, v)[i]);
+  p.v_terms = 1;
+  for (int i = 0; i < 1 << shape->bits; i++) {
+    auto put = [&](auto x, uint32_t* lo, uint32_t* hi) {
       uint16_t bits;
-      std::memcpy(&bits, &hv, 2);
-      (v ? p.lut_v_lo : p.lut_lo)[i >> 2] |= (uint32_t)(bits & 0xFFu) << (8 * (i & 3));
-      (v ? p.lut_v_hi : p.lut_hi)[i >> 2] |= (uint32_t)(bits >> 8) << (8 * (i & 3));
-    }
+      std::memcpy(&bits, &x, 2);
+      lo[i >> 2] |= (uint32_t)(bits & 0xFFu) << (8 * (i & 3));
+      hi[i >> 2] |= (uint32_t)(bits >> 8) << (8 * (i & 3));
+    };
+    put(__float2half_rn(grid8 ? (float)n8[0][i] : side_levels(codebook, 0)[i]), p.lut_lo, p.lut_hi);
+    const float level = grid8 ? (float)n8[1][i] : side_levels(codebook, 1)[i];
+    const __nv_bfloat16 first = __float2bfloat16_rn(level);
+    const float rest = level - __bfloat162float(first);  // (at most 3 of the 11 bits of a binary16 value)
+    put(first, p.lut_v_lo[0], p.lut_v_hi[0]);
+    put(__float2bfloat16_rn(rest), p.lut_v_lo[1], p.lut_v_hi[1]);
+    if (rest != 0.f) p.v_terms = 2;
+  }
   p.lookup = iq::LOOKUP_CONST;
   const double root_d = std::sqrt((double)shape->head_dim), sm = shape->sm_scale > 0.f ? (double)shape->sm_scale : 1.0 / root_d;
   p.score_unit = (float)(sm * 1.4426950408889634 * delta[0] / root_d);

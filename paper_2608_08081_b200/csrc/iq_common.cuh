@@ -149,6 +149,12 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   return d;
 }
 
+__device__ __forceinline__ uint32_t pack_bf162(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+
 __device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
 }

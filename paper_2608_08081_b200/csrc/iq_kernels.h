@@ -187,9 +187,10 @@ struct TreeParams {
   PageMap pm;
   int scale_f16;
   int bits;
-  // The levels as exact binary16 values times a unit per side (8-bit grid: the integers and delta; else the levels and 1): low and
-  // high bytes, 4 per register (2^bits / 4 registers used).
-  uint32_t lut_lo[4], lut_hi[4], lut_v_lo[4], lut_v_hi[4];
+  // The levels, exact, times a unit per side (8-bit grid: the integers and delta; else the levels and 1). K: binary16 values, V: bfloat16
+  // values, or where they have more than 8 bits sums of two (v_terms). Low and high bytes, 4 per register (2^bits / 4 registers used).
+  uint32_t lut_lo[4], lut_hi[4], lut_v_lo[2][4], lut_v_hi[2][4];
+  int v_terms;
   LookupConst lookup;
   float score_unit;          // sm_scale log2(e) unit_K / sqrt(d): a score in units of log2 is this times scale times the product
   float value_unit;          // unit_V / sqrt(d)

@@ -3,10 +3,15 @@
 //
 // A block of 128 rows: S[row][column] = A_K B_Q, A_K the levels of the K codes (binary16, exact: the integers of an 8-bit grid or the levels
 // themselves), B_Q the rotated queries; t = S scale_row unit - reference_column in units of log2; p = 2^t; O[coordinate][column] += A_V B_P,
-// A_V the levels of the V codes, B_P = p times the row's V scale. Both tiles are dequantised into tensor memory (the A operands), the
-// queries and probabilities are shared memory (B). A column's sum of p stays with the row's thread until the piece ends; a reference
-// that a score leaves behind is raised for all columns, and sums and O scaled. q~ and p are two binary16 terms each (22 bits): one
-// term's 11 would be as much error again as the rounding of a binary16 output. Products with both terms go to the same accumulator.
+// A_V the levels of the V codes (bfloat16), B_P = p times the row's V scale. Both tiles are dequantised into tensor memory (the A operands),
+// the queries and probabilities are shared memory (B). A column's sum of p stays with the row's thread until the piece ends; a reference
+// that a score leaves behind is raised for all columns, and sums and O scaled. Products with both terms of an operand go to the same
+// accumulator.
+// q~ is two binary16 terms (22 bits): one term's 11 would be as much error again as the rounding of a binary16 output. p times the V scale
+// is two bfloat16 terms, which leave out 2^-18 of it at most, however far it lies below the largest one: where a row takes 99 % of the
+// weight and has next to no value the output is the other rows' (with binary16 terms it was off by 1 %). The integers of an 8-bit
+// grid are bfloat16 values; other levels (11 bits) are sums of two, and their blocks have two tiles of V levels one after the other (16
+// sequences of 16 K rows, 32 columns: 162 us, one tile 132).
 //
 // What bounds it: neither memory nor a pipe. 32 sequences of up to 32 K rows, 8 KV heads, 32 columns, 3 bits: 0.33 ms = 2.0 TB/s of packed
 // rows and 0.23 PFLOP/s; the shift/logic pipe, which has the lookups (216 instructions for 128 codes), is busy half of the time, the
@@ -27,16 +32,13 @@ namespace iq {
 // to a row), one that dequantises V (a thread to a coordinate), and one of which a warp each issues the score products, issues the value
 // products, loads, and finds the work.
 
-// With 4 and 3 in the place of 9 and 2 one block in six raised (16 sequences of 16 K rows, 32 columns), now one in twenty.
-constexpr float TREE_RAISE = 9.f;      // a score this far (log2) above its column's reference raises the references,
-constexpr float TREE_HEADROOM = 2.f;   // to this far above the block's maximum
-constexpr float TREE_V_ROOM = 2.f;     // and the reference of the V scales to at least this times their maximum
-// A probability of 1 of a row with the longest V scale as a binary16 operand: the largest, 2^9, stays below 2^15, and of one of 2^-20
-// the second term still holds 9 bits.
-constexpr float TREE_P_UNIT = 32.f;
+// A score this far (log2) above its column's reference raises the references, to this far above the block's maximum. (fp32 and
+// bfloat16 have room for more; further from the reference a score relative to it is rounded more coarsely.)
+constexpr float TREE_RAISE = 16.f;
+constexpr float TREE_HEADROOM = 2.f;
 // The tensor core cuts its sums off, always towards zero: 3e-7 of the sum a block in the values of a piece (160 blocks: 4.9e-5 of the
-// output). They are added up in fp32 after every so many blocks, in the piece's partial. (Every 8: 32 columns and 220 blocks to a CTA
-// 345 us, 16: 338, 32: 334, with shrinkage of 2e-6, 4e-6 and twice that.)
+// output). They are added up in fp32 in the piece's partial after every so many tiles of V levels. (Every 8: 32 columns and 220 blocks
+// to a CTA 345 us, 16: 338, 32: 334, with shrinkage of 2e-6, 4e-6 and twice that.)
 constexpr int TREE_FOLD = 16;
 
 // The pieces of a CTA's range: runs of blocks of an item. One warp walks along the range and leaves the pieces in shared memory, up to
@@ -56,14 +58,14 @@ constexpr int TREE_STAGES = 6;  // at most
 template <int N>
 struct TreeShared {
   uint64_t full[TREE_STAGES], taken[TREE_STAGES], q_ready, drain;
-  uint64_t k_ready[2], s_done[2], s_read[2], v_ready[2], p_ready[2], o_done[2];  // of even and odd blocks
+  uint64_t k_ready[2], s_done[2], s_read[2], p_ready[2], o_done[2];  // of even and odd blocks
+  uint64_t v_ready[2], v_used[2];  // of even and odd tiles of V levels
   uint32_t tmem, failed;
   uint32_t fresh[2];                // the values of an even or odd block start the accumulator anew
   alignas(16) float neg_ref[N];     // minus the reference of each column, log2 units
   alignas(16) float l_factor[N];    // of the last raise
-  alignas(16) float o_factor[N];
   alignas(16) float warp_max[4][N];             // per quarter of the rows; at the end of a piece: sums
-  float warp_v[8], warp_q[16];
+  float warp_q[16];
   int token[N];                     // the token of a column, counted from the tile's first
   TreeMasks<N> masks;
   TreeBatch batch[2];
@@ -102,9 +104,9 @@ struct TreeLayout {
   static constexpr int K_COL = 0, V_COL = K_BUFS * TILE_COLS, S_COL = V_COL + V_BUFS * TILE_COLS, O_COL = S_COL + S_BUFS * N;
   static_assert(O_COL + DJ * N <= COLS, "tensor memory");
   static_assert(STAGES >= 2 && SMEM <= ROOM, "shared memory");
-  // fp32 result, binary16 operands, M = 128; B_Q K-major, B_P MN-major
+  // fp32 result, M = 128; scores: binary16 operands, B_Q K-major; values: bfloat16 operands, B_P MN-major
   static constexpr uint32_t IDESC_Q = (1u << 4) | (((uint32_t)N >> 3) << 17) | ((128u >> 4) << 24);
-  static constexpr uint32_t IDESC_P = IDESC_Q | (1u << 16);
+  static constexpr uint32_t IDESC_P = IDESC_Q | (1u << 7) | (1u << 10) | (1u << 16);
 };
 
 // Bounded wait of a converged warp. A wait that gives up is noted in `failed`, and from then on no wait of the CTA lasts: every thread
@@ -142,6 +144,15 @@ __device__ __forceinline__ void tree_ld(uint32_t taddr, float (&o)[C]) {
 #pragma unroll
   for (int i = 0; i < C; i++) o[i] = __uint_as_float(r[i]);
 }
+// A pair of values as two bfloat16 terms each, 2^-18 of the value left out. The difference is a mixed-precision subtraction: without the
+// shift and mask that would make fp32 values of the first terms (64 columns 186 us instead of 188).
+__device__ __forceinline__ void tree_two_terms(float y0, float y1, uint32_t& first, uint32_t& second) {
+  first = pack_bf162(y0, y1);
+  float r0, r1;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tsub.rn.f32.bf16 %0, l, %3;\n\tsub.rn.f32.bf16 %1, h, %4;\n\t}" : "=f"(r0), "=f"(r1) : "r"(first), "f"(y0), "f"(y1));
+  second = pack_bf162(-r0, -r1);
+}
+
 // 128 codes of a packed run in shared memory -> 64 columns of the thread's tensor-memory lane.
 template <int BITS>
 __device__ __forceinline__ void tree_dequant(const uint8_t* run, const uint32_t (&lo)[4], const uint32_t (&hi)[4], LookupConst c, uint32_t taddr) {
@@ -278,6 +289,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
     for (int i = 0; i < 2; i++) {
       mbar_init(&s.k_ready[i], 4);
       mbar_init(&s.v_ready[i], 4);
+      mbar_init(&s.v_used[i], 1);
       mbar_init(&s.o_done[i], 1);
       mbar_init(&s.p_ready[i], 4 * L::SW);
       mbar_init(&s.s_done[i], 1);
@@ -361,25 +373,32 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
     } else if (warp == L::PV_WARP) {
       // ---- value products
       const uint64_t desc = smem_desc_mn(smem_u32(bp), L::BP_LBO, L::BP_SBO);
+      uint32_t tile = 0;  // of V levels so far
       for (int k = 0; batch(k); k++) for (int j = 0; j < s.batch[k & 1].pieces; j++) {
         for (const uint32_t end = i + s.batch[k & 1].piece[j].hi - s.batch[k & 1].piece[j].lo; i < end; i++) {
           tree_wait2(s.p_ready, i, p.wait_polls, &s.failed);
-          tree_wait2(s.v_ready, i, p.wait_polls, &s.failed);
-          tc_fence_after();
           const uint32_t more = !*(volatile uint32_t*)&s.fresh[i & 1];
-          if (elect_one()) {
-            mbar_arrive(&s.taken[i % NST]);
-            const uint32_t a = tmem + L::V_COL + (L::V_BUFS == 2 ? (i & 1) * L::TILE_COLS : 0);
 #pragma unroll 1
-            for (int t = 0; t < 2 * DJ; t++) {  // terms of the probabilities, halves of the coordinates
-              const uint32_t x = t >> 1, at = ((t & 1) + 2 * (i & 1)) * L::BP_TERM;
+          for (int y = 0; y < p.v_terms; y++, tile++) {  // terms of the levels; of the second one's products the smaller is left out
+            tree_wait2(s.v_ready, tile, p.wait_polls, &s.failed);
+            tc_fence_after();
+            if (elect_one()) {
+              const uint32_t a = tmem + L::V_COL + (L::V_BUFS == 2 ? (tile & 1) * L::TILE_COLS : 0);
+#pragma unroll 1
+              for (int t = 0; t < 2 * DJ; t += 1 + y) {  // terms of the probabilities, halves of the coordinates
+                const uint32_t x = t >> 1, at = ((t & 1) + 2 * (i & 1)) * L::BP_TERM;
 #pragma unroll
-              for (int m = 0; m < 8; m++)
-                tc_mma_f16(tmem + L::O_COL + x * N, a + 64 * x + 8 * m, desc + ((at + 2 * m * L::BP_LBO) >> 4), L::IDESC_P, more || (t & 1) || m);
+                for (int m = 0; m < 8; m++)
+                  tc_mma_f16(tmem + L::O_COL + x * N, a + 64 * x + 8 * m, desc + ((at + 2 * m * L::BP_LBO) >> 4), L::IDESC_P, more || y || (t & 1) || m);
+              }
+              if (p.v_terms > 1) tc_commit(&s.v_used[tile & 1]);
+              if (y + 1 == p.v_terms) {
+                mbar_arrive(&s.taken[i % NST]);
+                tc_commit(&s.o_done[i & 1]);
+              }
             }
-            tc_commit(&s.o_done[i & 1]);
+            __syncwarp();
           }
-          __syncwarp();
         }
       }
     }
@@ -430,14 +449,16 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
     uint32_t lo[4], hi[4];
 #pragma unroll
     for (int x = 0; x < 4; x++) {
-      lo[x] = k_side ? p.lut_lo[x] : p.lut_v_lo[x];
-      hi[x] = k_side ? p.lut_hi[x] : p.lut_v_hi[x];
+      lo[x] = k_side ? p.lut_lo[x] : p.lut_v_lo[0][x];
+      hi[x] = k_side ? p.lut_hi[x] : p.lut_v_hi[0][x];
     }
+    const int terms = k_side ? 1 : p.v_terms;
+    uint32_t n = 0;  // tiles so far
     const uint8_t* const run = stages + (k_side ? r * L::P : L::TILE_BYTES + r * (16 * BITS));
     const int next = k_side ? 16 * BITS : 128 * 16 * BITS;
     const uint32_t col = tmem + lanes + (k_side ? L::K_COL : L::V_COL), bufs = k_side ? L::K_BUFS : L::V_BUFS;
     uint64_t* const ready = k_side ? s.k_ready : s.v_ready;
-    uint64_t* const used = k_side ? s.s_done : s.o_done;
+    uint64_t* const used = k_side ? s.s_done : terms > 1 ? s.v_used : s.o_done;
     for (int k = 0; batch(k); k++) {
       if (k == 0) {  // a hand with the first piece's queries, while its first tiles come
         const TreePiece c = s.batch[0].piece[0];
@@ -447,15 +468,25 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
       for (const uint32_t end = i + s.batch[k & 1].blocks; i < end; i++) {
         const uint32_t st = i % NST;
         tree_wait(&s.full[st], (i / NST) & 1, p.wait_polls, &s.failed);
-        if (i >= bufs) tree_wait2(used, i - bufs, p.wait_polls, &s.failed);  // the tile before is read no more
-        tc_fence_after();
 #pragma unroll 1
-        for (int x = 0; x < DJ; x++)
-          tree_dequant<BITS>(run + st * L::BLOCK_BYTES + x * next, lo, hi, p.lookup, col + (bufs == 2 ? (i & 1) * L::TILE_COLS : 0) + 64 * x);
-        tc_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(ready + (i & 1));
+        for (int y = 0; y < terms; y++, n++) {
+          if (terms > 1) {
+#pragma unroll
+            for (int x = 0; x < 4; x++) {
+              lo[x] = p.lut_v_lo[y][x];
+              hi[x] = p.lut_v_hi[y][x];
+            }
+          }
+          if (n >= bufs) tree_wait2(used, n - bufs, p.wait_polls, &s.failed);  // the tile before is read no more
+          tc_fence_after();
+#pragma unroll 1
+          for (int x = 0; x < DJ; x++)
+            tree_dequant<BITS>(run + st * L::BLOCK_BYTES + x * next, lo, hi, p.lookup, col + (bufs == 2 ? (n & 1) * L::TILE_COLS : 0) + 64 * x);
+          tc_wait_st();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(ready + (n & 1));
+        }
       }
     }
   } else {
@@ -484,12 +515,12 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
       float l[NC];
 #pragma unroll
       for (int n = 0; n < NC; n++) l[n] = 0.f;
-      // The values: those of the last `held` blocks in tensor memory, those before in the piece's partial (in units of v_ref, too).
+      // The values: those of the last `held` blocks in tensor memory, those before in the piece's partial.
       const size_t part = (c.item + blockIdx.x) * N;
       float* const part_row = p.part_acc + (part + c0) * D + r;
+      const int fold = TREE_FOLD / p.v_terms;
       int held = 0;
       bool kept = false;
-      float v_ref = 0.f, v_unit = 0.f;  // a power of two at least as large as every V scale so far; TREE_P_UNIT over it
       // blocks that every token of the tile sees in full (those of the sinks are looked at row by row)
       const int from_max = s.masks.from_max, all_from = from_max ? max(c.sq.sink_blocks, ((from_max + 127) >> 7) - c.sq.skipped) : 0;
       const int all_to = (c.sq.ctx >> 7) - c.sq.skipped;
@@ -510,7 +541,6 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
             if (tree_sees(s.masks, s.token[c0 + m], row, c.sq.ctx, c.sq.rows, p.sinks)) sees |= 1u << m;
           if (!sees) vs = 0.f;
         }
-        const float vs_fin = vs < INFINITY ? vs : 0.f;  // (an infinite or undefined scale is its own row's affair)
 
         // scores relative to the references; -inf where the token does not see the row
         float t[NC];
@@ -533,11 +563,9 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
         float top = fmaxf(t[0], t[1]);
 #pragma unroll
         for (int m = 2; m < NC; m += 2) top = max3f(top, t[m], t[m + 1]);
-        const bool raised = cta_bar_or_n(1, L::SOFTMAX, top > TREE_RAISE || vs_fin > v_ref);
+        const bool raised = cta_bar_or_n(1, L::SOFTMAX, top > TREE_RAISE);
         if (__builtin_expect(raised, 0)) {
-          // ---- new references: the maximum of each column over the block, and of the V scales
-          const float vm = tree_warp_max(vs_fin);
-          if (lane == 0) s.warp_v[warp] = vm;
+          // ---- new references: the maximum of each column over the block
 #pragma unroll 1
           for (int n0 = 0; n0 < NC; n0 += 8) {
             float z[8], m[8];
@@ -550,24 +578,14 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
             }
           }
           cta_bar_sync_n(1, L::SOFTMAX);
-          float v_new = s.warp_v[0];
-#pragma unroll 1
-          for (int x = 1; x < 4 * L::SW; x++) v_new = fmaxf(v_new, s.warp_v[x]);
-          // the power of two at or above it, with room, within 2^-100 .. 2^127
-          v_new = v_new > v_ref ? fmaxf(__uint_as_float((__float_as_uint(v_new) + 0x7FFFFFu) & 0x7F800000u) * TREE_V_ROOM, 7.888609e-31f) : v_ref;
-          if (!(v_new < INFINITY)) v_new = 1.7014118e38f;
           if (tid < N) {
             const float m = fmaxf(fmaxf(s.warp_max[0][tid], s.warp_max[1][tid]), fmaxf(s.warp_max[2][tid], s.warp_max[3][tid]));
             const float old = -s.neg_ref[tid];
             const float ref = m > -2e38f ? fmaxf(old, m + TREE_HEADROOM) : old;
-            const float f = ex2f(old - ref);
             s.neg_ref[tid] = -ref;
-            s.l_factor[tid] = f;
-            s.o_factor[tid] = v_new > 0.f ? f * (v_ref / v_new) : f;
+            s.l_factor[tid] = ex2f(old - ref);
           }
           cta_bar_sync_n(1, L::SOFTMAX);
-          v_ref = v_new;
-          v_unit = v_ref > 0.f ? TREE_P_UNIT / v_ref : 0.f;
 #pragma unroll
           for (int m = 0; m < NC; m += 4) {
             const float4 f = *reinterpret_cast<const float4*>(s.l_factor + c0 + m);
@@ -578,9 +596,8 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.s_read[i & 1]);
-        // ---- probabilities, and times the V scale as two binary16 terms of the operand B_P
+        // ---- probabilities, and times the V scale as two bfloat16 terms of the operand B_P
         uint8_t* const bp_block = bp_row + (i & 1) * 2 * L::BP_TERM;
-        const float vn = vs * v_unit;
 #pragma unroll
         for (int n0 = 0; n0 < NC; n0 += 8) {
           uint32_t hi[4], lo[4];
@@ -588,12 +605,10 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
           for (int x = 0; x < 4; x++) {
             const int m = n0 + 2 * x;
             const float p0 = ex2f(t[m]), p1 = ex2f(t[m + 1]);
-            const F32x2 ls = add2(f32x2(l[m], l[m + 1]), f32x2(p0, p1)), y = mul2(f32x2(p0, p1), f32x2(vn, vn));
+            const F32x2 ls = add2(f32x2(l[m], l[m + 1]), f32x2(p0, p1)), y = mul2(f32x2(p0, p1), f32x2(vs, vs));
             l[m] = ls.lo();
             l[m + 1] = ls.hi();
-            hi[x] = pack_half2(y.lo(), y.hi());
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[x]));
-            lo[x] = pack_half2(y.lo() - f.x, y.hi() - f.y);
+            tree_two_terms(y.lo(), y.hi(), hi[x], lo[x]);
           }
           uint8_t* const dst = bp_block + (n0 / 8) * L::BP_SBO;
           *reinterpret_cast<uint4*>(dst) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
@@ -611,7 +626,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
         fence_proxy_async();
         // ---- the values so far into the partial, to the new references. (Sixteen columns at a time where a thread has the registers.)
         constexpr int FC = L::CTAS == 2 ? 16 : 8;
-        if (held && (raised || held == TREE_FOLD)) {
+        if (held && (raised || held == fold)) {
           tree_wait2(s.o_done, i - 1, p.wait_polls, &s.failed);
           tc_fence_after();
 #pragma unroll 1
@@ -626,7 +641,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
             for (int x = 0; x < FC; x++) o[x] += old[x];
             if (raised) {
 #pragma unroll
-              for (int x = 0; x < FC; x++) o[x] *= s.o_factor[c0 + n1 + x];
+              for (int x = 0; x < FC; x++) o[x] *= s.l_factor[c0 + n1 + x];
             }
 #pragma unroll
             for (int x = 0; x < FC; x++) dst[x * D] = o[x];
@@ -651,7 +666,6 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
         const float sum = (s.warp_max[0][tid] + s.warp_max[1][tid]) + (s.warp_max[2][tid] + s.warp_max[3][tid]);
         *reinterpret_cast<float2*>(p.part_ml + 2 * (part + tid)) = make_float2(-s.neg_ref[tid], sum);
       }
-      const float unit = p.value_unit * (v_ref / TREE_P_UNIT);
       tree_wait2(s.o_done, i - 1, p.wait_polls, &s.failed);
       tc_fence_after();
 #pragma unroll 1
@@ -667,7 +681,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
           }
 #pragma unroll
           for (int n = 0; n < 8; n++)
-            if (c0 + n0 + n < nq) dst[n * D] = o[n] * unit;
+            if (c0 + n0 + n < nq) dst[n * D] = o[n] * p.value_unit;
         }
       tc_fence_before();
     }

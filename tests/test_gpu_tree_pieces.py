@@ -1,9 +1,12 @@
 """iq_tree_attention where a CTA works off long pieces, many pieces, or pieces whose rows differ much in weight and length. Many sequences
 share the pages of one context, so the cache stays small; a few sequences are compared with the definition in 64 bits."""
+import math
+
 import numpy as np
 import pytest
 
 import branching as br
+import oracle
 from test_gpu_tree import Case, dev
 
 torch = pytest.importorskip("torch")
@@ -87,4 +90,38 @@ def test_sums_over_long_pieces(iq, tile, kind):
     some = [0, c.B // 2, c.B - 1]
     o, l, tol, tol_lse = expected(c, some)
     assert off(out[some], o) <= 1e-5
+    assert np.all(np.abs(lse[some].double().cpu().numpy() - l) <= tol_lse)
+
+
+def towards(c, k, score):
+    """Every query's part along k (in the original space) made so large that a row whose key is k scores `score`."""
+    q = c.q.astype(np.float64)
+    q += (score * math.sqrt(c.d) - q @ k)[..., None] * k / (k @ k)
+    c.q = q.astype(np.float16)
+
+
+def bound(c, score):
+    """Of the output: 2^-18 of each weight, q~ and exp2 below that, the sums as over long pieces: 1e-5; and for a row that scores much, what
+    the tensor core cuts off its score (d / 16 additions of first terms, 2^-24 in the mean) and its rounding."""
+    return 1e-5 + (c.d / 16 + 2) * 2.0 ** -24 * max(score, 0.0)
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=ids)
+@pytest.mark.parametrize("tile", TILES, ids=ids)
+@pytest.mark.parametrize("weight,length", [(0.99, 1e-6), (0.9999, 1e-6), (1e-12, 1e5)], ids=["sink99", "sink9999", "long"])
+def test_one_row_unlike_the_others(iq, weight, length, tile, kind):
+    """A row near the start of a piece of some 100 blocks has almost all of the weight and next to no value (an attention sink), or a value
+    1e5 times the others' and no weight: the output is the other rows' either way. A weight's rounding may not depend on how large
+    another row's weight or value is."""
+    c = shared(iq, 22, ctx=100 * 128, **tile, **kind)
+    c.rows.scales[0] *= np.float32(0.1)
+    page, row = int(c.table[0, 0]), 5
+    c.rows.scales[0][page, 0, row] = math.sqrt(c.d)
+    c.rows.scales[1][page, 0, row] = math.sqrt(c.d) * length
+    score = math.log(int(c.ctx[0])) + math.log(weight / (1 - weight))
+    towards(c, c.lk[c.rows.codes[0][page, 0, row]].astype(np.float64) @ oracle.rotation_matrix(c.d, c.quats[0]), score)
+    out, lse = run(c)
+    some = [0, c.B - 1]
+    o, l, tol, tol_lse = expected(c, some)
+    assert off(out[some], o) <= bound(c, score)
     assert np.all(np.abs(lse[some].double().cpu().numpy() - l) <= tol_lse)
