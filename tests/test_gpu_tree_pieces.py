@@ -125,3 +125,50 @@ def test_one_row_unlike_the_others(iq, weight, length, tile, kind):
     o, l, tol, tol_lse = expected(c, some)
     assert off(out[some], o) <= bound(c, score)
     assert np.all(np.abs(lse[some].double().cpu().numpy() - l) <= tol_lse)
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=ids)
+@pytest.mark.parametrize("tile", TILES, ids=ids)
+def test_references_that_rise_within_a_piece(iq, tile, kind):
+    """One row in some blocks of a piece of 40 scores 12 more than the last one (17 in units of log2: the references rise), before and
+    after the values have been taken over into fp32 sums, and in blocks next to each other. The earlier rows have the longer values, so
+    that all count: a factor that is left out, or applied to only a part, shows."""
+    c = shared(iq, 23, ctx=40 * 128, **tile, **kind)
+    blocks = [0, 3, 4, 20, 37]
+    last = 12.0 * (len(blocks) - 1) + 4
+    c.rows.scales[0] *= np.float32(0.05)
+    c.rows.scales[1] *= np.float32(math.exp(last) / 100)
+    first = int(c.table[0, 0])
+    for i, blk in enumerate(blocks):
+        page, score = int(c.table[0, blk]), 12.0 * i + 4
+        c.rows.codes[0][page, 0, 77] = c.rows.codes[0][first, 0, 77]
+        c.rows.scales[0][page, 0, 77] = math.sqrt(c.d) * score / last
+        c.rows.scales[1][page, 0, 77] = math.sqrt(c.d) * math.exp(last - score)
+    towards(c, c.lk[c.rows.codes[0][first, 0, 77]].astype(np.float64) @ oracle.rotation_matrix(c.d, c.quats[0]), last)
+    out, lse = run(c)
+    some = [0, c.B - 1]
+    o, l, tol, tol_lse = expected(c, some)
+    assert off(out[some], o) <= bound(c, last)
+    assert np.all(np.abs(lse[some].double().cpu().numpy() - l) <= tol_lse)
+
+
+@pytest.mark.parametrize("kw", [dict(T=1, H=64, hk=8), dict(T=3, H=64, hk=8), dict(T=5, H=64, hk=8), dict(T=1, H=16, hk=8, d=256, bits=4), dict(T=9, H=32, hk=8, d=256)], ids=ids)
+def test_more_pieces_than_are_found_at_a_time(iq, kw):
+    """A CTA's pieces are found sixteen at a time: here it has some forty, a block each."""
+    c = shared(iq, 24, sequences=1500, ctx=1, t_cap=128, **kw)
+    T = c.T
+    c.ctx = c.rng.integers(0, 129 - T, c.B).astype(np.int32)
+    c.table = c.rng.integers(0, c.rows.codes[0].shape[0], (c.B, 1)).astype(np.int32)
+    c.see[:] = np.tril(np.ones((T, T), bool))
+    c.mask = None
+    assert blocks_per_cta(c) > 32
+    out, lse = run(c)
+    some = [0, 1, 2, 300, 301, 749, 750, 1111, 1498, 1499]
+    want = expected(c, some)
+    c.tokens = c.tokens[some]
+    c.check(out[some], lse[some], want=want)
+    # sequences that are alike in everything have the same outputs, wherever their pieces lie
+    c.ctx[:], c.table[:], c.q[:] = c.ctx[7], c.table[7], c.q[7]
+    c.tokens = np.full(c.B, T, np.int32)
+    out, _ = run(c)
+    assert bool((out == out[:1]).all())
