@@ -471,8 +471,9 @@ int iq_selftest_bounded_wait(uint32_t* status_dev, uint32_t polls, void* stream)
  *   out            device [batch][n_tokens_max][n_q_heads][head_dim], fp32 or binary16 (out_is_fp16), 16-byte aligned.
  *   lse_out        device fp32 [batch][n_tokens_max][n_q_heads] or NULL.
  *   status_dev     optional (see top).
- * Codebooks as for iq_decode_attention. Blocks of 128 rows that no token sees are not read, and their pages need not be in the
- * block table. The cache is read once for every 64 (token, query head) pairs of a KV head.
+ * Codebooks as for iq_decode_attention. Pages whose rows no token sees need not be in the block table, if they hold no row of
+ * a drafted token: those are read whether a mask names them or not. The cache is read once for every 64 (token, query head) pairs of a
+ * KV head, without the blocks of 128 rows before the windows.
  * The same inputs give the same bits in every call on the same kind of device.
  * Limits: batch * n_kv_heads * ceil(n_tokens_max * heads per KV head / 16) below 2^31 - 2^20, batch * n_tokens_max * n_q_heads below 2^31,
  * t_cap at most 2^31 - 513 (IQ_ERR_LIMIT).

@@ -13,6 +13,21 @@ struct TreeSeq {
   long long weight;        // blocks of all its items, each item counting TREE_SEG_COST more
   __device__ __forceinline__ int block(int v) const { return v < sink_blocks ? v : v + skipped; }
 };
+__device__ __forceinline__ uint32_t tree_mask_word(const TreeParams& p, int b, int t, int w, int tokens) {
+  const int left = tokens - 32 * w;  // bits of tokens that the sequence has
+  const uint32_t have = left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
+  if (p.mask) return p.mask[((size_t)b * p.n_tokens_max + t) * p.mask_words + w] & have;
+  const int k = t + 1 - 32 * w;  // the chain: tokens 0 .. t
+  return have & (k >= 32 ? 0xFFFFFFFFu : k <= 0 ? 0u : (1u << k) - 1u);
+}
+__device__ __forceinline__ int tree_seen(const TreeParams& p, int b, int t, int tokens) {  // drafted tokens that token t sees
+  int n = 0;
+  for (int w = 0; w < p.mask_words; w++) n += __popc(tree_mask_word(p, b, t, w, tokens));
+  return n;
+}
+__device__ __forceinline__ int tree_position(const TreeParams& p, int b, int t, const TreeSeq& s) {
+  return s.ctx + tree_seen(p, b, t, s.tokens) - 1;
+}
 template <int TILE>
 __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
   TreeSeq s;
@@ -24,13 +39,36 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
   s.skipped = 0;
   if (p.window > 0) {
     s.sink_blocks = min(total, (p.sinks >> 7) + ((p.sinks & 127) != 0));
-    // a token's position is ctx - 1 at least (it sees no drafted token): what lies before that one's window is seen by none
-    s.skipped = max(0, (max(0, s.ctx - p.window) >> 7) - s.sink_blocks);
+    // The first token of a chain sees itself; by its mask a token may see no drafted token, and its window begin a row further back. (To
+    // look at the masks here took a launch over one sequence 1 us. Where they say more, the pages that it concerns are not missed:
+    // tree_block_row.)
+    s.skipped = max(0, (max(0, s.ctx - p.window + (p.mask ? 0 : min(s.tokens, 1))) >> 7) - s.sink_blocks);
   }
   s.blocks = total - s.skipped;
   s.tiles = (s.tokens * p.group + TILE - 1) / TILE;
   s.weight = (long long)p.n_kv_heads * s.tiles * (s.blocks + TREE_SEG_COST);
   return s;
+}
+
+// The first context row of the tokens' windows, a token's being ctx - window + (drafted tokens that it sees).
+__device__ __forceinline__ int tree_first_row(const TreeParams& p, int b, const TreeSeq& s) {
+  int n = s.tokens;
+  for (int t = 0; t < s.tokens; t++) n = min(n, tree_seen(p, b, t, s.tokens));
+  return max(0, s.ctx - p.window + n);
+}
+// Row of the cache arrays where block v of the sequence starts. Its page may be missing if the block holds context rows only and lies before
+// all windows: page 0, read in its place like in that of any entry outside the pool, is then not flagged, and no token sees it.
+__device__ __forceinline__ size_t tree_block_row(const TreeParams& p, int b, int g, const TreeSeq& s, int v, uint32_t* status) {
+  const int row = s.block(v) * 128;
+  if (p.pm.table == nullptr) return cache_row(p.pm, b, g, row, nullptr);
+  const int j = row / p.pm.page_rows;
+  int page = p.pm.table[(size_t)b * (p.t_cap / p.pm.page_rows) + j];
+  if (__builtin_expect((unsigned)page >= (unsigned)p.pm.num_pages, 0)) {
+    page = 0;
+    const bool unseen = p.window > 0 && v >= s.sink_blocks && row + 128 <= min(s.ctx, tree_first_row(p, b, s));
+    if (status && !unseen) atomicOr(&status[0], IQ_STATUS_BAD_PAGE);
+  }
+  return ((size_t)page * p.n_kv_heads + g) * (size_t)p.pm.page_rows + (size_t)(row - j * p.pm.page_rows);
 }
 
 // The launch's items (sequence, KV head, tile of (token, head) pairs) laid end to end, each as TREE_SEG_COST + its blocks units long,
@@ -93,18 +131,6 @@ struct TreeMasks {
   int from[TILE];
   int from_max;  // of all tokens of the tile
 };
-__device__ __forceinline__ uint32_t tree_mask_word(const TreeParams& p, int b, int t, int w, int tokens) {
-  const int left = tokens - 32 * w;  // bits of tokens that the sequence has
-  const uint32_t have = left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
-  if (p.mask) return p.mask[((size_t)b * p.n_tokens_max + t) * p.mask_words + w] & have;
-  const int k = t + 1 - 32 * w;  // the chain: tokens 0 .. t
-  return have & (k >= 32 ? 0xFFFFFFFFu : k <= 0 ? 0u : (1u << k) - 1u);
-}
-__device__ __forceinline__ int tree_position(const TreeParams& p, int b, int t, const TreeSeq& s) {
-  int n = 0;
-  for (int w = 0; w < p.mask_words; w++) n += __popc(tree_mask_word(p, b, t, w, s.tokens));
-  return s.ctx + n - 1;
-}
 // Threads tid, tid + threads, ... take a token each; the caller's barrier follows. from_max has to be 0 before (and behind a barrier).
 template <int TILE>
 __device__ __forceinline__ void tree_masks(const TreeParams& p, TreeMasks<TILE>& m, int b, const TreeSeq& s, int first, int n, int tid, int threads) {

@@ -327,7 +327,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
         const TreePiece c = s.batch[k & 1].piece[j];
         for (int v = c.lo; v < c.hi && !tree_failed(&s.failed); v++, i++) {
           const int st = i % NST;
-          const size_t row0 = cache_row(p.pm, c.b, c.g, (long long)c.sq.block(v) * 128, lane == 0 ? p.status : nullptr);
+          const size_t row0 = tree_block_row(p, c.b, c.g, c.sq, v, lane == 0 ? p.status : nullptr);
           if (i >= NST) tree_wait(&s.taken[st], (i / NST - 1) & 1, p.wait_polls, &s.failed);
           if (tree_failed(&s.failed)) break;  // (a second load on a barrier that still expects the first is no use to anybody)
           if (elect_one()) {
