@@ -543,9 +543,10 @@ def iq_tree_attention(shape: Shape, rot_dev, codebook: Codebook, q, cache: Cache
     if sizes is None:
         object.__setattr__(shape, "_tree_bytes", {})
         sizes = shape._tree_bytes
-    if T not in sizes:
-        sizes[T] = iq_tree_workspace_bytes(shape, T)
-    assert workspace.nbytes >= sizes[T] and workspace.is_contiguous()
+    where = torch.cuda.current_device(), T     # (the size goes by the device's SMs)
+    if where not in sizes:
+        sizes[where] = iq_tree_workspace_bytes(shape, T)
+    assert workspace.nbytes >= sizes[where] and workspace.is_contiguous()
     rc = _lib.iq_tree_attention(ctypes.byref(shape.c()), rot_dev.data_ptr(), ctypes.byref(codebook.c()), q.data_ptr(), sb, st, sh,
                                 ctypes.byref(cache.c()), _ints(ctx_lens_dev, B), _ints(tree_mask_dev, B * T * ((T + 31) // 32)),
                                 _ints(n_tokens_dev, B), T, window, sinks, workspace.data_ptr(), out.data_ptr(), 1 if f16 else 0, _ptr(lse_out),
