@@ -170,7 +170,10 @@ cudaError_t launch_reconstruct_rows(const ReconstructParams& p, int head_dim, in
 bool launch_reconstruct_tiles(const ReconstructParams& p, int head_dim, int batch, cudaStream_t stream, cudaError_t& e);
 
 // ---- tree attention: drafted tokens over the packed cache
-constexpr int TREE_SEG_COST = 1;  // what an item of the launch costs beside its blocks, in blocks (see tree_kernel)
+// What an item of the launch costs beside its blocks (queries, first references, partial), in blocks. With 1, 5, 7, 9 in its place: 32
+// sequences of 4000 and 100 rows in turn, 32 columns, 160, 90, 75, 73 us; 64 of 250 to 500 rows 68.9, 66.9, 62.4, 62.5; one of 32 K rows,
+// 240 pairs, 101, 98, 95, 93; 64 windows of 1 K rows 58.2, 57.0, 56.6, 56.4; one of 1000 rows 17.5, 17.4, 17.9, 18.1.
+constexpr int TREE_SEG_COST = 7;
 struct TreeParams {
   const uint8_t* k_codes;
   const float* k_scales;
