@@ -172,3 +172,27 @@ def test_more_pieces_than_are_found_at_a_time(iq, kw):
     c.tokens = np.full(c.B, T, np.int32)
     out, _ = run(c)
     assert bool((out == out[:1]).all())
+
+
+@pytest.mark.parametrize("kw", [dict(T=2, H=8), dict(T=8, H=8, d=256, grid="fp16")], ids=ids)
+def test_long_pieces_give_the_same_bits_again(iq, kw):
+    """Called twice, and replayed from a graph on another stream, over a workspace that holds something else each time."""
+    c = shared(iq, 25, ctx=70 * 128, **kw)
+    out, lse = run(c)
+    again, lse2 = torch.zeros_like(out), torch.zeros_like(lse)
+    q = dev(c.q)
+    c.workspace.fill_(255)
+    c.call(again, lse2, q=q)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.call(again, lse2, q=q)
+    s = torch.cuda.Stream()
+    for _ in range(2):
+        again.zero_()
+        c.workspace.fill_(255)
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            g.replay()
+        torch.cuda.current_stream().wait_stream(s)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)

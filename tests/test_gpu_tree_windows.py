@@ -42,3 +42,15 @@ def test_no_page_before_the_windows_is_needed(iq, rest, T, tree):
     torch.cuda.synchronize()
     assert c.status.tolist() == [0, 0, 0, 0]
     c.check(out, want=want)
+
+
+@pytest.mark.parametrize("kw", [dict(ctx=256, window=1), dict(ctx=256, window=1, sinks=5), dict(ctx=256, window=2, T=3), dict(ctx=255, window=1, T=3),
+                                dict(ctx=256, window=129, T=2), dict(ctx=128, window=1, t_cap=256, T=2), dict(ctx=384, window=128, t_cap=512, T=4),
+                                dict(ctx=384, window=129, t_cap=512, T=4)], ids=lambda k: "-".join(f"{a}{v}" for a, v in k.items()))
+@pytest.mark.parametrize("tree", ["chain", "tree", "any"])
+def test_windows_at_the_edge_of_a_block_or_of_the_cache(iq, kw, tree):
+    """Short windows whose first row, or whose token's own row, begins a block or lies behind the cache (t_cap 256: a token there sees
+    what sinks there are, or nothing)."""
+    c = Case(iq, 37, **{**dict(T=1, H=4, hk=2, t_cap=256, tree=tree), **kw})
+    c.poison()
+    c.run()
