@@ -474,6 +474,8 @@ int iq_selftest_bounded_wait(uint32_t* status_dev, uint32_t polls, void* stream)
  * Codebooks as for iq_decode_attention. Pages whose rows no token sees need not be in the block table, if they hold no row of
  * a drafted token: those are read whether a mask names them or not. The cache is read once for every 64 (token, query head) pairs of a
  * KV head, without the blocks of 128 rows before the windows.
+ * Arithmetic: q~ as two binary16 terms (22 bits), each weight times its V scale as two bfloat16 terms (2^-18 of it left out at most, however
+ * small it is), levels exact; tensor-core sums of up to 16 blocks, added up in fp32.
  * The same inputs give the same bits in every call on the same kind of device.
  * Limits: batch * n_kv_heads * ceil(n_tokens_max * heads per KV head / 16) below 2^31 - 2^20, batch * n_tokens_max * n_q_heads below 2^31,
  * t_cap at most 2^31 - 513 (IQ_ERR_LIMIT).
@@ -534,8 +536,8 @@ size_t iq_page_pool_state_ints(int32_t num_pages);
 int iq_reserve_pages(const iq_page_pool* pool, const int32_t* first_row_dev, const int32_t* end_row_dev, uint32_t* status_dev,
                      void* stream);
 /* Gives back the pages of which all rows lie in [first_row[b], end_row[b]): the entry becomes -1, the page's count drops by one, and
- * pages whose count reaches 0 are put on the stack in ascending order. An entry outside the pool, or of a page whose count is 0
- * already, becomes -1 and changes nothing else (IQ_STATUS_BAD_PAGE, counted in status[2]). */
+ * pages whose count reaches 0 are put on the stack in ascending order. An entry of num_pages or more, or of a page whose count is
+ * 0 already, becomes -1 and changes nothing else (IQ_STATUS_BAD_PAGE, counted in status[2]). */
 int iq_release_pages(const iq_page_pool* pool, const int32_t* first_row_dev, const int32_t* end_row_dev, uint32_t* status_dev,
                      void* stream);
 /*

@@ -860,7 +860,7 @@ int tree_plan(const iq_shape* s, int32_t n_tokens_max, TreePlan& w) {
   const long long queries = (long long)n_tokens_max * (s->n_q_heads / s->n_kv_heads);
   if ((long long)s->batch * s->n_kv_heads * ((queries + 15) / 16) >= (1ll << 31) - (1 << 20) || (long long)s->batch * n_tokens_max * s->n_q_heads >= (1ll << 31))
     return IQ_ERR_LIMIT;
-  w.tile = iq::tree_tile(s->head_dim, (int)queries);
+  w.tile = iq::tree_tile((int)queries);
   w.tiles = (int)((queries + w.tile - 1) / w.tile);
   w.ctas = sm_count() * iq::tree_ctas_per_sm(s->head_dim, w.tile);
   w.items = (long long)s->batch * s->n_kv_heads * w.tiles;

@@ -214,7 +214,7 @@ cudaError_t launch_tree_attention(const TreeParams& p, int head_dim, cudaStream_
 // CTAs per SM: two where they fit, so that one's items end and begin under the other's blocks: 64 sequences with a window of 1 K rows, 3
 // tokens and 8 heads per KV head, 112 us instead of 130
 constexpr int tree_ctas_per_sm(int head_dim, int tile) { return head_dim == 128 && tile <= 32 ? 2 : 1; }
-int tree_tile(int head_dim, int queries);  // tile for that many (token, head) pairs of a KV head
+int tree_tile(int queries);  // tile for that many (token, head) pairs of a KV head
 
 // ---- rows and pages of the cache
 struct CacheArrays {

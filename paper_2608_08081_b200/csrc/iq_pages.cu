@@ -2,8 +2,9 @@
 // a pool. Integer work on a few kilobytes (the copies apart): what bounds these kernels is a launch and a few trips to memory one after
 // the other, so each is one launch, and what has to be agreed on between CTAs (the top of the stack of free pages) is worked out by
 // every CTA for itself and written by the one that arrives last. In a captured graph, one B200: three of five rows of one sequence kept
-// 1.7 us, up to a quarter of 60 in each of 64 sequences (8 KV heads) 10.2; pages of 8 sequences given back and reserved 6.8, of 512 12.1;
-// four branches given back and made anew 8.9, 64 with 24 MB copied 17.9.
+// 1.9 us, up to a quarter of 60 in each of 64 sequences (8 KV heads) 10.3; pages of 8 sequences given back and reserved 7.2, of 512 12.4;
+// four branches given back and made anew 9.3, 64 with 13.7 MB of rows (16.9 MB with the rest of their blocks) copied 19.9; 512 pages of 53
+// KB a side copied 24.5.
 #include "iq_common.cuh"
 #include "iq_format.cuh"
 

@@ -96,9 +96,9 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(const __gr
 }  // namespace
 
 // The smallest tile that takes all pairs, up to 64: every item reads and dequantises its blocks, so more pairs to an item are worth the
-// columns that stay empty (16 sequences of 16 K rows, 8 KV heads: 16 columns 115 us, 32 138, not 230; a sequence of 32 K rows with 240
-// pairs as four items of 64 105 us).
-int tree_tile(int head_dim, int queries) { return queries <= 16 ? 16 : queries <= 32 ? 32 : 64; }
+// columns that stay empty (16 sequences of 16 K rows, 8 KV heads: 16 columns 105 us, 32 132, not 210, 64 181, not 264; a sequence of 32 K
+// rows with 240 pairs as four items of 64 96 us).
+int tree_tile(int queries) { return queries <= 16 ? 16 : queries <= 32 ? 32 : 64; }
 
 cudaError_t launch_tree_attention(const TreeParams& p, int head_dim, cudaStream_t stream) {
   const cudaError_t e = p.bits == 2 ? launch_tree_b2(p, head_dim, stream) : p.bits == 3 ? launch_tree_b3(p, head_dim, stream) : launch_tree_b4(p, head_dim, stream);

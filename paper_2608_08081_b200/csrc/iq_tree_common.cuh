@@ -80,7 +80,8 @@ struct TreeRange {
   int b;                     // the sequence in which the range starts
   long long seq_at;          // where that sequence starts
 };
-// (total < 2^47: the host's limits. The products of most launches fit 32 bits, whose division takes a fraction of the time.)
+// (total * ctas < 2^63: an item takes 8 KB of the workspace, so a launch has some 2^25 of them at most, each of at most 2^24 blocks. The
+// products of most launches fit 32 bits, whose division takes a fraction of the time.)
 __device__ __forceinline__ long long tree_div(long long a, long long b) {
   return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }

@@ -13,14 +13,15 @@
 // grid are bfloat16 values; other levels (11 bits) are sums of two, and their blocks have two tiles of V levels one after the other (16
 // sequences of 16 K rows, 32 columns: 162 us, one tile 132).
 //
-// What bounds it: neither memory nor a pipe. 32 sequences of up to 32 K rows, 8 KV heads, 32 columns, 3 bits: 0.33 ms = 2.0 TB/s of packed
+// What bounds it: neither memory nor a pipe. 32 sequences of up to 32 K rows, 8 KV heads, 32 columns, 3 bits: 0.336 ms = 2.0 TB/s of packed
 // rows and 0.23 PFLOP/s; the shift/logic pipe, which has the lookups (216 instructions for 128 codes), is busy half of the time, the
 // tensor pipe a quarter, and the schedulers issue in 0.6 of the cycles: a warp has an instruction ready every five cycles or so, and
 // the waits between the warpgroups (90 cycles each when there is nothing to wait for) come on top. By measurement (the same launch):
 // every warp dequantising and taking half of the softmax 0.44 ms; dequantisation and softmax apart, one control warp 0.38; K, V, each
 // product, loads and the search for work in warps of their own 0.37 (the search in one place: the loops then stay in the instruction
 // cache, which half of the fetches missed before); two softmax groups 0.39; one CTA per SM with two blocks to a step and everything in
-// pairs 0.35; two groups each for K and V 0.37; this one, pairs of everything and one wait per block, with two CTAs, 0.33.
+// pairs 0.35; two groups each for K and V 0.37; this one, pairs of everything and one wait per block, with two CTAs, 0.33 (the fp32 sums and
+// bfloat16 terms, which came later, and a better share of the work: 0.336).
 #pragma once
 #include "iq_decode_common.cuh"
 #include "iq_format.cuh"
