@@ -196,3 +196,33 @@ def test_long_pieces_give_the_same_bits_again(iq, kw):
             g.replay()
         torch.cuda.current_stream().wait_stream(s)
         assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("kw", [dict(T=2, H=8, bits=4), dict(T=8, H=8, d=256)], ids=ids)
+def test_a_wait_that_gives_up_over_levels_of_two_terms(iq, kw):
+    """Limit 0, with two tiles of V levels to a block: the call ends, says so, and the next one is right."""
+    c = shared(iq, 26, sequences=40, ctx=20 * 128, grid="fp16", **kw).upload()
+    out = torch.zeros((c.B, c.T, c.H, c.d), device="cuda")
+    iq.iq_selftest_tree_wait(c.shape, c.rot, c.cb, dev(c.q), c.cache, c.ctx_dev, c.mask, c.n_tokens, c.workspace, out, c.status, 0)
+    torch.cuda.synchronize()
+    assert c.status.tolist() == [2, 0, 0, 0]
+    out, _ = run(c)
+    some = [0, 39]
+    assert off(out[some], expected(c, some)[0]) <= 1e-5
+
+
+def test_two_calls_at_once(iq):
+    """Two streams, each with a workspace of its own, over one cache: the results are those of the calls one after the other."""
+    cases = [shared(iq, 27, ctx=30 * 128, T=4, H=8), shared(iq, 27, ctx=30 * 128, T=8, H=8, d=256, grid="fp16")]
+    want = [run(c)[0] for c in cases]
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [[torch.zeros_like(w) for _ in range(5)] for w in want]
+    qs = [dev(c.q) for c in cases]
+    torch.cuda.synchronize()
+    for i in range(5):
+        for c, s, o, q in zip(cases, streams, outs, qs):
+            with torch.cuda.stream(s):
+                c.call(o[i], q=q)
+    torch.cuda.synchronize()
+    for c, w, o in zip(cases, want, outs):
+        assert c.status.tolist() == [0, 0, 0, 0] and all(torch.equal(w, x) for x in o)
