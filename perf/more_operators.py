@@ -298,7 +298,7 @@ def prepare(case, seed):
         s["rot"] = s["quats"]  # (unit quaternion pairs: the rotation as the library keeps it)
         lv, th = _levels(c["bits"], c["grid"])
         s["codebook"] = iq.Codebook(tuple(lv), tuple(th))
-        s["workspace"] = torch.empty(iq.iq_chunk_workspace_bytes(s["shape"], _room(c) if c["packed"] else T, packed=c["packed"]), dtype=torch.uint8, device=dev)
+        s["workspace"] = torch.empty(iq.iq_chunk_workspace_bytes(s["shape"]), dtype=torch.uint8, device=dev)
         s["out"] = torch.zeros_like(s["q"])
     return s
 
