@@ -560,6 +560,123 @@ int iq_fork_sequences(const iq_shape* shape, const iq_cache* cache, const iq_pag
 int iq_copy_pages(const iq_shape* shape, const iq_cache* cache, const int32_t* src_pages_dev, const int32_t* dst_pages_dev,
                   int32_t n_pages, uint32_t* status_dev, void* stream);
 
+/*
+ * A step over requests of any lengths: prompts, pieces of prompts and single tokens together (the paper decodes one token at a time).
+ * Its tokens may come padded, n_tokens_max places per sequence, or packed, one request after the other: token_start_dev, device int32
+ * [batch + 1], then says where each sequence's tokens start among the n_tokens_max places of the step (clamped to [0, n_tokens_max]; a start
+ * behind the next counts as no tokens). The calls below take them in either form.
+ *
+ * iq_plan_tokens lays out a packed step from the requests' lengths: token_start[b] = sum of n_new[0 .. b - 1] (negative counts as 0), and
+ * for place i, which is token j of sequence b: positions[i] = ctx_lens[b] + j, sequences[i] = b, slots[i] = the cache row that holds the token:
+ * page * page_rows + row in the page (contiguous cache: b * t_cap + position), in rows of one KV head. Places behind the last token hold
+ * IQ_NO_POSITION, -1 and -1. slots[i] = -1 where the position lies outside [0, t_cap) (IQ_STATUS_ROW_OUT_OF_RANGE) or its page is not in the
+ * pool (IQ_STATUS_BAD_PAGE); both are counted in status[2], as are tokens for which n_tokens_max places are too few: those
+ * are left out (IQ_STATUS_ROW_OUT_OF_RANGE).
+ *   ctx_lens_dev, n_new_dev   device int32 [batch]: rows in the cache, new tokens.
+ *   block_table_dev           device int32 [batch][t_cap / page_rows], or NULL: contiguous (page_rows and num_pages are then not read). Pages
+ *                             for the new rows are reserved before (iq_reserve_pages).
+ *   token_start_dev           device int32 [batch + 1]; positions_dev, sequences_dev device int32 [n_tokens_max], slots_dev device
+ *                             int64 [n_tokens_max], each of the three may be NULL. Nothing may overlap the inputs.
+ * shape: its batch and t_cap are read. batch up to 65535 (IQ_ERR_LIMIT).
+ */
+#define IQ_NO_POSITION INT32_MIN
+int iq_plan_tokens(const iq_shape* shape, const int32_t* ctx_lens_dev, const int32_t* n_new_dev, const int32_t* block_table_dev,
+                   int32_t page_rows, int32_t num_pages, int32_t n_tokens_max, int32_t* token_start_dev, int32_t* positions_dev,
+                   int32_t* sequences_dev, int64_t* slots_dev, uint32_t* status_dev, void* stream);
+
+/*
+ * Rotary positions. Pair i of the first rotary_dim elements of a head is turned by position * f_i radians and multiplied by `magnitude`:
+ * (a, b) -> (a cos - b sin, a sin + b cos); the pairs are (x[i], x[i + rotary_dim / 2]), or with `interleaved` (x[2 i], x[2 i + 1]). Elements
+ * behind them stay. iq_make_rotary (host only) fills the struct:
+ *   rotary_dim   multiple of 16, up to 256 (the head_dim of the calls that take it at most).
+ *   base         f_i = base^(-2 i / rotary_dim), base > 1.
+ *   scaling      IQ_ROTARY_PLAIN; IQ_ROTARY_LINEAR: f_i / factor; IQ_ROTARY_BASE: base * factor^(rotary_dim / (rotary_dim - 2)) as the base;
+ *                IQ_ROTARY_PARTS: f_i / factor for slow pairs, f_i for fast ones and a mix between, f_i (1 - r_i) + f_i r_i / factor with
+ *                r_i = clamp((i - low) / max(high - low, 0.001), 0, 1), low = max(floor(pair(beta_fast)), 0), high = min(ceil(pair(beta_slow)),
+ *                rotary_dim - 1), pair(t) = rotary_dim ln(original_len / (2 pi t)) / (2 ln base): the pair that makes t turns over original_len positions;
+ *                the magnitude is then 0.1 ln(factor) + 1, in the others 1.
+ *   factor       >= 1 (PLAIN: not read); original_len >= 1, beta_fast > beta_slow > 0 (PARTS only).
+ *   inv_freq_host  or NULL. double [rotary_dim / 2]: the f_i themselves (finite), instead of base and scaling; the magnitude is 1 (set the member for another).
+ * turns[i] is f_i / (2 pi) as a 64-bit fraction (modulo 1, which whole positions do not see): position * turns[i] modulo 2^64 is the angle,
+ * exact for every int32 position; a negative position turns back.
+ */
+#define IQ_ROTARY_MAX_PAIRS 128
+enum { IQ_ROTARY_PLAIN = 0, IQ_ROTARY_LINEAR = 1, IQ_ROTARY_BASE = 2, IQ_ROTARY_PARTS = 3 };
+typedef struct iq_rotary {
+  int32_t rotary_dim;
+  int32_t interleaved;
+  float magnitude;
+  uint64_t turns[IQ_ROTARY_MAX_PAIRS];
+} iq_rotary;
+int iq_make_rotary(int32_t rotary_dim, int32_t interleaved, double base, int32_t scaling, double factor, int32_t original_len,
+                   double beta_fast, double beta_slow, const double* inv_freq_host, iq_rotary* out_host);
+/*
+ * Applies them to the queries and keys of n_tokens tokens, before iq_quantize_append and the attention calls.
+ *   q, k         device binary16, element (t, h, c) at t*stride_t + h*stride_h + c (strides in elements, multiples of 8, not negative;
+ *                16-byte aligned): n_q_heads and n_kv_heads heads of head_dim (shape's; its batch and t_cap are not read). One of
+ *                them may be NULL.
+ *   q_out, k_out the same, with strides of their own; they may be q and k themselves, with the same strides (in place: the elements behind
+ *                rotary_dim are then not touched). Otherwise outputs must not overlap inputs.
+ *   positions_dev device int32 [n_tokens]; tokens at IQ_NO_POSITION are left as they are in the outputs.
+ * fp32 arithmetic on angles that are off by 2^-24 of half a turn at most, one rounding to binary16.
+ */
+int iq_apply_rotary(const iq_shape* shape, const iq_rotary* rotary, const void* q, int64_t q_stride_t, int64_t q_stride_h, void* q_out,
+                    int64_t q_out_stride_t, int64_t q_out_stride_h, const void* k, int64_t k_stride_t, int64_t k_stride_h, void* k_out,
+                    int64_t k_out_stride_t, int64_t k_out_stride_h, const int32_t* positions_dev, int32_t n_tokens, void* stream);
+
+/*
+ * iq_quantize_append for a packed step: new row i of sequence b is k_new, v_new row token_start[b] + i (element (t, h, c) at t*stride_t +
+ * h*stride_h + c, t < n_tokens_max), for i < token_start[b + 1] - token_start[b], at most n_new_max of them. Everything else as there.
+ */
+int iq_quantize_append_packed(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* k_new,
+                              const void* v_new, int64_t stride_t, int64_t stride_h, const int32_t* append_pos_dev,
+                              const int32_t* token_start_dev, int32_t n_tokens_max, int32_t n_new_max, const iq_cache* cache,
+                              uint32_t* status_dev, void* stream);
+
+/*
+ * Attention of new tokens over the packed cache, any number of them per sequence. Token t of sequence b stands at position ctx_lens[b] + t, its
+ * row appended there before the call, and attends to the rows up to and with its own (of which those from t_cap on are not there). window
+ * > 0: rows below its position - window + 1 are left out, but for rows below `sinks`.
+ *   q              device binary16; padded: element (b, t, h, c) at b*stride_b + t*stride_t + h*stride_h + c, packed: (token, h, c) at
+ *                  token*stride_t + h*stride_h + c (stride_b is not read). Strides in elements, multiples of 8, not negative; 16-byte aligned.
+ *   ctx_lens_dev   device int32 [batch], clamped to [0, t_cap].
+ *   token_start_dev  device int32 [batch + 1]: packed; or NULL: padded.
+ *   n_tokens_dev   padded: device int32 [batch] tokens per sequence (clamped to [0, n_tokens_max]), or NULL for n_tokens_max everywhere. Packed: NULL.
+ *   n_tokens_max   padded: places per sequence; packed: places in all. 0 .. IQ_CHUNK_MAX_TOKENS.
+ *   window, sinks  >= 0; window = 0: all rows up to the token's own.
+ *   workspace_dev  device, iq_chunk_workspace_bytes(shape) bytes for the device the call runs on, 16-byte aligned; needs no initialisation.
+ *                  Calls that share a workspace must be ordered on one stream (a captured graph shares what it was captured with).
+ *   out            device binary16 [batch][n_tokens_max][n_q_heads][head_dim], packed: [n_tokens_max][n_q_heads][head_dim]; 16-byte aligned. Places
+ *                  without a token are left as they are, as in lse_out.
+ *   lse_out        device fp32, the same without the last dimension, or NULL.
+ *   status_dev     optional (see top). Pages whose rows no token sees need not be in the block table.
+ * Codebooks as for iq_decode_attention; scales must not be negative. A token that sees no row yields out = 0, lse = -inf.
+ * Arithmetic: q~ as two binary16 terms (22 bits of the largest element of 128 (token, head) pairs), levels exact; a row's weight times its V
+ * scale, relative to the largest such of its token, as one binary16 value (2^-12 of it, or 2^-30 of the largest); tensor-core sums
+ * over a CTA's share of the rows, joined in fp32. V scales below 2^-60 count as 2^-60. The same inputs give the same bits in every call on
+ * the same kind of device.
+ * Limits (IQ_ERR_LIMIT): n_tokens_max as above and times the heads per KV head below 2^31 - 128; t_cap at most 2^31 - 2^21; heads per KV head times
+ * t_cap times all tiles of 128 (token, head) pairs below about 2^53.
+ */
+#define IQ_CHUNK_MAX_TOKENS (1 << 20)
+size_t iq_chunk_workspace_bytes(const iq_shape* shape); /* 0: a shape that the calls refuse */
+int iq_chunk_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                       int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                       const int32_t* token_start_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int32_t window, int32_t sinks,
+                       void* workspace_dev, void* out, float* lse_out, uint32_t* status_dev, void* stream);
+/* The same for an encoder's states: every token attends to all rows [0, enc_lens[b]) of its sequence (device int32 [batch], clamped to [0, t_cap]);
+ * the tokens have no rows of their own in the cache. */
+int iq_cross_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                       int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* enc_lens_dev,
+                       const int32_t* token_start_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, void* workspace_dev, void* out,
+                       float* lse_out, uint32_t* status_dev, void* stream);
+/* Diagnostic: iq_chunk_attention (padded, no window) with `polls` (0 .. 65536) as the limit of its waits. 0: a wait that does not find what it
+ * waits for gives up at once, IQ_STATUS_WAIT_TIMEOUT is set, products in flight are waited for before the kernel returns; the outputs are invalid. */
+int iq_selftest_chunk_wait(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                           int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                           const int32_t* n_tokens_dev, int32_t n_tokens_max, void* workspace_dev, void* out, float* lse_out,
+                           uint32_t* status_dev, uint32_t polls, void* stream);
+
 /* A slot count that leaves the decode kernel free to balance the launch when the longest sequence has
  * max_seq_len rows (more slots than needed only cost the writing and merging of unused ones). */
 int32_t iq_suggest_splits(const iq_shape* shape, int32_t max_seq_len);

@@ -35,6 +35,10 @@ class _IqPagePool(ctypes.Structure):
                 ("n_seqs", _i32), ("pages_per_seq", _i32), ("num_pages", _i32), ("page_rows", _i32)]
 
 
+class _IqRotary(ctypes.Structure):
+    _fields_ = [("rotary_dim", _i32), ("interleaved", _i32), ("magnitude", ctypes.c_float), ("turns", ctypes.c_uint64 * 128)]
+
+
 class IQError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -106,6 +110,18 @@ def _load():
     lib.iq_fork_sequences.argtypes = [ctypes.POINTER(_IqShape), ctypes.POINTER(_IqCache), ctypes.POINTER(_IqPagePool), _vp, _vp, _vp,
                                       _i32, _vp, _vp]
     lib.iq_copy_pages.argtypes = [ctypes.POINTER(_IqShape), ctypes.POINTER(_IqCache), _vp, _vp, _i32, _vp, _vp]
+    lib.iq_plan_tokens.argtypes = [ctypes.POINTER(_IqShape), _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.iq_make_rotary.argtypes = [_i32, _i32, ctypes.c_double, _i32, ctypes.c_double, _i32, ctypes.c_double, ctypes.c_double, _vp,
+                                   ctypes.POINTER(_IqRotary)]
+    lib.iq_apply_rotary.argtypes = [ctypes.POINTER(_IqShape), ctypes.POINTER(_IqRotary)] + 2 * [_vp, _i64, _i64, _vp, _i64, _i64] + [_vp, _i32, _vp]
+    lib.iq_quantize_append_packed.argtypes = [ctypes.POINTER(_IqShape), _vp, ctypes.POINTER(_IqCodebook), _vp, _vp, _i64, _i64, _vp, _vp, _i32, _i32,
+                                              ctypes.POINTER(_IqCache), _vp, _vp]
+    lib.iq_chunk_workspace_bytes.argtypes = [ctypes.POINTER(_IqShape)]
+    lib.iq_chunk_workspace_bytes.restype = ctypes.c_size_t
+    head = [ctypes.POINTER(_IqShape), _vp, ctypes.POINTER(_IqCodebook), _vp, _i64, _i64, _i64, ctypes.POINTER(_IqCache), _vp]
+    lib.iq_chunk_attention.argtypes = head + [_vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp]
+    lib.iq_cross_attention.argtypes = head + [_vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp]
+    lib.iq_selftest_chunk_wait.argtypes = head + [_vp, _i32, _vp, _vp, _vp, _vp, ctypes.c_uint32, _vp]
     return lib
 
 
@@ -599,6 +615,159 @@ def iq_copy_pages(shape: Shape, cache: Cache, src_pages_dev, dst_pages_dev, stat
     cs, cc = shape.c(), cache.c()
     _check(_lib.iq_copy_pages(ctypes.byref(cs), ctypes.byref(cc), _ints(src_pages_dev, n), _ints(dst_pages_dev, n), n, _ptr(status_dev),
                               _stream(stream)), "iq_copy_pages")
+
+
+# ------------------------------------------------------------------ steps over requests of any lengths
+IQ_NO_POSITION = -(1 << 31)  # position of the places behind a step's last token
+
+
+@dataclass(frozen=True)
+class Rotary:
+    """Rotary positions as iq_make_rotary lays them out: frequencies in turns per position, 64-bit fractions. Immutable; builds its C struct once."""
+    rotary_dim: int
+    interleaved: bool
+    magnitude: float
+    turns: tuple
+
+    def c(self) -> _IqRotary:
+        cr = self.__dict__.get("_c")
+        if cr is None:
+            assert len(self.turns) == self.rotary_dim // 2
+            cr = _IqRotary(self.rotary_dim, 1 if self.interleaved else 0, self.magnitude)
+            for i, x in enumerate(self.turns):
+                cr.turns[i] = x
+            object.__setattr__(self, "_c", cr)
+        return cr
+
+
+def iq_make_rotary(rotary_dim: int, interleaved: bool = False, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_len: int = 1,
+                   beta_fast: float = 32.0, beta_slow: float = 1.0, inv_freq=None, magnitude: Optional[float] = None) -> Rotary:
+    """scaling: "none", "linear", "base" or "parts" (original_len, beta_fast, beta_slow). inv_freq: rotary_dim / 2 frequencies in radians per
+    position in place of base and scaling. magnitude: instead of the scaling's own."""
+    f = None
+    if inv_freq is not None:
+        assert len(inv_freq) == rotary_dim // 2
+        f = (ctypes.c_double * max(1, len(inv_freq)))(*[float(x) for x in inv_freq])
+    out = _IqRotary()
+    _check(_lib.iq_make_rotary(rotary_dim, 1 if interleaved else 0, base, {"none": 0, "linear": 1, "base": 2, "parts": 3}[scaling], factor, original_len,
+                               beta_fast, beta_slow, f, ctypes.byref(out)), "iq_make_rotary")
+    return Rotary(rotary_dim, bool(interleaved), float(out.magnitude if magnitude is None else magnitude), tuple(out.turns[:rotary_dim // 2]))
+
+
+def _token_rows(x, heads, head_dim):
+    """(tokens, stride between tokens, stride between heads) of x fp16 [tokens][heads][d] or [B][T][heads][d] with evenly spaced tokens."""
+    assert x.dtype is torch.float16 and x.shape[-2] == heads and x.shape[-1] == head_dim and x.stride(-1) == 1
+    if x.dim() == 3:
+        return x.shape[0], x.stride(0), x.stride(1)
+    assert x.dim() == 4
+    assert x.shape[0] <= 1 or x.stride(0) == x.shape[1] * x.stride(1)  # the tokens of all sequences as one run
+    return x.shape[0] * x.shape[1], x.stride(1), x.stride(2)
+
+
+def iq_apply_rotary(shape: Shape, rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream=None) -> None:
+    """Rotary positions of queries q [tokens][H_q][d] and keys k [tokens][H_kv][d] (fp16; also [B][T][...]; strided views, last dim contiguous;
+    either may be None) into q_out, k_out, or in place where these are None. positions: int32, one per token."""
+    n, sides = None, []
+    for x, y, heads in ((q, q_out, shape.n_q_heads), (k, k_out, shape.n_kv_heads)):
+        if x is None:
+            assert y is None
+            sides += [None, 0, 0, None, 0, 0]
+            continue
+        y = x if y is None else y
+        nx, xt, xh = _token_rows(x, heads, shape.head_dim)
+        ny, yt, yh = _token_rows(y, heads, shape.head_dim)
+        assert nx == ny and n in (None, nx)
+        n = nx
+        sides += [x.data_ptr(), xt, xh, y.data_ptr(), yt, yh]
+    assert n is not None
+    _check(_lib.iq_apply_rotary(ctypes.byref(shape.c()), ctypes.byref(rotary.c()), *sides, _ints(positions, n), n, _stream(stream)), "iq_apply_rotary")
+
+
+def iq_plan_tokens(shape: Shape, ctx_lens_dev, n_new_dev, token_start, positions=None, sequences=None, slots=None, block_table=None, page_rows: int = 0,
+                   num_pages: int = 0, n_tokens_max: Optional[int] = None, status_dev=None, stream=None) -> None:
+    """Lays out a packed step: token_start int32 [B + 1], and for each of the step's places positions, sequences (int32) and slots (int64), each
+    [n_tokens_max] or None (n_tokens_max: their size). block_table int32 [B][t_cap / page_rows] or None."""
+    B = shape.batch
+    for t in (positions, sequences, slots):
+        if t is not None:
+            assert n_tokens_max in (None, t.numel())
+            n_tokens_max = t.numel()
+    assert n_tokens_max is not None
+    assert slots is None or (slots.dtype is torch.int64 and slots.is_contiguous())
+    table = None if block_table is None else _ints(block_table, B * (shape.t_cap // page_rows) if page_rows > 0 else block_table.numel())
+    _check(_lib.iq_plan_tokens(ctypes.byref(shape.c()), _ints(ctx_lens_dev, B), _ints(n_new_dev, B), table, page_rows, num_pages, n_tokens_max,
+                               _ints(token_start, B + 1), _ints(positions, n_tokens_max), _ints(sequences, n_tokens_max), _ptr(slots), _ptr(status_dev),
+                               _stream(stream)), "iq_plan_tokens")
+
+
+def iq_quantize_append_packed(shape: Shape, rot_dev, codebook: Codebook, k_new, v_new, append_pos_dev, token_start, n_new_max: int, cache: Cache,
+                              status_dev=None, stream=None) -> None:
+    """iq_quantize_append for packed rows k_new, v_new fp16 [tokens][H_kv][d]: sequence b's are token_start[b] .. token_start[b + 1] - 1, n_new_max
+    of them at most."""
+    assert k_new.dtype == torch.float16 and v_new.dtype == torch.float16 and k_new.shape == v_new.shape
+    assert k_new.dim() == 3 and k_new.shape[1] == shape.n_kv_heads and k_new.shape[2] == shape.head_dim
+    assert k_new.stride() == v_new.stride() and k_new.stride(2) == 1
+    cc = cache.c()
+    _check(_lib.iq_quantize_append_packed(ctypes.byref(shape.c()), _ptr(rot_dev), ctypes.byref(codebook.c()), _ptr(k_new), _ptr(v_new), k_new.stride(0),
+                                          k_new.stride(1), _ints(append_pos_dev, shape.batch), _ints(token_start, shape.batch + 1), k_new.shape[0],
+                                          n_new_max, ctypes.byref(cc), _ptr(status_dev), _stream(stream)), "iq_quantize_append_packed")
+
+
+def iq_chunk_workspace_bytes(shape: Shape) -> int:
+    return int(_lib.iq_chunk_workspace_bytes(ctypes.byref(shape.c())))
+
+
+def _chunk_args(shape, q, workspace, out, lens_dev, token_start, n_tokens, lse_out):
+    """The checked arguments that iq_chunk_attention and iq_cross_attention share: q's strides, lengths, layout."""
+    size, B = q.shape, shape.batch
+    packed = token_start is not None
+    assert q.dtype is torch.float16 and q.dim() == (3 if packed else 4) and size[-2] == shape.n_q_heads and size[-1] == shape.head_dim
+    assert packed or size[0] == B
+    assert out.shape == size and out.is_contiguous() and out.dtype is torch.float16
+    assert lse_out is None or (lse_out.dtype is torch.float32 and lse_out.shape == size[:-1] and lse_out.is_contiguous())
+    assert not (packed and n_tokens is not None)
+    st = q.stride()
+    assert st[-1] == 1
+    sizes = shape.__dict__.get("_chunk_bytes")  # (kept with the shape, like its C struct)
+    if sizes is None:
+        object.__setattr__(shape, "_chunk_bytes", {})
+        sizes = shape._chunk_bytes
+    where = torch.cuda.current_device()         # (the size goes by the device's SMs)
+    if where not in sizes:
+        sizes[where] = iq_chunk_workspace_bytes(shape)
+    assert workspace.nbytes >= sizes[where] and workspace.is_contiguous()
+    return (0 if packed else st[0], st[-3], st[-2]), _ints(lens_dev, B), _ints(token_start, B + 1), _ints(n_tokens, B), size[-3]
+
+
+def iq_chunk_attention(shape: Shape, rot_dev, codebook: Codebook, q, cache: Cache, ctx_lens_dev, workspace, out, token_start=None, n_tokens=None,
+                       window: int = 0, sinks: int = 0, lse_out=None, status_dev=None, stream=None) -> None:
+    """Attention of new tokens, whose rows were appended behind the ctx_lens[b] rows of their sequences: token t sees rows 0 .. ctx_lens[b] + t.
+    Padded: q fp16 [B][T][H_q][d] (any strides with a contiguous last dim), n_tokens int32 [B] or None (T). Packed: q [tokens][H_q][d] and
+    token_start int32 [B + 1]. out fp16, contiguous, q's shape; lse_out fp32, without the last dim. window > 0: only the window's rows and
+    the first `sinks` are seen. workspace: a device uint8 tensor of iq_chunk_workspace_bytes(shape) bytes."""
+    strides, lens, start, count, places = _chunk_args(shape, q, workspace, out, ctx_lens_dev, token_start, n_tokens, lse_out)
+    rc = _lib.iq_chunk_attention(ctypes.byref(shape.c()), rot_dev.data_ptr(), ctypes.byref(codebook.c()), q.data_ptr(), *strides, ctypes.byref(cache.c()),
+                                 lens, start, count, places, window, sinks, workspace.data_ptr(), out.data_ptr(), _ptr(lse_out), _ptr(status_dev),
+                                 _stream(stream))
+    if rc:
+        raise IQError(rc, "iq_chunk_attention")
+
+
+def iq_cross_attention(shape: Shape, rot_dev, codebook: Codebook, q, cache: Cache, enc_lens_dev, workspace, out, token_start=None, n_tokens=None,
+                       lse_out=None, status_dev=None, stream=None) -> None:
+    """The same for an encoder's states: every token of sequence b sees rows 0 .. enc_lens[b] - 1."""
+    strides, lens, start, count, places = _chunk_args(shape, q, workspace, out, enc_lens_dev, token_start, n_tokens, lse_out)
+    rc = _lib.iq_cross_attention(ctypes.byref(shape.c()), rot_dev.data_ptr(), ctypes.byref(codebook.c()), q.data_ptr(), *strides, ctypes.byref(cache.c()),
+                                 lens, start, count, places, workspace.data_ptr(), out.data_ptr(), _ptr(lse_out), _ptr(status_dev), _stream(stream))
+    if rc:
+        raise IQError(rc, "iq_cross_attention")
+
+
+def iq_selftest_chunk_wait(shape: Shape, rot_dev, codebook: Codebook, q, cache: Cache, ctx_lens_dev, workspace, out, status_dev, polls: int, stream=None) -> None:
+    strides, lens, _, _, places = _chunk_args(shape, q, workspace, out, ctx_lens_dev, None, None, None)
+    _check(_lib.iq_selftest_chunk_wait(ctypes.byref(shape.c()), rot_dev.data_ptr(), ctypes.byref(codebook.c()), q.data_ptr(), *strides,
+                                       ctypes.byref(cache.c()), lens, None, places, workspace.data_ptr(), out.data_ptr(), None, _ptr(status_dev), int(polls),
+                                       _stream(stream)), "iq_selftest_chunk_wait")
 
 
 # ------------------------------------------------------------------ small conveniences (allocation only)

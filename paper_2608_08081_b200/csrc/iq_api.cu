@@ -1,5 +1,6 @@
 // C ABI of the IsoQuant library: argument validation and kernel launches. See include/isoquant.h for the
 // contract of every entry point. Nothing here allocates device memory or keeps state between calls.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <vector>
@@ -397,7 +398,8 @@ int iq_make_rotation(int32_t head_dim, int32_t n_kv_heads, uint64_t seed, const 
 static int quantize_append(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* k_new,
                            const void* v_new, int64_t stride_b, int64_t stride_t, int64_t stride_h,
                            const int32_t* append_pos_dev, const int32_t* n_new_dev, int32_t n_new_max,
-                           const iq_cache* cache, uint32_t* status_dev, uint32_t wait_polls, void* stream) {
+                           const int32_t* token_start_dev, int32_t n_rows, const iq_cache* cache, uint32_t* status_dev,
+                           uint32_t wait_polls, void* stream) {
   int rc = check_shape(shape);
   if (rc) return rc;
   if (!rot_dev || !append_pos_dev) return IQ_ERR_NULL;
@@ -419,6 +421,8 @@ static int quantize_append(const iq_shape* shape, const float* rot_dev, const iq
   p.append_pos = append_pos_dev;
   p.n_new = n_new_dev;
   p.n_new_max = n_new_max;
+  p.token_start = token_start_dev;
+  p.n_rows = n_rows;
   p.rot = rot_dev;
   p.bits = shape->bits;
   std::memcpy(p.thresholds_k, side_thresholds(codebook, 0), sizeof(p.thresholds_k));
@@ -442,7 +446,18 @@ int iq_quantize_append(const iq_shape* shape, const float* rot_dev, const iq_cod
                        const int32_t* append_pos_dev, const int32_t* n_new_dev, int32_t n_new_max,
                        const iq_cache* cache, uint32_t* status_dev, void* stream) {
   return quantize_append(shape, rot_dev, codebook, k_new, v_new, stride_b, stride_t, stride_h, append_pos_dev, n_new_dev, n_new_max,
-                         cache, status_dev, iq::DEC_WAIT_LIMIT, stream);
+                         nullptr, 0, cache, status_dev, iq::DEC_WAIT_LIMIT, stream);
+}
+
+int iq_quantize_append_packed(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* k_new,
+                              const void* v_new, int64_t stride_t, int64_t stride_h, const int32_t* append_pos_dev,
+                              const int32_t* token_start_dev, int32_t n_tokens_max, int32_t n_new_max, const iq_cache* cache,
+                              uint32_t* status_dev, void* stream) {
+  if (!token_start_dev) return IQ_ERR_NULL;
+  if (n_tokens_max < 0) return IQ_ERR_SHAPE;
+  return quantize_append(shape, rot_dev, codebook, k_new, v_new, 0, stride_t, stride_h, append_pos_dev, nullptr,
+                         n_new_max < 0 ? n_new_max : std::min(n_new_max, n_tokens_max), token_start_dev, n_tokens_max, cache, status_dev,
+                         iq::DEC_WAIT_LIMIT, stream);
 }
 
 int iq_selftest_append_wait(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* k_new,
@@ -451,7 +466,7 @@ int iq_selftest_append_wait(const iq_shape* shape, const float* rot_dev, const i
                             const iq_cache* cache, uint32_t* status_dev, uint32_t polls, void* stream) {
   if (polls > iq::DEC_WAIT_LIMIT) return IQ_ERR_LIMIT;
   return quantize_append(shape, rot_dev, codebook, k_new, v_new, stride_b, stride_t, stride_h, append_pos_dev, n_new_dev, n_new_max,
-                         cache, status_dev, polls, stream);
+                         nullptr, 0, cache, status_dev, polls, stream);
 }
 
 // Validation and kernel parameters shared by the decode entry points.
@@ -1075,6 +1090,243 @@ int iq_copy_pages(const iq_shape* shape, const iq_cache* cache, const int32_t* s
   p.n = n_pages;
   p.status = status_dev;
   return iq::launch_copy_pages(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+// ---- steps over requests of any lengths
+int iq_plan_tokens(const iq_shape* shape, const int32_t* ctx_lens_dev, const int32_t* n_new_dev, const int32_t* block_table_dev,
+                   int32_t page_rows, int32_t num_pages, int32_t n_tokens_max, int32_t* token_start_dev, int32_t* positions_dev,
+                   int32_t* sequences_dev, int64_t* slots_dev, uint32_t* status_dev, void* stream) {
+  int rc = check_shape(shape);
+  if (rc) return rc;
+  if (block_table_dev && (page_rows <= 0 || (page_rows & 127) || num_pages <= 0 || shape->t_cap % page_rows != 0)) return IQ_ERR_SHAPE;
+  if (n_tokens_max < 0) return IQ_ERR_SHAPE;
+  if (!token_start_dev || (shape->batch > 0 && (!ctx_lens_dev || !n_new_dev))) return IQ_ERR_NULL;
+  iq::PlanParams p = {};
+  p.ctx_lens = ctx_lens_dev;
+  p.n_new = n_new_dev;
+  p.batch = shape->batch;
+  p.n_tokens_max = n_tokens_max;
+  p.pm.table = block_table_dev;
+  p.pm.page_rows = page_rows;
+  p.pm.num_pages = num_pages;
+  p.pm.t_cap = shape->t_cap;
+  p.token_start = token_start_dev;
+  p.positions = positions_dev;
+  p.sequences = sequences_dev;
+  p.slots = slots_dev;
+  p.status = status_dev;
+  return iq::launch_plan_tokens(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+int iq_make_rotary(int32_t rotary_dim, int32_t interleaved, double base, int32_t scaling, double factor, int32_t original_len,
+                   double beta_fast, double beta_slow, const double* inv_freq_host, iq_rotary* out_host) {
+  if (!out_host) return IQ_ERR_NULL;
+  if (rotary_dim <= 0 || (rotary_dim & 15) || rotary_dim > 2 * IQ_ROTARY_MAX_PAIRS) return IQ_ERR_SHAPE;
+  const int pairs = rotary_dim / 2;
+  const long double two_pi = 6.283185307179586476925286766559005768L;
+  long double f[IQ_ROTARY_MAX_PAIRS];
+  double magnitude = 1.0;
+  if (inv_freq_host) {
+    for (int i = 0; i < pairs; i++) {
+      if (!std::isfinite(inv_freq_host[i])) return IQ_ERR_SHAPE;
+      f[i] = inv_freq_host[i];
+    }
+  } else {
+    if (!std::isfinite(base) || !(base > 1.0) || scaling < IQ_ROTARY_PLAIN || scaling > IQ_ROTARY_PARTS) return IQ_ERR_SHAPE;
+    if (scaling != IQ_ROTARY_PLAIN && !(std::isfinite(factor) && factor >= 1.0)) return IQ_ERR_SHAPE;
+    if (scaling == IQ_ROTARY_PARTS && !(original_len >= 1 && std::isfinite(beta_fast) && beta_slow > 0.0 && beta_fast > beta_slow)) return IQ_ERR_SHAPE;
+    long double b = base;
+    if (scaling == IQ_ROTARY_BASE) b *= std::pow((long double)factor, (long double)rotary_dim / (rotary_dim - 2));
+    for (int i = 0; i < pairs; i++) f[i] = std::pow(b, -2.0L * i / rotary_dim);
+    if (scaling == IQ_ROTARY_LINEAR)
+      for (int i = 0; i < pairs; i++) f[i] /= factor;
+    if (scaling == IQ_ROTARY_PARTS) {
+      auto pair = [&](double turns) { return rotary_dim * std::log(original_len / (double)(two_pi * turns)) / (2 * std::log(base)); };
+      const double low = std::fmax(std::floor(pair(beta_fast)), 0.0), high = std::fmin(std::ceil(pair(beta_slow)), rotary_dim - 1.0);
+      for (int i = 0; i < pairs; i++) {
+        const double r = std::fmin(1.0, std::fmax(0.0, (i - low) / std::fmax(high - low, 0.001)));
+        f[i] = f[i] / factor * r + f[i] * (1.0 - r);
+      }
+      magnitude = 0.1 * std::log(factor) + 1.0;
+    }
+  }
+  std::memset(out_host, 0, sizeof(*out_host));
+  out_host->rotary_dim = rotary_dim;
+  out_host->interleaved = interleaved ? 1 : 0;
+  out_host->magnitude = (float)magnitude;
+  for (int i = 0; i < pairs; i++) {
+    long double turns = std::fmod(f[i] / two_pi, 1.0L);
+    if (turns < 0) turns += 1.0L;
+    const long double x = std::round(turns * 18446744073709551616.0L);
+    out_host->turns[i] = x >= 18446744073709551616.0L ? 0 : (uint64_t)x;
+  }
+  return IQ_OK;
+}
+
+int iq_apply_rotary(const iq_shape* shape, const iq_rotary* rotary, const void* q, int64_t q_stride_t, int64_t q_stride_h, void* q_out,
+                    int64_t q_out_stride_t, int64_t q_out_stride_h, const void* k, int64_t k_stride_t, int64_t k_stride_h, void* k_out,
+                    int64_t k_out_stride_t, int64_t k_out_stride_h, const int32_t* positions_dev, int32_t n_tokens, void* stream) {
+  const int rc = check_shape(shape);
+  if (rc) return rc;
+  if (!rotary) return IQ_ERR_NULL;
+  if (rotary->rotary_dim <= 0 || (rotary->rotary_dim & 15) || rotary->rotary_dim > shape->head_dim) return IQ_ERR_SHAPE;
+  if (n_tokens < 0) return IQ_ERR_SHAPE;
+  if (!q && !k) return IQ_ERR_NULL;
+  if ((q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr)) return IQ_ERR_NULL;
+  const int64_t strides[8] = {q_stride_t, q_stride_h, q_out_stride_t, q_out_stride_h, k_stride_t, k_stride_h, k_out_stride_t, k_out_stride_h};
+  for (int i = q ? 0 : 4; i < (k ? 8 : 4); i++) {
+    if (strides[i] < 0) return IQ_ERR_SHAPE;
+    if (strides[i] & 7) return IQ_ERR_ALIGN;
+  }
+  if (!aligned16(q) || !aligned16(q_out) || !aligned16(k) || !aligned16(k_out)) return IQ_ERR_ALIGN;
+  if ((q && q == q_out && (q_stride_t != q_out_stride_t || q_stride_h != q_out_stride_h)) ||
+      (k && k == k_out && (k_stride_t != k_out_stride_t || k_stride_h != k_out_stride_h)))
+    return IQ_ERR_SHAPE;  // in place, with other strides
+  if (n_tokens == 0) return IQ_OK;
+  if (!positions_dev) return IQ_ERR_NULL;
+  iq::RotaryParams p = {};
+  p.side[0] = {static_cast<const __half*>(q), static_cast<__half*>(q_out), q_stride_t, q_stride_h, q_out_stride_t, q_out_stride_h, q ? shape->n_q_heads : 0};
+  p.side[1] = {static_cast<const __half*>(k), static_cast<__half*>(k_out), k_stride_t, k_stride_h, k_out_stride_t, k_out_stride_h, k ? shape->n_kv_heads : 0};
+  p.positions = positions_dev;
+  p.n_tokens = n_tokens;
+  p.head_dim = shape->head_dim;
+  p.rotary = *rotary;
+  return iq::launch_apply_rotary(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+// CTAs of a chunk attention launch, and the sections of its workspace, in bytes from its start.
+namespace {
+struct ChunkPlan {
+  int ctas;
+  size_t part_acc, part_ml, cut_info, total;
+};
+int chunk_plan(const iq_shape* s, ChunkPlan& w) {
+  const int rc = check_shape(s);
+  if (rc) return rc;
+  if (s->t_cap > INT32_MAX - (1 << 21)) return IQ_ERR_LIMIT;
+  w.ctas = sm_count();
+  const size_t rows = 2 * (size_t)w.ctas * 128;
+  size_t o = 0;
+  w.part_acc = o; o += rows * s->head_dim * 4;
+  w.part_ml = o; o += rows * 8;
+  w.cut_info = o; o += (size_t)w.ctas * iq::CHUNK_INFO * 8;
+  w.total = o;
+  return IQ_OK;
+}
+}  // namespace
+
+size_t iq_chunk_workspace_bytes(const iq_shape* shape) {
+  ChunkPlan w;
+  return chunk_plan(shape, w) == IQ_OK ? w.total : 0;
+}
+
+static int chunk_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                           int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                           const int32_t* token_start_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int causal, int32_t window,
+                           int32_t sinks, void* workspace_dev, void* out, float* lse_out, uint32_t* status_dev, uint32_t wait_polls,
+                           void* stream) {
+  ChunkPlan w;
+  int rc = chunk_plan(shape, w);
+  if (rc) return rc;
+  if (!rot_dev || !ctx_lens_dev) return IQ_ERR_NULL;
+  if ((rc = check_codebook(codebook, shape->bits, false))) return rc;
+  int n8[2][16];
+  float delta[2];
+  const bool grid8 = int8_grid(codebook, n8[0], delta[0], n8[1], delta[1]);
+  if (!grid8 && (rc = check_codebook(codebook, shape->bits, true))) return rc;
+  if (!grid8) delta[0] = delta[1] = 1.f;  // levels as they are
+  if ((rc = check_cache(cache, shape))) return rc;
+  if (n_tokens_max < 0 || window < 0 || sinks < 0 || stride_t < 0 || stride_h < 0 || (!token_start_dev && stride_b < 0)) return IQ_ERR_SHAPE;
+  if (token_start_dev && n_tokens_dev) return IQ_ERR_SHAPE;
+  const int group = shape->n_q_heads / shape->n_kv_heads;
+  if (n_tokens_max > IQ_CHUNK_MAX_TOKENS || (long long)n_tokens_max * group >= (1ll << 31) - 128) return IQ_ERR_LIMIT;
+  const double tokens = token_start_dev ? (double)n_tokens_max : (double)n_tokens_max * shape->batch;
+  // units of the launch (chunk_units): tiles times what one can count
+  const double tiles = shape->n_kv_heads * (tokens * group / 128.0 + shape->batch);
+  if (tiles * ((double)group * ((double)shape->t_cap + n_tokens_max + 1024.0) + 256.0) >= 9007199254740992.0) return IQ_ERR_LIMIT;
+  if (shape->batch == 0 || n_tokens_max == 0) return IQ_OK;
+  if (!q || !workspace_dev || !out) return IQ_ERR_NULL;
+  if (!aligned16(q) || !aligned16(rot_dev) || !aligned16(workspace_dev) || !aligned16(out)) return IQ_ERR_ALIGN;
+  if ((!token_start_dev && (stride_b & 7)) || (stride_t & 7) || (stride_h & 7)) return IQ_ERR_ALIGN;
+
+  iq::ChunkParams p = {};
+  p.k_codes = cache->k_codes;
+  p.k_scales = cache->k_scales;
+  p.v_codes = cache->v_codes;
+  p.v_scales = cache->v_scales;
+  p.q = static_cast<const __half*>(q);
+  p.qs_b = stride_b;
+  p.qs_t = stride_t;
+  p.qs_h = stride_h;
+  p.rot = rot_dev;
+  p.ctx_lens = ctx_lens_dev;
+  p.token_start = token_start_dev;
+  p.n_tokens = n_tokens_dev;
+  p.n_tokens_max = n_tokens_max;
+  p.causal = causal;
+  p.window = window;
+  p.sinks = window > 0 ? std::min(sinks, shape->t_cap) : 0;
+  p.batch = shape->batch;
+  p.n_q_heads = shape->n_q_heads;
+  p.n_kv_heads = shape->n_kv_heads;
+  p.group = group;
+  p.t_cap = shape->t_cap;
+  p.pm = page_map(cache, shape);
+  p.scale_f16 = cache->scales_fp16 ? 1 : 0;
+  p.bits = shape->bits;
+  for (int i = 0; i < 1 << shape->bits; i++) {
+    auto put = [&](float level, uint32_t* lo, uint32_t* hi) {
+      const __half x = __float2half_rn(level);
+      uint16_t bits;
+      std::memcpy(&bits, &x, 2);
+      lo[i >> 2] |= (uint32_t)(bits & 0xFFu) << (8 * (i & 3));
+      hi[i >> 2] |= (uint32_t)(bits >> 8) << (8 * (i & 3));
+    };
+    put(grid8 ? (float)n8[0][i] : side_levels(codebook, 0)[i], p.lut_lo, p.lut_hi);
+    put(grid8 ? (float)n8[1][i] : side_levels(codebook, 1)[i], p.lut_v_lo, p.lut_v_hi);
+  }
+  p.lookup = iq::LOOKUP_CONST;
+  const double root_d = std::sqrt((double)shape->head_dim), sm = shape->sm_scale > 0.f ? (double)shape->sm_scale : 1.0 / root_d;
+  p.score_unit = (float)(sm * 1.4426950408889634 * delta[0] / root_d);
+  p.value_unit = (float)(delta[1] / root_d);
+  p.ctas = w.ctas;
+  p.seg_units = (long long)group * 128 * iq::CHUNK_SEG_COST;
+  p.cap_units = window > 0 ? (long long)group * std::min((long long)window + p.sinks, (long long)INT32_MAX) + 256 : 1ll << 60;
+  p.least_units = (long long)group * 128 * iq::CHUNK_LEAST;
+  uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
+  p.part_acc = reinterpret_cast<float*>(ws + w.part_acc);
+  p.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
+  p.cut_info = reinterpret_cast<long long*>(ws + w.cut_info);
+  p.out = static_cast<__half*>(out);
+  p.lse = lse_out;
+  p.status = status_dev;
+  p.wait_polls = wait_polls;
+  return iq::launch_chunk_attention(p, shape->head_dim, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
+}
+
+int iq_chunk_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                       int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                       const int32_t* token_start_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, int32_t window, int32_t sinks,
+                       void* workspace_dev, void* out, float* lse_out, uint32_t* status_dev, void* stream) {
+  return chunk_attention(shape, rot_dev, codebook, q, stride_b, stride_t, stride_h, cache, ctx_lens_dev, token_start_dev, n_tokens_dev,
+                         n_tokens_max, 1, window, sinks, workspace_dev, out, lse_out, status_dev, iq::DEC_WAIT_LIMIT, stream);
+}
+
+int iq_cross_attention(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                       int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* enc_lens_dev,
+                       const int32_t* token_start_dev, const int32_t* n_tokens_dev, int32_t n_tokens_max, void* workspace_dev, void* out,
+                       float* lse_out, uint32_t* status_dev, void* stream) {
+  return chunk_attention(shape, rot_dev, codebook, q, stride_b, stride_t, stride_h, cache, enc_lens_dev, token_start_dev, n_tokens_dev,
+                         n_tokens_max, 0, 0, 0, workspace_dev, out, lse_out, status_dev, iq::DEC_WAIT_LIMIT, stream);
+}
+
+int iq_selftest_chunk_wait(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* q, int64_t stride_b,
+                           int64_t stride_t, int64_t stride_h, const iq_cache* cache, const int32_t* ctx_lens_dev,
+                           const int32_t* n_tokens_dev, int32_t n_tokens_max, void* workspace_dev, void* out, float* lse_out,
+                           uint32_t* status_dev, uint32_t polls, void* stream) {
+  if (polls > iq::DEC_WAIT_LIMIT) return IQ_ERR_LIMIT;
+  return chunk_attention(shape, rot_dev, codebook, q, stride_b, stride_t, stride_h, cache, ctx_lens_dev, nullptr, n_tokens_dev, n_tokens_max,
+                         1, 0, 0, workspace_dev, out, lse_out, status_dev, polls, stream);
 }
 
 int32_t iq_suggest_splits(const iq_shape* shape, int32_t max_seq_len) {

@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(BulkLayout<D>::THREADS, 1) append_bulk_kernel(
 
   // ---- blocks of every sequence; this CTA's share of the tiles
   auto seq_blocks = [&](int b, int& pos0, int& n, long long& blk0) {
-    n = min(p.n_new ? p.n_new[b] : p.n_new_max, p.n_new_max);
+    n = append_rows(p, b);
     pos0 = p.append_pos[b];
     if (n <= 0) { n = 0; blk0 = 0; return 0; }
     blk0 = (long long)pos0 >> 7;  // floor
@@ -570,7 +570,7 @@ __global__ void __launch_bounds__(BulkLayout<D>::THREADS, 1) append_bulk_kernel(
           found = t0 >= 0 && t0 + 128 <= p.t_cap;
           if (!found && lane == 0 && p.status) atomicOr(&p.status[0], IQ_STATUS_ROW_OUT_OF_RANGE);
           if (found) found = cache_row_for_write(p.pm, w.b, h, t0, lane == 0 ? p.status : nullptr, nt.row0);
-          if (found) nt.src = (is_v ? p.v_new : p.k_new) + (size_t)w.b * p.stride_b + (size_t)h * p.stride_h + (t0 - (long long)w.pos0) * p.stride_t;
+          if (found) nt.src = (is_v ? p.v_new : p.k_new) + append_source(p, w.b) + (size_t)h * p.stride_h + (t0 - (long long)w.pos0) * p.stride_t;
           else if (lane == 0 && p.status) atomicAdd(&p.status[2], (unsigned)(nt.c_hi - nt.c_lo));
         }
         if (lane == 0) {

@@ -1,0 +1,6 @@
+// The chunk attention kernel for 3-bit codes.
+#include "iq_chunk_kernel.cuh"
+
+namespace iq {
+cudaError_t launch_chunk_b3(const ChunkParams& p, int head_dim, cudaStream_t stream) { return chunk_launch<3>(p, head_dim, stream); }
+}  // namespace iq

@@ -1,0 +1,186 @@
+// Chunk and cross attention: which rows a tile of queries sees, and how the launch's work is dealt out.
+#pragma once
+#include "iq_decode_common.cuh"
+
+namespace iq {
+
+constexpr int CHUNK_ROWS = 128;  // (token, query head) pairs of a tile: the rows of a product
+
+// One sequence of the launch.
+struct ChunkSeq {
+  int ctx, n, tiles;    // cached rows before its tokens (cross attention: all it has), tokens, tiles per KV head
+  long long tok0;       // its first token among those of q and out, where they are packed; else batch row times n_tokens_max
+};
+__device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams& p, int b) {
+  ChunkSeq s;
+  s.ctx = max(0, min(p.ctx_lens[b], p.t_cap));
+  if (p.token_start) {
+    const int first = max(0, min(p.token_start[b], p.n_tokens_max));
+    s.n = max(0, min(p.token_start[b + 1], p.n_tokens_max) - first);
+    s.tok0 = first;
+  } else {
+    s.n = p.n_tokens ? max(0, min(p.n_tokens[b], p.n_tokens_max)) : p.n_tokens_max;
+    s.tok0 = (long long)b * p.n_tokens_max;
+  }
+  s.tiles = (int)(((long long)s.n * p.group + CHUNK_ROWS - 1) / CHUNK_ROWS);
+  return s;
+}
+
+// Work is counted in units of 1 / group of a row: a tile counts the rows that its last token sees, a little rounded so that the sum over
+// the first tiles of a sequence has a closed form, and p.seg_units more for its beginning and end.
+__device__ __forceinline__ long long chunk_units(const ChunkParams& p, const ChunkSeq& s, int t) {
+  const long long v = (long long)p.group * s.ctx;
+  return p.seg_units + (p.causal ? min(v + (long long)CHUNK_ROWS * (t + 1), p.cap_units) : v);
+}
+// Units of tiles 0 .. t - 1 of a KV head.
+__device__ __forceinline__ long long chunk_units_before(const ChunkParams& p, const ChunkSeq& s, int t) {
+  const long long v = (long long)p.group * s.ctx;
+  if (!p.causal) return t * (p.seg_units + v);
+  const long long m = max(0ll, min((long long)t, (p.cap_units - v) / CHUNK_ROWS));  // tiles below the cap
+  return t * p.seg_units + m * v + CHUNK_ROWS * (m * (m + 1) / 2) + (t - m) * p.cap_units;
+}
+__device__ __forceinline__ long long chunk_seq_units(const ChunkParams& p, const ChunkSeq& s) {
+  return (long long)p.n_kv_heads * chunk_units_before(p, s, s.tiles);
+}
+// (The products of most launches fit 32 bits, whose division takes a fraction of the time.)
+__device__ __forceinline__ long long chunk_div(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+__device__ __forceinline__ long long chunk_cut(long long total, int cta, int ctas) { return chunk_div(total * cta, ctas); }
+
+// The blocks of 128 rows that a tile's tokens see: the first `sink_blocks`, then those from the first window on.
+struct ChunkTile {
+  int t0, t1;                      // first and last token
+  int end;                         // rows behind this are seen by none of them
+  int blocks, sink_blocks, first;
+  __device__ __forceinline__ int block(int v) const { return v < sink_blocks ? v : v - sink_blocks + first; }
+};
+__device__ __forceinline__ ChunkTile chunk_tile(const ChunkParams& p, const ChunkSeq& s, int t) {
+  ChunkTile x;
+  x.t0 = t * CHUNK_ROWS / p.group;  // (n_tokens_max * group fits 31 bits: the host's limit)
+  x.t1 = min(s.n - 1, (t * CHUNK_ROWS + CHUNK_ROWS - 1) / p.group);
+  x.end = p.causal ? min(s.ctx + x.t1 + 1, p.t_cap) : s.ctx;
+  const int total = (x.end + 127) >> 7;
+  x.first = p.window > 0 ? min(total, max(0, s.ctx + x.t0 - p.window + 1) >> 7) : 0;
+  x.sink_blocks = min((p.sinks >> 7) + ((p.sinks & 127) != 0), x.first);
+  x.blocks = total - x.first + x.sink_blocks;
+  return x;
+}
+// Blocks of an item before its unit o.
+__device__ __forceinline__ int chunk_blocks_before(const ChunkParams& p, long long o, long long units, int blocks) {
+  if (o >= units) return blocks;
+  return o <= p.seg_units ? 0 : (int)chunk_div((o - p.seg_units) * blocks, units - p.seg_units);
+}
+
+// The launch's items (sequence, KV head, tile), laid end to end and cut into one range of equal length per CTA.
+struct ChunkRange {
+  long long at, end, total;  // units
+  long long seq_at;          // where sequence b, in which the range starts, starts
+  int b, ctas;               // CTAs that have a range
+};
+// By one converged warp.
+__device__ __forceinline__ ChunkRange chunk_range(const ChunkParams& p, int lane) {
+  ChunkRange r;
+  long long total = 0;
+  for (int b = lane; b < p.batch; b += 32) total += chunk_seq_units(p, chunk_seq(p, b));
+#pragma unroll 1
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(FULL, total, o);
+  r.total = total;
+  r.ctas = (int)max(1ll, min((long long)p.ctas, total / p.least_units));
+  r.at = r.end = total;
+  r.b = 0;
+  r.seq_at = 0;
+  if (total == 0 || blockIdx.x >= r.ctas) return r;
+  r.at = chunk_cut(total, blockIdx.x, r.ctas);
+  r.end = chunk_cut(total, blockIdx.x + 1, r.ctas);
+  for (int b0 = 0;; b0 += 32) {
+    const long long w = b0 + lane < p.batch ? chunk_seq_units(p, chunk_seq(p, b0 + lane)) : 0;
+    long long x = w;
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(FULL, x, o);
+      if (lane >= o) x += y;
+    }
+    const uint32_t behind = __ballot_sync(FULL, r.at < r.seq_at + x);
+    if (behind) {
+      const int at = __ffs(behind) - 1;
+      r.b = b0 + at;
+      r.seq_at += __shfl_sync(FULL, x - w, at);
+      return r;
+    }
+    r.seq_at += __shfl_sync(FULL, x, 31);
+  }
+}
+
+// A piece: the blocks [lo, hi) of an item that lie in this CTA's range.
+struct ChunkPiece {
+  ChunkSeq sq;
+  ChunkTile x;
+  int b, g, t;
+  int lo, hi;
+  int slot;  // of its partial; -1: it is the whole item
+};
+// The pieces of a range, one after the other; every warp walks for itself.
+struct ChunkWalk {
+  ChunkSeq sq;
+  int b, g, t;
+  long long unit, end, item_at;  // next unit, end of the range, where item (b, g, t) starts
+  bool begun;                    // that item begins in this range
+  int info_b, info_g, info_t;    // the item that begins here and ends in a later range (-1: none) ...
+  long long info_at;             // ... and where it starts
+  __device__ __forceinline__ void start(const ChunkParams& p, const ChunkRange& r) {
+    unit = r.at;
+    end = r.end;
+    info_b = -1;
+    info_g = info_t = 0;
+    info_at = 0;
+    b = g = t = 0;
+    item_at = 0;
+    begun = true;
+    if (unit >= end) return;
+    b = r.b;
+    sq = chunk_seq(p, b);
+    const long long head = chunk_units_before(p, sq, sq.tiles);
+    long long rest = unit - r.seq_at;
+    g = (int)chunk_div(rest, head);
+    rest -= g * head;
+    int lo = 0, hi = sq.tiles;  // the last tile that starts at or before it
+    while (hi - lo > 1) {
+      const int m = (lo + hi) >> 1;
+      if (chunk_units_before(p, sq, m) <= rest) lo = m; else hi = m;
+    }
+    t = lo;
+    item_at = unit - (rest - chunk_units_before(p, sq, t));
+    begun = item_at == unit;
+  }
+  // False: the range is done. A piece without blocks is an item that no token of sees a row.
+  __device__ __forceinline__ bool next(const ChunkParams& p, ChunkPiece& c) {
+    while (unit < end) {
+      const long long units = chunk_units(p, sq, t);
+      c.sq = sq;
+      c.b = b;
+      c.g = g;
+      c.t = t;
+      c.x = chunk_tile(p, sq, t);
+      c.lo = chunk_blocks_before(p, unit - item_at, units, c.x.blocks);
+      c.hi = chunk_blocks_before(p, end - item_at, units, c.x.blocks);
+      c.slot = c.lo == 0 && c.hi == c.x.blocks ? -1 : 2 * (int)blockIdx.x + (begun ? 1 : 0);
+      const bool first = begun;
+      if (begun && item_at + units > end) { info_b = b; info_g = g; info_t = t; info_at = item_at; }
+      unit = min(end, item_at + units);
+      item_at += units;
+      begun = true;
+      if (++t == sq.tiles && unit < end) {
+        t = 0;
+        if (++g == p.n_kv_heads) {
+          g = 0;
+          do sq = chunk_seq(p, ++b); while (sq.tiles == 0);  // (units are left, so there is such a sequence)
+        }
+      }
+      if (c.hi > c.lo || (c.x.blocks == 0 && first)) return true;
+    }
+    return false;
+  }
+};
+
+}  // namespace iq

@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../../include/isoquant.h"
+
 namespace iq {
 
 // Polls one mbarrier wait of a kernel may take before it gives up (IQ_STATUS_WAIT_TIMEOUT; the reconstruction: rows of NaN):
@@ -29,6 +31,8 @@ struct QuantizeParams {
   const int32_t* append_pos;
   const int32_t* n_new;
   int n_new_max;
+  const int32_t* token_start;  // [batch + 1]: packed rows, n_rows of them in all (stride_b and n_new are then not read); or nullptr
+  int n_rows;
   const float* rot;
   int bits;                 // 2, 3 or 4
   float thresholds_k[15];   // the first 2^bits - 1 are read
@@ -44,6 +48,17 @@ struct QuantizeParams {
   float big;                // bulk: 0.5 over the band around a threshold (set by the launcher)
   uint32_t wait_polls;      // bulk: limit of the waits for tensor-core results: DEC_WAIT_LIMIT, or what the self-test asks for
 };
+#ifdef __CUDACC__
+// New rows of sequence b, and where its first one starts, in elements from k_new or v_new.
+__device__ __forceinline__ int append_rows(const QuantizeParams& p, int b) {
+  int n = p.n_new ? p.n_new[b] : p.n_new_max;
+  if (p.token_start) n = min(p.token_start[b + 1], p.n_rows) - max(0, min(p.token_start[b], p.n_rows));
+  return min(n, p.n_new_max);
+}
+__device__ __forceinline__ size_t append_source(const QuantizeParams& p, int b) {
+  return p.token_start ? (size_t)max(0, min(p.token_start[b], p.n_rows)) * p.stride_t : (size_t)b * p.stride_b;
+}
+#endif
 cudaError_t launch_quantize_append(const QuantizeParams& p, int head_dim, int batch, cudaStream_t stream);
 bool append_bulk_takes(const QuantizeParams& p, int head_dim);
 cudaError_t launch_append_bulk(const QuantizeParams& p, int head_dim, int batch, cudaStream_t stream);
@@ -215,6 +230,74 @@ cudaError_t launch_tree_attention(const TreeParams& p, int head_dim, cudaStream_
 // tokens and 8 heads per KV head, 112 us instead of 130
 constexpr int tree_ctas_per_sm(int head_dim, int tile) { return head_dim == 128 && tile <= 32 ? 2 : 1; }
 int tree_tile(int queries);  // tile for that many (token, head) pairs of a KV head
+
+// ---- chunk and cross attention: any number of new tokens over the packed cache
+struct ChunkParams {
+  const uint8_t* k_codes;
+  const float* k_scales;
+  const uint8_t* v_codes;
+  const float* v_scales;
+  const __half* q;
+  long long qs_b, qs_t, qs_h;  // strides of q, in elements (packed tokens: qs_b is not read)
+  const float* rot;
+  const int32_t* ctx_lens;
+  const int32_t* token_start;  // [batch + 1]: packed tokens, n_tokens_max of them in all; or nullptr: n_tokens_max places per sequence
+  const int32_t* n_tokens;     // [batch], or nullptr
+  int n_tokens_max, causal, window, sinks;
+  int batch, n_q_heads, n_kv_heads, group, t_cap;
+  PageMap pm;
+  int scale_f16;
+  int bits;
+  // The levels as binary16 values, exact, times a unit per side (8-bit grid: the integers and delta; else the levels and 1). Low and high
+  // bytes, 4 per register.
+  uint32_t lut_lo[4], lut_hi[4], lut_v_lo[4], lut_v_hi[4];
+  LookupConst lookup;
+  float score_unit;            // sm_scale log2(e) unit_K / sqrt(d)
+  float value_unit;            // unit_V / sqrt(d)
+  int ctas;                    // CTAs of the launch
+  long long seg_units, cap_units, least_units;  // see chunk_units; a launch has no more CTAs at work than total / least_units
+  // Workspace. Of a CTA's items at most the first and the last are cut: two partials each.
+  float* part_acc;             // [2 ctas][128][head_dim], rotated space
+  float* part_ml;              // [2 ctas][128][2]: reference (log2 units), sum
+  long long* cut_info;         // [ctas][4]: the item that begins in the CTA's range and ends in a later one
+  __half* out;
+  float* lse;
+  uint32_t* status;
+  uint32_t wait_polls;
+};
+constexpr int CHUNK_INFO = 4;
+// What an item costs beside its blocks (queries, outputs or a partial), and the least that a CTA is given, in blocks.
+constexpr int CHUNK_SEG_COST = 3, CHUNK_LEAST = 2;
+cudaError_t launch_chunk_attention(const ChunkParams& p, int head_dim, cudaStream_t stream);
+
+// ---- a step's tokens: places, positions, cache rows
+struct PlanParams {
+  const int32_t* ctx_lens;
+  const int32_t* n_new;
+  int batch, n_tokens_max;
+  PageMap pm;
+  int32_t* token_start;
+  int32_t* positions;
+  int32_t* sequences;
+  int64_t* slots;
+  uint32_t* status;
+};
+cudaError_t launch_plan_tokens(const PlanParams& p, cudaStream_t stream);
+
+// ---- rotary positions
+struct RotarySide {
+  const __half* x;
+  __half* y;
+  long long xs_t, xs_h, ys_t, ys_h;  // strides in elements
+  int heads;
+};
+struct RotaryParams {
+  RotarySide side[2];
+  const int32_t* positions;
+  int n_tokens, head_dim;
+  iq_rotary rotary;
+};
+cudaError_t launch_apply_rotary(const RotaryParams& p, cudaStream_t stream);
 
 // ---- rows and pages of the cache
 struct CacheArrays {

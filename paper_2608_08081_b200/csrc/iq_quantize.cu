@@ -123,8 +123,7 @@ __global__ void __launch_bounds__(32) quantize_append_few_kernel(const __grid_co
   const bool is_v = (blockIdx.x & 1) != 0;
   const int chunk = blockIdx.x >> 1;  // the warp takes the rows that fall into one 128-row block of the cache
   const int h = blockIdx.y, b = blockIdx.z;
-  int n_new = p.n_new ? p.n_new[b] : p.n_new_max;
-  n_new = min(n_new, p.n_new_max);
+  const int n_new = append_rows(p, b);
   if (n_new <= 0) return;
   const long long pos0 = p.append_pos[b];
   // rows i with floor((pos0 + i) / 128) == floor(pos0 / 128) + chunk (rows at negative positions: chunk 0, they are refused below)
@@ -132,7 +131,7 @@ __global__ void __launch_bounds__(32) quantize_append_few_kernel(const __grid_co
   const long long lo = max(0ll, (blk0 + chunk) * 128 - pos0), hi = min((long long)n_new, (blk0 + chunk + 1) * 128 - pos0);
   const int i_lo = (int)((chunk == 0) ? 0 : lo), i_hi = (int)hi;
   if (i_lo >= i_hi) return;
-  const __half* src_base = (is_v ? p.v_new : p.k_new) + (size_t)b * p.stride_b + (size_t)h * p.stride_h + lane * E;
+  const __half* src_base = (is_v ? p.v_new : p.k_new) + append_source(p, b) + (size_t)h * p.stride_h + lane * E;
   __half2 raw[E / 2];  // the first row is requested before the rotation blocks are set up: two latencies in one
 #pragma unroll
   for (int k = 0; k < E / 2; k++) raw[k] = reinterpret_cast<const __half2*>(src_base + (size_t)i_lo * p.stride_t)[k];
