@@ -1194,22 +1194,22 @@ int iq_apply_rotary(const iq_shape* shape, const iq_rotary* rotary, const void* 
   return iq::launch_apply_rotary(p, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
 }
 
-// CTAs of a chunk attention launch, and the sections of its workspace, in bytes from its start.
+// Pairs of CTAs of a chunk attention launch, and the sections of its workspace, in bytes from its start.
 namespace {
 struct ChunkPlan {
-  int ctas;
+  int pairs;
   size_t part_acc, part_ml, cut_info, total;
 };
 int chunk_plan(const iq_shape* s, ChunkPlan& w) {
   const int rc = check_shape(s);
   if (rc) return rc;
   if (s->t_cap > INT32_MAX - (1 << 21)) return IQ_ERR_LIMIT;
-  w.ctas = sm_count();
-  const size_t rows = 2 * (size_t)w.ctas * 128;
+  w.pairs = std::max(1, sm_count() / 2);
+  const size_t rows = 2 * (size_t)w.pairs * 256;
   size_t o = 0;
   w.part_acc = o; o += rows * s->head_dim * 4;
   w.part_ml = o; o += rows * 8;
-  w.cut_info = o; o += (size_t)w.ctas * iq::CHUNK_INFO * 8;
+  w.cut_info = o; o += (size_t)w.pairs * iq::CHUNK_INFO * 8;
   w.total = o;
   return IQ_OK;
 }
@@ -1289,9 +1289,9 @@ static int chunk_attention(const iq_shape* shape, const float* rot_dev, const iq
   const double root_d = std::sqrt((double)shape->head_dim), sm = shape->sm_scale > 0.f ? (double)shape->sm_scale : 1.0 / root_d;
   p.score_unit = (float)(sm * 1.4426950408889634 * delta[0] / root_d);
   p.value_unit = (float)(delta[1] / root_d);
-  p.ctas = w.ctas;
+  p.pairs = w.pairs;
   p.seg_units = (long long)group * 128 * iq::CHUNK_SEG_COST;
-  p.cap_units = window > 0 ? (long long)group * std::min((long long)window + p.sinks, (long long)INT32_MAX) + 256 : 1ll << 60;
+  p.cap_units = window > 0 ? (long long)group * std::min((long long)window + p.sinks, (long long)INT32_MAX) + 512 : 1ll << 60;
   p.least_units = (long long)group * 128 * iq::CHUNK_LEAST;
   uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
   p.part_acc = reinterpret_cast<float*>(ws + w.part_acc);

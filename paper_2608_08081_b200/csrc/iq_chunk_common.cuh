@@ -4,7 +4,7 @@
 
 namespace iq {
 
-constexpr int CHUNK_ROWS = 128;  // (token, query head) pairs of a tile: the rows of a product
+constexpr int CHUNK_ROWS = 256;  // (token, query head) pairs of a tile: the rows of a product of two SMs
 
 // One sequence of the launch.
 struct ChunkSeq {
@@ -46,7 +46,7 @@ __device__ __forceinline__ long long chunk_seq_units(const ChunkParams& p, const
 __device__ __forceinline__ long long chunk_div(long long a, long long b) {
   return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
-__device__ __forceinline__ long long chunk_cut(long long total, int cta, int ctas) { return chunk_div(total * cta, ctas); }
+__device__ __forceinline__ long long chunk_cut(long long total, int pair, int pairs) { return chunk_div(total * pair, pairs); }
 
 // The blocks of 128 rows that a tile's tokens see: the first `sink_blocks`, then those from the first window on.
 struct ChunkTile {
@@ -72,27 +72,27 @@ __device__ __forceinline__ int chunk_blocks_before(const ChunkParams& p, long lo
   return o <= p.seg_units ? 0 : (int)chunk_div((o - p.seg_units) * blocks, units - p.seg_units);
 }
 
-// The launch's items (sequence, KV head, tile), laid end to end and cut into one range of equal length per CTA.
+// The launch's items (sequence, KV head, tile), laid end to end and cut into one range of equal length per pair of CTAs.
 struct ChunkRange {
   long long at, end, total;  // units
   long long seq_at;          // where sequence b, in which the range starts, starts
-  int b, ctas;               // CTAs that have a range
+  int b, pairs;              // pairs of CTAs that have a range
 };
 // By one converged warp.
-__device__ __forceinline__ ChunkRange chunk_range(const ChunkParams& p, int lane) {
+__device__ __forceinline__ ChunkRange chunk_range(const ChunkParams& p, int pair, int lane) {
   ChunkRange r;
   long long total = 0;
   for (int b = lane; b < p.batch; b += 32) total += chunk_seq_units(p, chunk_seq(p, b));
 #pragma unroll 1
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(FULL, total, o);
   r.total = total;
-  r.ctas = (int)max(1ll, min((long long)p.ctas, total / p.least_units));
+  r.pairs = (int)max(1ll, min((long long)p.pairs, total / p.least_units));
   r.at = r.end = total;
   r.b = 0;
   r.seq_at = 0;
-  if (total == 0 || blockIdx.x >= r.ctas) return r;
-  r.at = chunk_cut(total, blockIdx.x, r.ctas);
-  r.end = chunk_cut(total, blockIdx.x + 1, r.ctas);
+  if (total == 0 || pair >= r.pairs) return r;
+  r.at = chunk_cut(total, pair, r.pairs);
+  r.end = chunk_cut(total, pair + 1, r.pairs);
   for (int b0 = 0;; b0 += 32) {
     const long long w = b0 + lane < p.batch ? chunk_seq_units(p, chunk_seq(p, b0 + lane)) : 0;
     long long x = w;
@@ -112,7 +112,7 @@ __device__ __forceinline__ ChunkRange chunk_range(const ChunkParams& p, int lane
   }
 }
 
-// A piece: the blocks [lo, hi) of an item that lie in this CTA's range.
+// A piece: the blocks [lo, hi) of an item that lie in this pair's range.
 struct ChunkPiece {
   ChunkSeq sq;
   ChunkTile x;
@@ -164,7 +164,7 @@ struct ChunkWalk {
       c.x = chunk_tile(p, sq, t);
       c.lo = chunk_blocks_before(p, unit - item_at, units, c.x.blocks);
       c.hi = chunk_blocks_before(p, end - item_at, units, c.x.blocks);
-      c.slot = c.lo == 0 && c.hi == c.x.blocks ? -1 : 2 * (int)blockIdx.x + (begun ? 1 : 0);
+      c.slot = c.lo == 0 && c.hi == c.x.blocks ? -1 : 2 * (int)(blockIdx.x >> 1) + (begun ? 1 : 0);
       const bool first = begun;
       if (begun && item_at + units > end) { info_b = b; info_g = g; info_t = t; info_at = item_at; }
       unit = min(end, item_at + units);

@@ -254,19 +254,19 @@ struct ChunkParams {
   LookupConst lookup;
   float score_unit;            // sm_scale log2(e) unit_K / sqrt(d)
   float value_unit;            // unit_V / sqrt(d)
-  int ctas;                    // CTAs of the launch
-  long long seg_units, cap_units, least_units;  // see chunk_units; a launch has no more CTAs at work than total / least_units
-  // Workspace. Of a CTA's items at most the first and the last are cut: two partials each.
-  float* part_acc;             // [2 ctas][128][head_dim], rotated space
-  float* part_ml;              // [2 ctas][128][2]: reference (log2 units), sum
-  long long* cut_info;         // [ctas][4]: the item that begins in the CTA's range and ends in a later one
+  int pairs;                   // pairs of CTAs of the launch
+  long long seg_units, cap_units, least_units;  // see chunk_units; a launch has no more pairs at work than total / least_units
+  // Workspace. Of a pair's items at most the first and the last are cut: two partials each.
+  float* part_acc;             // [2 pairs][256][head_dim], rotated space
+  float* part_ml;              // [2 pairs][256][2]: reference (log2 units), sum
+  long long* cut_info;         // [pairs][4]: the item that begins in the pair's range and ends in a later one
   __half* out;
   float* lse;
   uint32_t* status;
   uint32_t wait_polls;
 };
 constexpr int CHUNK_INFO = 4;
-// What an item costs beside its blocks (queries, outputs or a partial), and the least that a CTA is given, in blocks.
+// What an item costs beside its blocks (queries, outputs or a partial), and the least that a pair of CTAs is given, in blocks.
 constexpr int CHUNK_SEG_COST = 3, CHUNK_LEAST = 2;
 cudaError_t launch_chunk_attention(const ChunkParams& p, int head_dim, cudaStream_t stream);
 
