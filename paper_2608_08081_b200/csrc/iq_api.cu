@@ -888,6 +888,50 @@ int tree_plan(const iq_shape* s, int32_t n_tokens_max, TreePlan& w) {
   w.total = o;
   return IQ_OK;
 }
+// What a tree attention launch needs of the cache, the codebook and the windows (arguments that have been checked).
+iq::TreeParams tree_params(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const iq_cache* cache, int32_t window, int32_t sinks) {
+  int n8[2][16];
+  float delta[2];
+  const bool grid8 = int8_grid(codebook, n8[0], delta[0], n8[1], delta[1]);
+  if (!grid8) delta[0] = delta[1] = 1.f;  // levels as they are
+  iq::TreeParams p = {};
+  p.k_codes = cache->k_codes;
+  p.k_scales = cache->k_scales;
+  p.v_codes = cache->v_codes;
+  p.v_scales = cache->v_scales;
+  p.rot = rot_dev;
+  p.window = window;
+  p.sinks = sinks;
+  p.batch = shape->batch;
+  p.n_q_heads = shape->n_q_heads;
+  p.n_kv_heads = shape->n_kv_heads;
+  p.group = shape->n_q_heads / shape->n_kv_heads;
+  p.t_cap = shape->t_cap;
+  p.pm = page_map(cache, shape);
+  p.scale_f16 = cache->scales_fp16 ? 1 : 0;
+  p.bits = shape->bits;
+  p.v_terms = 1;
+  for (int i = 0; i < 1 << shape->bits; i++) {
+    auto put = [&](auto x, uint32_t* lo, uint32_t* hi) {
+      uint16_t bits;
+      std::memcpy(&bits, &x, 2);
+      lo[i >> 2] |= (uint32_t)(bits & 0xFFu) << (8 * (i & 3));
+      hi[i >> 2] |= (uint32_t)(bits >> 8) << (8 * (i & 3));
+    };
+    put(__float2half_rn(grid8 ? (float)n8[0][i] : side_levels(codebook, 0)[i]), p.lut_lo, p.lut_hi);
+    const float level = grid8 ? (float)n8[1][i] : side_levels(codebook, 1)[i];
+    const __nv_bfloat16 first = __float2bfloat16_rn(level);
+    const float rest = level - __bfloat162float(first);  // (at most 3 of the 11 bits of a binary16 value)
+    put(first, p.lut_v_lo[0], p.lut_v_hi[0]);
+    put(__float2bfloat16_rn(rest), p.lut_v_lo[1], p.lut_v_hi[1]);
+    if (rest != 0.f) p.v_terms = 2;
+  }
+  p.lookup = iq::LOOKUP_CONST;
+  const double root_d = std::sqrt((double)shape->head_dim), sm = shape->sm_scale > 0.f ? (double)shape->sm_scale : 1.0 / root_d;
+  p.score_unit = (float)(sm * 1.4426950408889634 * delta[0] / root_d);
+  p.value_unit = (float)(delta[1] / root_d);
+  return p;
+}
 iq::CacheArrays cache_arrays(const iq_cache* c) { return {c->k_codes, c->k_scales, c->v_codes, c->v_scales, c->scales_fp16 ? 1 : 0}; }
 
 int check_pool(const iq_page_pool* p) {
@@ -919,9 +963,7 @@ static int tree_attention(const iq_shape* shape, const float* rot_dev, const iq_
   if ((rc = check_codebook(codebook, shape->bits, false))) return rc;
   int n8[2][16];
   float delta[2];
-  const bool grid8 = int8_grid(codebook, n8[0], delta[0], n8[1], delta[1]);
-  if (!grid8 && (rc = check_codebook(codebook, shape->bits, true))) return rc;
-  if (!grid8) delta[0] = delta[1] = 1.f;  // levels as they are
+  if (!int8_grid(codebook, n8[0], delta[0], n8[1], delta[1]) && (rc = check_codebook(codebook, shape->bits, true))) return rc;
   if ((rc = check_cache(cache, shape))) return rc;
   if (window < 0 || sinks < 0 || stride_b < 0 || stride_t < 0 || stride_h < 0) return IQ_ERR_SHAPE;
   if (shape->batch == 0 || n_tokens_max == 0) return IQ_OK;
@@ -929,51 +971,16 @@ static int tree_attention(const iq_shape* shape, const float* rot_dev, const iq_
   if (!aligned16(q) || !aligned16(rot_dev) || !aligned16(workspace_dev) || !aligned16(out)) return IQ_ERR_ALIGN;
   if ((stride_b & 7) || (stride_t & 7) || (stride_h & 7)) return IQ_ERR_ALIGN;
 
-  iq::TreeParams p = {};
-  p.k_codes = cache->k_codes;
-  p.k_scales = cache->k_scales;
-  p.v_codes = cache->v_codes;
-  p.v_scales = cache->v_scales;
+  iq::TreeParams p = tree_params(shape, rot_dev, codebook, cache, window, sinks);
   p.q = static_cast<const __half*>(q);
   p.qs_b = stride_b;
   p.qs_t = stride_t;
   p.qs_h = stride_h;
-  p.rot = rot_dev;
   p.ctx_lens = ctx_lens_dev;
   p.mask = tree_mask_dev;
   p.n_tokens = n_tokens_dev;
-  p.n_tokens_max = n_tokens_max;
+  p.n_tokens_max = p.places = n_tokens_max;
   p.mask_words = (n_tokens_max + 31) / 32;
-  p.window = window;
-  p.sinks = sinks;
-  p.batch = shape->batch;
-  p.n_q_heads = shape->n_q_heads;
-  p.n_kv_heads = shape->n_kv_heads;
-  p.group = shape->n_q_heads / shape->n_kv_heads;
-  p.t_cap = shape->t_cap;
-  p.pm = page_map(cache, shape);
-  p.scale_f16 = cache->scales_fp16 ? 1 : 0;
-  p.bits = shape->bits;
-  p.v_terms = 1;
-  for (int i = 0; i < 1 << shape->bits; i++) {
-    auto put = [&](auto x, uint32_t* lo, uint32_t* hi) {
-      uint16_t bits;
-      std::memcpy(&bits, &x, 2);
-      lo[i >> 2] |= (uint32_t)(bits & 0xFFu) << (8 * (i & 3));
-      hi[i >> 2] |= (uint32_t)(bits >> 8) << (8 * (i & 3));
-    };
-    put(__float2half_rn(grid8 ? (float)n8[0][i] : side_levels(codebook, 0)[i]), p.lut_lo, p.lut_hi);
-    const float level = grid8 ? (float)n8[1][i] : side_levels(codebook, 1)[i];
-    const __nv_bfloat16 first = __float2bfloat16_rn(level);
-    const float rest = level - __bfloat162float(first);  // (at most 3 of the 11 bits of a binary16 value)
-    put(first, p.lut_v_lo[0], p.lut_v_hi[0]);
-    put(__float2bfloat16_rn(rest), p.lut_v_lo[1], p.lut_v_hi[1]);
-    if (rest != 0.f) p.v_terms = 2;
-  }
-  p.lookup = iq::LOOKUP_CONST;
-  const double root_d = std::sqrt((double)shape->head_dim), sm = shape->sm_scale > 0.f ? (double)shape->sm_scale : 1.0 / root_d;
-  p.score_unit = (float)(sm * 1.4426950408889634 * delta[0] / root_d);
-  p.value_unit = (float)(delta[1] / root_d);
   p.tile = w.tile;
   p.tiles = w.tiles;
   p.ctas = w.ctas;
@@ -1196,9 +1203,11 @@ int iq_apply_rotary(const iq_shape* shape, const iq_rotary* rotary, const void* 
 
 // Pairs of CTAs of a chunk attention launch, and the sections of its workspace, in bytes from its start.
 namespace {
+constexpr size_t CHUNK_SHORT_ITEMS = 1 << 15;  // (sequence, KV head) pairs of a launch up to which short sequences go their own way: 0.5 GB of partials at head_dim 128
 struct ChunkPlan {
   int pairs;
-  size_t part_acc, part_ml, cut_info, total;
+  int short_tokens;  // sequences of up to so many tokens can be the tree attention kernel's (0: none can)
+  size_t part_acc, part_ml, cut_info, short_acc, short_ml, short_info, total;
 };
 int chunk_plan(const iq_shape* s, ChunkPlan& w) {
   const int rc = check_shape(s);
@@ -1210,6 +1219,13 @@ int chunk_plan(const iq_shape* s, ChunkPlan& w) {
   w.part_acc = o; o += rows * s->head_dim * 4;
   w.part_ml = o; o += rows * 8;
   w.cut_info = o; o += (size_t)w.pairs * iq::CHUNK_INFO * 8;
+  const int group = s->n_q_heads / s->n_kv_heads;
+  const size_t items = (size_t)s->batch * s->n_kv_heads;
+  w.short_tokens = items <= CHUNK_SHORT_ITEMS ? iq::CHUNK_SHORT / group : 0;
+  const size_t parts = w.short_tokens ? (items + sm_count() * iq::tree_ctas_per_sm(s->head_dim, iq::CHUNK_SHORT)) * iq::CHUNK_SHORT : 0;
+  w.short_acc = o; o += parts * s->head_dim * 4;
+  w.short_ml = o; o += parts * 8;
+  w.short_info = o; o += w.short_tokens ? (items + 1) / 2 * 16 : 0;
   w.total = o;
   return IQ_OK;
 }
@@ -1301,6 +1317,38 @@ static int chunk_attention(const iq_shape* shape, const float* rot_dev, const iq
   p.lse = lse_out;
   p.status = status_dev;
   p.wait_polls = wait_polls;
+  // Sequences of a few tokens are the tree attention kernel's, in a launch of their own where the batch can have both kinds.
+  const bool all_short = n_tokens_max <= w.short_tokens;
+  const int short_tokens = all_short ? n_tokens_max : shape->batch > 1 && w.short_tokens ? iq::CHUNK_SHORT_MIXED / group : 0;
+  if (short_tokens) {
+    iq::TreeParams r = tree_params(shape, rot_dev, codebook, cache, window, sinks);
+    r.q = p.q;
+    r.qs_b = p.qs_b;
+    r.qs_t = p.qs_t;
+    r.qs_h = p.qs_h;
+    r.ctx_lens = ctx_lens_dev;
+    r.n_tokens = n_tokens_dev;
+    r.token_start = token_start_dev;
+    r.places = n_tokens_max;
+    r.n_tokens_max = short_tokens;
+    r.mask_words = 1;
+    r.leave_longer = 1;
+    r.cross = !causal;
+    r.tile = iq::tree_tile(short_tokens * group);
+    r.tiles = 1;
+    r.ctas = sm_count() * iq::tree_ctas_per_sm(shape->head_dim, r.tile);  // (as many for all tiles up to CHUNK_SHORT)
+    r.part_acc = reinterpret_cast<float*>(ws + w.short_acc);
+    r.part_ml = reinterpret_cast<float*>(ws + w.short_ml);
+    r.item_info = reinterpret_cast<int2*>(ws + w.short_info);
+    r.out = out;
+    r.out_is_fp16 = 1;
+    r.lse = lse_out;
+    r.status = status_dev;
+    r.wait_polls = wait_polls;
+    if (iq::launch_tree_attention(r, shape->head_dim, static_cast<cudaStream_t>(stream)) != cudaSuccess) return IQ_ERR_CUDA;
+    if (all_short) return IQ_OK;
+    p.least_tokens = short_tokens + 1;
+  }
   return iq::launch_chunk_attention(p, shape->head_dim, static_cast<cudaStream_t>(stream)) == cudaSuccess ? IQ_OK : IQ_ERR_CUDA;
 }
 

@@ -22,6 +22,7 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams& p, int b) {
     s.n = p.n_tokens ? max(0, min(p.n_tokens[b], p.n_tokens_max)) : p.n_tokens_max;
     s.tok0 = (long long)b * p.n_tokens_max;
   }
+  if (s.n < p.least_tokens) s.n = 0;
   s.tiles = (int)(((long long)s.n * p.group + CHUNK_ROWS - 1) / CHUNK_ROWS);
   return s;
 }

@@ -201,6 +201,11 @@ struct TreeParams {
   const uint32_t* mask;      // [batch][n_tokens_max][mask_words], or nullptr: a chain
   const int32_t* n_tokens;   // [batch], or nullptr
   int n_tokens_max, mask_words, window, sinks;
+  // For the short sequences of a step of any lengths: packed tokens (token_start [batch + 1] among `places`, or nullptr: `places` per sequence);
+  // sequences of more than n_tokens_max tokens are left out; with `cross` no token has a row of its own. iq_tree_attention: nullptr,
+  // n_tokens_max, 0, 0.
+  const int32_t* token_start;
+  int places, leave_longer, cross;
   int batch, n_q_heads, n_kv_heads, group, t_cap;
   PageMap pm;
   int scale_f16;
@@ -244,6 +249,7 @@ struct ChunkParams {
   const int32_t* token_start;  // [batch + 1]: packed tokens, n_tokens_max of them in all; or nullptr: n_tokens_max places per sequence
   const int32_t* n_tokens;     // [batch], or nullptr
   int n_tokens_max, causal, window, sinks;
+  int least_tokens;            // sequences of fewer tokens are left to the tree attention kernel
   int batch, n_q_heads, n_kv_heads, group, t_cap;
   PageMap pm;
   int scale_f16;
@@ -268,6 +274,9 @@ struct ChunkParams {
 constexpr int CHUNK_INFO = 4;
 // What an item costs beside its blocks (queries, outputs or a partial), and the least that a pair of CTAs is given, in blocks.
 constexpr int CHUNK_SEG_COST = 3, CHUNK_LEAST = 2;
+// (token, head) pairs of a KV head up to which a sequence of a step is the tree attention kernel's, whose tiles are that small: where the call
+// says that no sequence has more; and where it may (the launch's tile is then the limit's, and most such sequences have one token).
+constexpr int CHUNK_SHORT = 32, CHUNK_SHORT_MIXED = 16;
 cudaError_t launch_chunk_attention(const ChunkParams& p, int head_dim, cudaStream_t stream);
 
 // ---- a step's tokens: places, positions, cache rows

@@ -19,7 +19,8 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(const __gr
   const int t = (int)(bt % p.n_tokens_max);
   const int b = (int)(bt / p.n_tokens_max);
   if (b >= p.batch) return;
-  if (p.n_tokens && t >= p.n_tokens[b]) return;
+  long long tok0;
+  if (t >= tree_tokens(p, b, tok0)) return;
   const int g = h / p.group, n = t * p.group + h % p.group, tile = n / p.tile;
   const size_t item = ((size_t)b * p.n_kv_heads + g) * p.tiles + tile;
   QuatPairs<E> qp;
@@ -78,7 +79,7 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) tree_merge_kernel(const __gr
   for (int e = 0; e < E; e++) v[e] *= inv;
   qp.template apply<true>(v);
   wht_warp<float, E>(v, lane);
-  const size_t o = ((size_t)b * p.n_tokens_max + t) * p.n_q_heads + h;
+  const size_t o = ((size_t)tok0 + t) * p.n_q_heads + h;
 #pragma unroll
   for (int e = 0; e < E; e++) v[e] *= rsqrtf((float)D);
   if (p.out_is_fp16) {

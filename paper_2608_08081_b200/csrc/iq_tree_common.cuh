@@ -10,12 +10,14 @@ struct TreeSeq {
   int ctx, tokens, rows;   // context rows, drafted tokens, rows of the two inside the cache
   int blocks, sink_blocks, skipped;
   int tiles;               // items per KV head
+  long long tok0;          // its first token among those of q (packed) and out
   long long weight;        // blocks of all its items, each item counting TREE_SEG_COST more
   __device__ __forceinline__ int block(int v) const { return v < sink_blocks ? v : v + skipped; }
 };
 __device__ __forceinline__ uint32_t tree_mask_word(const TreeParams& p, int b, int t, int w, int tokens) {
   const int left = tokens - 32 * w;  // bits of tokens that the sequence has
   const uint32_t have = left >= 32 ? 0xFFFFFFFFu : left <= 0 ? 0u : (1u << left) - 1u;
+  if (p.cross) return 0u;
   if (p.mask) return p.mask[((size_t)b * p.n_tokens_max + t) * p.mask_words + w] & have;
   const int k = t + 1 - 32 * w;  // the chain: tokens 0 .. t
   return have & (k >= 32 ? 0xFFFFFFFFu : k <= 0 ? 0u : (1u << k) - 1u);
@@ -28,12 +30,25 @@ __device__ __forceinline__ int tree_seen(const TreeParams& p, int b, int t, int 
 __device__ __forceinline__ int tree_position(const TreeParams& p, int b, int t, const TreeSeq& s) {
   return s.ctx + tree_seen(p, b, t, s.tokens) - 1;
 }
+// Tokens of a sequence, and the first of them among those of q (packed) and out.
+__device__ __forceinline__ int tree_tokens(const TreeParams& p, int b, long long& tok0) {
+  int n;
+  if (p.token_start) {
+    const int first = max(0, min(p.token_start[b], p.places));
+    n = max(0, min(p.token_start[b + 1], p.places) - first);
+    tok0 = first;
+  } else {
+    n = p.n_tokens ? max(0, min(p.n_tokens[b], p.places)) : p.places;
+    tok0 = (long long)b * p.places;
+  }
+  return n <= p.n_tokens_max ? n : p.leave_longer ? 0 : p.n_tokens_max;
+}
 template <int TILE>
 __device__ __forceinline__ TreeSeq tree_seq(const TreeParams& p, int b) {
   TreeSeq s;
   s.ctx = max(0, min(p.ctx_lens[b], p.t_cap));
-  s.tokens = p.n_tokens ? max(0, min(p.n_tokens[b], p.n_tokens_max)) : p.n_tokens_max;
-  s.rows = min(s.ctx + s.tokens, p.t_cap);  // (t_cap + IQ_TREE_MAX_TOKENS fits 31 bits: the host's limit)
+  s.tokens = tree_tokens(p, b, s.tok0);
+  s.rows = p.cross ? s.ctx : min(s.ctx + s.tokens, p.t_cap);  // (t_cap + IQ_TREE_MAX_TOKENS fits 31 bits: the host's limit)
   const int total = (s.rows + 127) >> 7;
   s.sink_blocks = total;
   s.skipped = 0;

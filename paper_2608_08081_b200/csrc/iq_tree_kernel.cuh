@@ -203,7 +203,7 @@ __device__ __forceinline__ int tree_queries(const TreeParams& p, TreeShared<N>& 
   constexpr int E = D / 32;
   auto load = [&](int n, uint32_t (&raw)[E / 2]) {
     const int t = (q0 + n) / p.group, h = c.g * p.group + (q0 + n) - t * p.group;
-    const __half* q = p.q + c.b * p.qs_b + t * p.qs_t + h * p.qs_h + lane * E;
+    const __half* q = p.q + (p.token_start ? c.sq.tok0 * p.qs_t : c.b * p.qs_b) + t * p.qs_t + h * p.qs_h + lane * E;
     if constexpr (E == 4) {
       const uint2 x = *reinterpret_cast<const uint2*>(q);
       raw[0] = x.x; raw[1] = x.y;
