@@ -21,7 +21,6 @@ namespace iq {
 
 constexpr float CHUNK_LIMIT = 15.f;                // log2 of the largest p ...
 constexpr float CHUNK_START = 5.f;                 // ... and of the block's largest behind a raise
-constexpr float CHUNK_UNSET = 1e30f;               // minus the reference of a pair that has seen no row: whatever comes is too large for it
 constexpr float CHUNK_LEAST_SCALE = 8.67361738e-19f;  // 2^-60: V scales below it count as this
 
 // Layouts of the loads: 16x256b leaves rows lane / 4 and lane / 4 + 8 of 16 and columns 2 (lane % 4), + 1 of every 8 with a thread (so that it needs the
@@ -54,6 +53,11 @@ __device__ __forceinline__ void chunk_st_pairs(uint32_t taddr, const uint32_t (&
 __device__ __forceinline__ void chunk_ld8(uint32_t taddr, uint32_t (&r)[8]) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void chunk_ld32(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
                : "r"(taddr) : "memory");
 }
 // Values that a tcgen05.ld has left in registers are not used before the wait for it.
@@ -129,11 +133,15 @@ struct ChunkShared {
   uint64_t q_ready, raw_full, raw_empty, drain;
   uint32_t tmem, failed;
   ChunkRange range;
-  ChunkPiece coming, piece[4];            // the one whose queries are there (no blocks: there are no more); those at work
-  alignas(16) float4 m[2][D];             // SO(4) matrices of the KV head of even and odd pieces
-  alignas(16) float column[L::COLUMNS][3][L::NB];  // of a step's rows: scale of S, log2 of the V scale, 1 / V scale
+  ChunkPiece piece[4];                    // pieces 0, 4, ..., 1, 5, ...: with their queries (no blocks: there are no more)
+  uint32_t go[4];                         // whether there is such a piece: one thread's finding, so that all find the same
+  alignas(16) float4 m[3][D];             // SO(4) matrices of the KV head of pieces 0, 3, ...
+  // Factors of a step's rows: of two at a time the scales of S, then the log2 of the V scales; of each 1 / V scale.
+  alignas(16) float4 column[L::COLUMNS][L::NB / 2];
+  float weight[L::COLUMNS][L::NB];
   float row_sum[128], row_ref[128];       // at the end of a piece
-  float warp_q[L::SOFTMAX_WARPS];
+  float warp_q[4][3];                     // the largest elements of a piece's queries
+  const __half* query[128];               // where the queries of the tile's rows lie (nullptr: a row without a token)
 };
 template <int D>
 constexpr int CHUNK_SMEM = ChunkLayout<D>::OFF_S + (int)sizeof(ChunkShared<D>) + 1024;
@@ -293,7 +301,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
     uint32_t pieces = 0;
     if (warp >= L::QUERY_WARP) {
       // ================================================================ the queries of the next piece, as they are
-      const int t = tid - 32 * L::QUERY_WARP;
+      const int t = tid - 32 * L::QUERY_WARP, query_bar = 6;
       constexpr int CHUNKS = D / 8;  // of 16 bytes, of a row
       for (bool more = true; more;) {
         more = walk.next(p, c);
@@ -310,21 +318,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         if (pieces > 0) chunk_wait(&s.raw_empty, (pieces - 1) & 1, p.wait_polls, &s.failed);
         if (__any_sync(FULL, *(volatile uint32_t*)&s.failed != 0)) break;  // (what is there may still be read)
         if (!more) c.hi = c.lo = 0;
-        if (t == 0) s.coming = c;
+        if (t == 0) s.piece[pieces & 3] = c;
         if (more) {
           const __half* const q = p.q + (p.token_start ? c.sq.tok0 * p.qs_t : c.b * p.qs_b);
+          for (int r = t; r < 128; r += 96) {
+            const int at = c.t * CHUNK_ROWS + rank * 128 + r, tok = at / p.group, head = c.g * p.group + at - tok * p.group;
+            s.query[r] = tok < c.sq.n ? q + tok * p.qs_t + head * p.qs_h : nullptr;
+          }
+          cta_bar_sync_n(query_bar, 96);
+#pragma unroll 4
           for (int i = t; i < 128 * CHUNKS; i += 96) {
             const int r = i / CHUNKS, k = i % CHUNKS;
-            const int at = c.t * CHUNK_ROWS + rank * 128 + r, tok = at / p.group, head = c.g * p.group + at - tok * p.group;
-            const bool valid = tok < c.sq.n;
-            const __half* const src = valid ? q + tok * p.qs_t + head * p.qs_h + 8 * k : p.q;
+            const __half* const row = s.query[r];
             const uint32_t dst = smem_u32(smem + L::OFF_RAW + r * (2 * D) + ((k ^ (r & 7)) << 4));
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(row ? row + 8 * k : p.q), "r"(row ? 16 : 0) : "memory");
+          }
+          if (t < D / 4) {
+            float M[4][4];
+            so4_matrix<float>(p.rot + ((size_t)c.g * (D / 4) + t) * 8, M);
+            float4* const m = s.m[pieces % 3] + 4 * t;
+#pragma unroll
+            for (int i = 0; i < 4; i++) m[i] = make_float4(M[i][0], M[i][1], M[i][2], M[i][3]);
           }
           asm volatile("cp.async.wait_all;" ::: "memory");
+          __half2 top = __float2half2_rn(0.f);  // of the elements that this thread brought
+#pragma unroll 4
+          for (int i = t; i < 128 * CHUNKS; i += 96) {
+            const int r = i / CHUNKS, k = i % CHUNKS;
+            const uint4 x = *reinterpret_cast<const uint4*>(smem + L::OFF_RAW + r * (2 * D) + ((k ^ (r & 7)) << 4));
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int k2 = 0; k2 < 4; k2++) top = __hmax2(top, __habs2(*reinterpret_cast<const __half2*>(&w[k2])));
+          }
+          const float most = warp_max(fminf(fmaxf(__low2float(top), __high2float(top)), 65504.f));  // (an infinite query is its own affair)
+          if (lane == 0) s.warp_q[pieces & 3][warp - L::QUERY_WARP] = most;
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.raw_full);
+        cta_bar_sync_n(query_bar, 96);  // (the rows' places have been read)
         pieces++;
       }
       if (t == 0 && rank == 0) {  // the item that a later pair ends, for the merge
@@ -449,11 +480,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       const uint32_t st = n % ST;
       if (n >= ST) chunk_wait(&s.k_empty[st], ((n / ST) - 1) & 1, p.wait_polls, &s.failed);
       if (t < NB) {
-        float* const col = &s.column[n % L::COLUMNS][0][t];
+        float* const col = reinterpret_cast<float*>(&s.column[n % L::COLUMNS][t >> 1]) + (t & 1);
         vs = vs < CHUNK_LEAST_SCALE ? CHUNK_LEAST_SCALE : vs;
         col[0] = ks * p.score_unit;
-        col[NB] = log2f(vs);
-        col[2 * NB] = vs < INFINITY ? 1.f / vs : 1.f;  // (finite: tokens that do not see the row multiply it by 0)
+        col[2] = log2f(vs);
+        s.weight[n % L::COLUMNS][t] = vs < INFINITY ? 1.f / vs : 1.f;  // (finite: tokens that do not see the row multiply it by 0)
       }
       chunk_levels<BITS>(raw, p.lut_lo, p.lut_hi, p.lookup, slab + st * L::OPERAND, r);
       have = steps.next<SUB>(p, lane, status);
@@ -481,83 +512,65 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
     // The rotated queries of piece `count`, q~ = M H q, a thread half of a row's coordinates. False: there is no such piece.
     float q_unit = 0.f;  // what a unit of a score is
     auto queries = [&](uint32_t count) {
-      float4* const m = s.m[count & 1];
-      const ChunkPiece& c = s.piece[count & 3];
+      const float4* const m = s.m[count % 3];
       const uint8_t* const raw_row = smem + L::OFF_RAW + row * (2 * D);
       auto q = [&](int k) { return *reinterpret_cast<const uint4*>(raw_row + ((k ^ (row & 7)) << 4)); };  // 16 bytes of the thread's row
       chunk_wait(&s.raw_full, count & 1, p.wait_polls, &s.failed);
-      // One thread looks, so that all find the same. (Behind the first barrier everybody is done with the piece before the last, whose place and
-      // matrices are taken.)
-      if (tid == 0) {
-        ChunkPiece x = s.coming;
-        if (*(volatile uint32_t*)&s.failed) x.hi = x.lo = 0;
-        s.piece[count & 3] = x;
-      }
+      if (tid == 0) s.go[count & 3] = *(volatile uint32_t*)&s.failed ? 0u : s.piece[count & 3].hi > s.piece[count & 3].lo;
       cta_bar_sync_n(all_bar, 32 * L::SOFTMAX_WARPS);
-      if (c.hi == c.lo) return false;
-      float qmax;
-      {
-        if (tid < D / 4) {
-          float M[4][4];
-          so4_matrix<float>(p.rot + ((size_t)c.g * (D / 4) + tid) * 8, M);
-#pragma unroll
-          for (int i = 0; i < 4; i++) m[4 * tid + i] = make_float4(M[i][0], M[i][1], M[i][2], M[i][3]);
-        }
-        __half2 top = __float2half2_rn(0.f);
-#pragma unroll 8
-        for (int i = 0; i < D / 16; i++) {
-          const uint4 x = q(half * (D / 16) + i);
-          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-          for (int k = 0; k < 4; k++) top = __hmax2(top, __habs2(*reinterpret_cast<const __half2*>(&w[k])));
-        }
-        qmax = fminf(fmaxf(__low2float(top), __high2float(top)), 65504.f);  // (an infinite query is its own affair)
-      }
-      qmax = warp_max(qmax);
-      if (lane == 0) s.warp_q[warp] = qmax;
-      cta_bar_sync_n(all_bar, 32 * L::SOFTMAX_WARPS);
-#pragma unroll
-      for (int k = 0; k < L::SOFTMAX_WARPS; k++) qmax = fmaxf(qmax, s.warp_q[k]);
+      if (!s.go[count & 3]) return false;
+      const float qmax = fmaxf(fmaxf(s.warp_q[count & 3][0], s.warp_q[count & 3][1]), s.warp_q[count & 3][2]);
       const int e2 = qmax > 0.f ? 13 - ((int)(__float_as_uint(qmax) >> 23) - 126 + 4) : 0;  // |q~| <= sqrt(D) max |q|: at most 2^13
       const float q_scale = rsqrtf((float)D) * __uint_as_float((uint32_t)(127 + e2) << 23);
 #pragma unroll 1
-      for (int set = set0; set < set1; set++) {
-        float v[32];
+      for (int set = set0; set < set1; set += 2) {  // two runs at a time: sums over the even runs of the row plus and minus those over the odd ones
+        float v[2][32];
 #pragma unroll
-        for (int i = 0; i < 32; i++) v[i] = 0.f;
+        for (int i = 0; i < 32; i++) v[0][i] = v[1][i] = 0.f;
 #pragma unroll 2
-        for (int r = 0; r < SETS; r++) {
-          const float sg = chunk_sign(set, r);
+        for (int r = 0; r < SETS; r += 2) {
+          const float sg = chunk_sign(set >> 1, r >> 1);
 #pragma unroll
-          for (int i = 0; i < 4; i++) {
-            const uint4 x = q(4 * r + i);
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+          for (int y = 0; y < 2; y++)
 #pragma unroll
-            for (int k = 0; k < 4; k++) {
-              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
-              v[8 * i + 2 * k] = fmaf(sg, f.x, v[8 * i + 2 * k]);
-              v[8 * i + 2 * k + 1] = fmaf(sg, f.y, v[8 * i + 2 * k + 1]);
+            for (int i = 0; i < 4; i++) {
+              const uint4 x = q(4 * (r + y) + i);
+              const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+              for (int k = 0; k < 4; k++) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+                v[y][8 * i + 2 * k] = fmaf(sg, f.x, v[y][8 * i + 2 * k]);
+                v[y][8 * i + 2 * k + 1] = fmaf(sg, f.y, v[y][8 * i + 2 * k + 1]);
+              }
             }
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i++) {
+          const float x = v[0][i], y = v[1][i];
+          v[0][i] = x + y;
+          v[1][i] = x - y;
+        }
+#pragma unroll
+        for (int y = 0; y < 2; y++) {
+          chunk_wht32(v[y]);
+          chunk_so4<false>(m + 32 * (set + y), v[y]);
+          uint32_t hi[16], lo[16];
+#pragma unroll
+          for (int k = 0; k < 16; k++) {
+            const float a0 = v[y][2 * k] * q_scale, a1 = v[y][2 * k + 1] * q_scale;
+            hi[k] = pack_half2(a0, a1);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[k]));
+            lo[k] = pack_half2(a0 - f.x, a1 - f.y);
           }
-        }
-        chunk_wht32(v);
-        chunk_so4<false>(m + 32 * set, v);
-        uint32_t hi[16], lo[16];
+          tc_st16(tmem + lanes + L::Q_COL + (set + y) * 16, hi);
+          if constexpr (D == 128) {
+            tc_st16(tmem + lanes + L::Q_COL + D / 2 + (set + y) * 16, lo);
+          } else {
+            uint8_t* const slab = smem + L::OFF_Q + (set >> 1) * 16384;
 #pragma unroll
-        for (int k = 0; k < 16; k++) {
-          const float a0 = v[2 * k] * q_scale, a1 = v[2 * k + 1] * q_scale;
-          hi[k] = pack_half2(a0, a1);
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[k]));
-          lo[k] = pack_half2(a0 - f.x, a1 - f.y);
-        }
-        tc_st16(tmem + lanes + L::Q_COL + set * 16, hi);
-        if constexpr (D == 128) {
-          tc_st16(tmem + lanes + L::Q_COL + D / 2 + set * 16, lo);
-        } else {
-          uint8_t* const slab = smem + L::OFF_Q + (set >> 1) * 16384;
-#pragma unroll
-          for (int k = 0; k < 4; k++)
-            *reinterpret_cast<uint4*>(chunk_swizzled(slab, row, 4 * (set & 1) + k)) = make_uint4(lo[4 * k], lo[4 * k + 1], lo[4 * k + 2], lo[4 * k + 3]);
+            for (int k = 0; k < 4; k++)
+              *reinterpret_cast<uint4*>(chunk_swizzled(slab, row, 4 * y + k)) = make_uint4(lo[4 * k], lo[4 * k + 1], lo[4 * k + 2], lo[4 * k + 3]);
+          }
         }
       }
       tc_wait_st();
@@ -577,11 +590,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
     while (more) {
       const ChunkPiece& c = s.piece[pieces & 3];
       const int steps = (c.hi - c.lo) * SUB;
-      float neg_ref[2], l[2];
+      float neg_ref[2], limit[2];  // minus the reference; what an exponent may be beside it (-inf: the pair has seen no row)
+      F32x2 l[2];
 #pragma unroll
       for (int k = 0; k < 2; k++) {
-        neg_ref[k] = CHUNK_UNSET;
-        l[k] = 0.f;
+        neg_ref[k] = 0.f;
+        limit[k] = -INFINITY;
+        l[k] = f32x2(0.f, 0.f);
       }
       uint32_t whole_steps = 0;  // of 32 steps, those that all of the CTA's rows see whole: a lane looks at one
       auto first_of = [&](int j) { return c.x.block(c.lo + j / SUB) * 128 + (SUB > 1 ? (j & 1) * NB : 0); };  // a step's first row
@@ -594,93 +609,73 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         }
         const bool whole = whole_steps >> (j & 31) & 1u;
         const uint32_t s_col = tmem + lanes16 + L::S_COL + (n & 1) * NB;
-        const float* const col = &s.column[n % L::COLUMNS][0][2 * (lane & 3)];
+        const float4* const col = &s.column[n % L::COLUMNS][lane & 3];
+        const float* const wt = &s.weight[n % L::COLUMNS][2 * (lane & 3)];
         chunk_wait(&s.s_full[n & 1], (n >> 1) & 1, p.wait_polls, &s.failed);
         tc_fence_after();
-        // ---- exponents; w[c][k][i]: row row2 + 8 k, columns NC c + 8 i + 2 (lane % 4) and the next
-        F32x2 w[PARTS][2][NI];
-        F32x2 sum[2];
-        float top;
-        auto weights = [&](int x) {  // of a part of the columns, over its scores; their sums; the largest one's exponent
-          uint32_t pk[2 * NI];
-          F32x2 rv[NI];
+        // ---- exponents; t[x][k][i]: row row2 + 8 k, columns NC x + 8 i + 2 (lane % 4) and the next
+        F32x2 t[PARTS][2][NI];
+        {
+          uint32_t raw[PARTS][4 * NI];
 #pragma unroll
-          for (int i = 0; i < NI; i++) {
-            const float2 a = *reinterpret_cast<const float2*>(col + 2 * NB + NC * x + 8 * i);
-            rv[i] = f32x2(a.x, a.y);
-          }
+          for (int x = 0; x < PARTS; x++) chunk_ld_rows(s_col + NC * x, raw[x]);
+          tc_wait_ld();
 #pragma unroll
-          for (int k = 0; k < 2; k++)
+          for (int x = 0; x < PARTS; x++) chunk_landed(raw[x]);
+#pragma unroll
+          for (int x = 0; x < PARTS; x++)
 #pragma unroll
             for (int i = 0; i < NI; i++) {
-              const F32x2 t = add2(w[x][k][i], f32x2(neg_ref[k], neg_ref[k]));
-              top = max3f(top, t.lo(), t.hi());
-              const float p0 = ex2f(t.lo()), p1 = ex2f(t.hi());
-              sum[k] = fma2(f32x2(p0, p1), rv[i], sum[k]);
-              pk[2 * i + k] = pack_half2(p0, p1);
+              const float4 a = col[(NC * x + 8 * i) / 2];
+              const F32x2 ks = mul2(f32x2(a.x, a.y), f32x2(q_unit, q_unit)), lv = f32x2(a.z, a.w);
+#pragma unroll
+              for (int k = 0; k < 2; k++)
+                t[x][k][i] = add2(fma2(f32x2(__uint_as_float(raw[x][4 * i + 2 * k]), __uint_as_float(raw[x][4 * i + 2 * k + 1])), ks, lv), f32x2(neg_ref[k], neg_ref[k]));
             }
-          chunk_st_pairs(s_col + NC * x, pk);
-        };
-        auto scores = [&](auto all, bool then) {
-          uint32_t raw[2][4 * NI];
-          chunk_ld_rows(s_col, raw[0]);
-          int last[2], from[2];  // rows are seen up to `last`, of those from `from` on and below the sinks
-          if constexpr (!decltype(all)::value) {
+        }
+        if (!whole) {  // rows are seen up to `last`, of those from `from` on and below the sinks
+          const int row0 = first_of(j) + 2 * (lane & 3);
 #pragma unroll
-            for (int k = 0; k < 2; k++) {
-              const int pos = c.sq.ctx + (c.t * CHUNK_ROWS + first_row + row2 + 8 * k) / p.group;
-              last[k] = p.causal ? min(pos, c.x.end - 1) : c.x.end - 1;
-              from[k] = p.window > 0 ? pos - p.window + 1 : 0;
-            }
-          }
+          for (int k = 0; k < 2; k++) {
+            const int pos = c.sq.ctx + (c.t * CHUNK_ROWS + first_row + row2 + 8 * k) / p.group;
+            const int last = p.causal ? min(pos, c.x.end - 1) : c.x.end - 1, from = p.window > 0 ? pos - p.window + 1 : 0;
 #pragma unroll
-          for (int x = 0; x < PARTS; x++) {
-            F32x2 ks[NI], lv[NI];
-#pragma unroll
-            for (int i = 0; i < NI; i++) {
-              const float2 a = *reinterpret_cast<const float2*>(col + NC * x + 8 * i), b = *reinterpret_cast<const float2*>(col + NB + NC * x + 8 * i);
-              ks[i] = mul2(f32x2(a.x, a.y), f32x2(q_unit, q_unit));
-              lv[i] = f32x2(b.x, b.y);
-            }
-            tc_wait_ld();
-            chunk_landed(raw[x & 1]);
-            if (x + 1 < PARTS) chunk_ld_rows(s_col + NC * (x + 1), raw[(x + 1) & 1]);
-#pragma unroll
-            for (int k = 0; k < 2; k++)
+            for (int x = 0; x < PARTS; x++)
 #pragma unroll
               for (int i = 0; i < NI; i++) {
-                w[x][k][i] = fma2(f32x2(__uint_as_float(raw[x & 1][4 * i + 2 * k]), __uint_as_float(raw[x & 1][4 * i + 2 * k + 1])), ks[i], lv[i]);
-                if constexpr (!decltype(all)::value) {
-                  const int r = first_of(j) + NC * x + 8 * i + 2 * (lane & 3);
-                  const bool a = r <= last[k] && (r >= from[k] || r < p.sinks), b = r + 1 <= last[k] && (r + 1 >= from[k] || r + 1 < p.sinks);
-                  w[x][k][i] = f32x2(a ? w[x][k][i].lo() : -INFINITY, b ? w[x][k][i].hi() : -INFINITY);
-                }
+                const int r = row0 + NC * x + 8 * i;
+                const bool a = r <= last && (r >= from || r < p.sinks), b = r + 1 <= last && (r + 1 >= from || r + 1 < p.sinks);
+                t[x][k][i] = f32x2(a ? t[x][k][i].lo() : -INFINITY, b ? t[x][k][i].hi() : -INFINITY);
               }
-            if (then) weights(x);
           }
-        };
-        // The references hold for almost all steps, so the weights come first and the question whether one is too large after them. (A piece's first
-        // step has none to begin with.)
-        top = -INFINITY;
-        sum[0] = sum[1] = f32x2(0.f, 0.f);
-        if (whole) scores(std::true_type(), j > 0); else scores(std::false_type(), j > 0);
-        if (__builtin_expect(j == 0 || __any_sync(FULL, top > CHUNK_LIMIT), 0)) {
+        }
+        float top[2];
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+          top[k] = -INFINITY;
+#pragma unroll
+          for (int x = 0; x < PARTS; x++)
+#pragma unroll
+            for (int i = 0; i < NI; i++) top[k] = max3f(top[k], t[x][k][i].lo(), t[x][k][i].hi());
+        }
+        if (__builtin_expect(__any_sync(FULL, top[0] > limit[0] || top[1] > limit[1]), 0)) {
           // ---- new references for the rows that need one
           float factor[2];
 #pragma unroll
           for (int k = 0; k < 2; k++) {
-            float most = -INFINITY;
-#pragma unroll
-            for (int x = 0; x < PARTS; x++)
-#pragma unroll
-              for (int i = 0; i < NI; i++) most = max3f(most, w[x][k][i].lo(), w[x][k][i].hi());
-            most = fmaxf(most, __shfl_xor_sync(FULL, most, 1));
+            float most = fmaxf(top[k], __shfl_xor_sync(FULL, top[k], 1));
             most = fmaxf(most, __shfl_xor_sync(FULL, most, 2));
             factor[k] = 1.f;
-            if (most + neg_ref[k] > CHUNK_LIMIT) {
-              factor[k] = ex2f((CHUNK_START - most) - neg_ref[k]);
-              neg_ref[k] = CHUNK_START - most;
-              l[k] *= factor[k];
+            if (most > limit[k]) {
+              const float less = CHUNK_START - most;
+              if (limit[k] > -INFINITY) factor[k] = ex2f(less);
+              neg_ref[k] += less;
+              limit[k] = CHUNK_LIMIT;
+              l[k] = mul2(l[k], f32x2(factor[k], factor[k]));
+#pragma unroll
+              for (int x = 0; x < PARTS; x++)
+#pragma unroll
+                for (int i = 0; i < NI; i++) t[x][k][i] = add2(t[x][k][i], f32x2(less, less));
             }
           }
           if (j > 0) {
@@ -697,27 +692,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
               chunk_st_rows(tmem + lanes16 + L::O_COL + x, o);
             }
           }
-          sum[0] = sum[1] = f32x2(0.f, 0.f);
+        }
+        // ---- weights, over the scores, and their sums
 #pragma unroll
-          for (int x = 0; x < PARTS; x++) weights(x);
+        for (int x = 0; x < PARTS; x++) {
+          uint32_t pk[2 * NI];
+#pragma unroll
+          for (int i = 0; i < NI; i++) {
+            const float2 a = *reinterpret_cast<const float2*>(wt + NC * x + 8 * i);
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+              const F32x2 e = f32x2(ex2f(t[x][k][i].lo()), ex2f(t[x][k][i].hi()));
+              l[k] = fma2(e, f32x2(a.x, a.y), l[k]);
+              pk[2 * i + k] = pack_half2(e.lo(), e.hi());
+            }
+          }
+          chunk_st_pairs(s_col + NC * x, pk);
         }
         tc_wait_st();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) chunk_arrive(p_full + 8 * (n & 1));
-#pragma unroll
-        for (int k = 0; k < 2; k++) l[k] += sum[k].lo() + sum[k].hi();
       }
 
       // ---- sums and references of the rows
 #pragma unroll
       for (int k = 0; k < 2; k++) {
-        float all = l[k];
+        float all = l[k].lo() + l[k].hi();
         all += __shfl_xor_sync(FULL, all, 1);
         all += __shfl_xor_sync(FULL, all, 2);
         if ((lane & 3) == 0) {
           s.row_sum[row2 + 8 * k] = all;
-          s.row_ref[row2 + 8 * k] = neg_ref[k] == CHUNK_UNSET ? -INFINITY : -neg_ref[k];
+          s.row_ref[row2 + 8 * k] = limit[k] > -INFINITY ? -neg_ref[k] : -INFINITY;
         }
       }
       // ---- the next piece's queries come first: its first products run under this one's outputs
@@ -747,52 +753,77 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         if (half == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * ((size_t)c.slot * CHUNK_ROWS + first_row + row)) = make_float2(ref, sum);
       } else {
         // ---- o = H M^T o~ / l: runs of 32 coordinates in place, then across the runs
-        const float4* const m = s.m[pieces & 1];
+        const float4* const m = s.m[pieces % 3];
         const float unit = sum == 0.f ? 0.f : p.value_unit * rsqrtf((float)D) / sum;
 #pragma unroll 1
-        for (int set = set0; set < set1; set++) {
-          uint32_t r[32];
-          float v[32];
-          tc_ld32(o_col + 32 * set, r);
-          chunk_landed(r);
+        for (int set = set0; set < set1; set += 2) {
+          float v[2][32];
+          {
+            uint32_t r[2][32];
+            chunk_ld32(o_col + 32 * set, r[0]);
+            chunk_ld32(o_col + 32 * set + 32, r[1]);
+            tc_wait_ld();
+            chunk_landed(r[0]);
+            chunk_landed(r[1]);
 #pragma unroll
-          for (int k = 0; k < 32; k++) v[k] = __uint_as_float(r[k]) * unit;
-          chunk_so4<true>(m + 32 * set, v);
-          chunk_wht32(v);
+            for (int k = 0; k < 32; k++) {
+              v[0][k] = __uint_as_float(r[0][k]) * unit;
+              v[1][k] = __uint_as_float(r[1][k]) * unit;
+            }
+          }
 #pragma unroll
-          for (int i = 0; i < 2; i++) {
-            uint32_t y[16];
+          for (int y = 0; y < 2; y++) {
+            chunk_so4<true>(m + 32 * (set + y), v[y]);
+            chunk_wht32(v[y]);
 #pragma unroll
-            for (int k = 0; k < 16; k++) y[k] = __float_as_uint(v[16 * i + k]);
-            tc_st16(o_col + 32 * set + 16 * i, y);
+            for (int i = 0; i < 2; i++) {
+              uint32_t z[16];
+#pragma unroll
+              for (int k = 0; k < 16; k++) z[k] = __float_as_uint(v[y][16 * i + k]);
+              tc_st16(o_col + 32 * (set + y) + 16 * i, z);
+            }
           }
         }
         tc_wait_st();
         tc_fence_before();
         cta_bar_sync_n(pair_bar, 64);
         tc_fence_after();
+        constexpr int XC = D == 128 ? 16 : 8;  // columns of a run at a time
 #pragma unroll 1
-        for (int x = 0; x < 32; x += 8) {
-          uint32_t u[SETS][8];
+        for (int x = 0; x < 32; x += XC) {
+          uint32_t u[SETS][XC];
 #pragma unroll
-          for (int r = 0; r < SETS; r++) chunk_ld8(o_col + 32 * r + x, u[r]);
+          for (int r = 0; r < SETS; r++) {
+            if constexpr (XC == 16) tc_ld16_issue(o_col + 32 * r + x, u[r]);
+            else chunk_ld8(o_col + 32 * r + x, u[r]);
+          }
           tc_wait_ld();
 #pragma unroll
           for (int r = 0; r < SETS; r++) chunk_landed(u[r]);
 #pragma unroll 1
-          for (int set = set0; set < set1; set++) {
-            float o[8];
+          for (int set = set0; set < set1; set += 2) {
+            float o[2][XC];
 #pragma unroll
-            for (int i = 0; i < 8; i++) o[i] = __uint_as_float(u[0][i]);
+            for (int i = 0; i < XC; i++) { o[0][i] = __uint_as_float(u[0][i]); o[1][i] = __uint_as_float(u[1][i]); }
 #pragma unroll
-            for (int r = 1; r < SETS; r++) {
-              const float sg = chunk_sign(set, r);
+            for (int r = 2; r < SETS; r += 2) {
+              const float sg = chunk_sign(set >> 1, r >> 1);
 #pragma unroll
-              for (int i = 0; i < 8; i++) o[i] = fmaf(sg, __uint_as_float(u[r][i]), o[i]);
+              for (int i = 0; i < XC; i++) {
+                o[0][i] = fmaf(sg, __uint_as_float(u[r][i]), o[0][i]);
+                o[1][i] = fmaf(sg, __uint_as_float(u[r + 1][i]), o[1][i]);
+              }
             }
-            if (valid)
-              *reinterpret_cast<uint4*>(p.out + out_row * D + 32 * set + x) =
-                  make_uint4(pack_half2(o[0], o[1]), pack_half2(o[2], o[3]), pack_half2(o[4], o[5]), pack_half2(o[6], o[7]));
+            if (valid) {
+              uint4* const dst = reinterpret_cast<uint4*>(p.out + out_row * D + 32 * set + x);
+#pragma unroll
+              for (int i = 0; i < XC; i += 8) {
+                auto both = [&](int k) { return pack_half2(o[0][k] + o[1][k], o[0][k + 1] + o[1][k + 1]); };
+                auto less = [&](int k) { return pack_half2(o[0][k] - o[1][k], o[0][k + 1] - o[1][k + 1]); };
+                dst[i / 8] = make_uint4(both(i), both(i + 2), both(i + 4), both(i + 6));
+                dst[i / 8 + 4] = make_uint4(less(i), less(i + 2), less(i + 4), less(i + 6));
+              }
+            }
           }
         }
         if (valid && p.lse && half == 0) p.lse[out_row] = sum == 0.f ? -INFINITY : fmaf(ref, 0.6931471805599453f, logf(sum));
