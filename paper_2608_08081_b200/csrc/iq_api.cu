@@ -1207,7 +1207,7 @@ constexpr size_t CHUNK_SHORT_ITEMS = 1 << 15;  // (sequence, KV head) pairs of a
 struct ChunkPlan {
   int pairs;
   int short_tokens;  // sequences of up to so many tokens can be the tree attention kernel's (0: none can)
-  size_t part_acc, part_ml, cut_info, short_acc, short_ml, short_info, total;
+  size_t part_acc, part_ml, cuts, short_acc, short_ml, short_info, total;
 };
 int chunk_plan(const iq_shape* s, ChunkPlan& w) {
   const int rc = check_shape(s);
@@ -1218,7 +1218,7 @@ int chunk_plan(const iq_shape* s, ChunkPlan& w) {
   size_t o = 0;
   w.part_acc = o; o += rows * s->head_dim * 4;
   w.part_ml = o; o += rows * 8;
-  w.cut_info = o; o += (size_t)w.pairs * iq::CHUNK_INFO * 8;
+  w.cuts = o; o += (size_t)w.pairs * sizeof(iq::ChunkCut);
   const int group = s->n_q_heads / s->n_kv_heads;
   const size_t items = (size_t)s->batch * s->n_kv_heads;
   w.short_tokens = items <= CHUNK_SHORT_ITEMS ? iq::CHUNK_SHORT / group : 0;
@@ -1312,7 +1312,7 @@ static int chunk_attention(const iq_shape* shape, const float* rot_dev, const iq
   uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
   p.part_acc = reinterpret_cast<float*>(ws + w.part_acc);
   p.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
-  p.cut_info = reinterpret_cast<long long*>(ws + w.cut_info);
+  p.cuts = reinterpret_cast<iq::ChunkCut*>(ws + w.cuts);
   p.out = static_cast<__half*>(out);
   p.lse = lse_out;
   p.status = status_dev;

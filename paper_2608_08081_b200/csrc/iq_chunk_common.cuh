@@ -127,14 +127,13 @@ struct ChunkWalk {
   int b, g, t;
   long long unit, end, item_at;  // next unit, end of the range, where item (b, g, t) starts
   bool begun;                    // that item begins in this range
-  int info_b, info_g, info_t;    // the item that begins here and ends in a later range (-1: none) ...
-  long long info_at;             // ... and where it starts
+  ChunkCut cut;                  // (last: 0 where there is such a tile, until it is known)
+  long long cut_end;             // where that tile ends
   __device__ __forceinline__ void start(const ChunkParams& p, const ChunkRange& r) {
     unit = r.at;
     end = r.end;
-    info_b = -1;
-    info_g = info_t = 0;
-    info_at = 0;
+    cut.last = -1;
+    cut.partials = 0;
     b = g = t = 0;
     item_at = 0;
     begun = true;
@@ -167,7 +166,15 @@ struct ChunkWalk {
       c.hi = chunk_blocks_before(p, end - item_at, units, c.x.blocks);
       c.slot = c.lo == 0 && c.hi == c.x.blocks ? -1 : 2 * (int)(blockIdx.x >> 1) + (begun ? 1 : 0);
       const bool first = begun;
-      if (begun && item_at + units > end) { info_b = b; info_g = g; info_t = t; info_at = item_at; }
+      if (begun && item_at + units > end) {
+        cut.g = g;
+        cut.t = t;
+        cut.n = sq.n;
+        cut.tok0 = sq.tok0;
+        cut.last = 0;
+        cut_end = item_at + units;
+      }
+      if (c.slot >= 0 && c.hi > c.lo) cut.partials |= begun ? 2 : 1;
       unit = min(end, item_at + units);
       item_at += units;
       begun = true;

@@ -358,12 +358,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         cta_bar_sync_n(query_bar, 96);  // (the rows' places have been read)
         pieces++;
       }
-      if (t == 0 && rank == 0) {  // the item that a later pair ends, for the merge
-        long long* const info = p.cut_info + CHUNK_INFO * pair;
-        info[0] = walk.info_b;
-        info[1] = ((long long)walk.info_g << 32) | (uint32_t)walk.info_t;
-        info[2] = walk.info_at;
-        info[3] = s.range.total;
+      if (t == 0 && rank == 0) {  // (also where a wait gave up, whose pieces have not all been walked: the outputs are invalid, the places are not)
+        if (walk.cut.last == 0) walk.cut.last = (int)min((long long)s.range.pairs - 1, chunk_div(walk.cut_end * s.range.pairs - 1, s.range.total));
+        p.cuts[pair] = walk.cut;
       }
     } else if (rank == 0) {
       // ================================================================ products, of both CTAs

@@ -237,6 +237,13 @@ constexpr int tree_ctas_per_sm(int head_dim, int tile) { return head_dim == 128 
 int tree_tile(int queries);  // tile for that many (token, head) pairs of a KV head
 
 // ---- chunk and cross attention: any number of new tokens over the packed cache
+// What a pair of CTAs leaves for the merge.
+struct alignas(16) ChunkCut {
+  int g, t, n;       // the tile that begins in the pair's range and ends in a later one (last < 0: there is none): KV head, tile, tokens of its sequence,
+  int last;          // the pair in which it ends,
+  long long tok0;    // the sequence's first token among those of out
+  int partials;      // bit 0: the pair has a partial of the tile that its range begins in the middle of; bit 1: of the one above
+};
 struct ChunkParams {
   const uint8_t* k_codes;
   const float* k_scales;
@@ -265,15 +272,14 @@ struct ChunkParams {
   // Workspace. Of a pair's items at most the first and the last are cut: two partials each.
   float* part_acc;             // [2 pairs][256][head_dim], rotated space
   float* part_ml;              // [2 pairs][256][2]: reference (log2 units), sum
-  long long* cut_info;         // [pairs][4]: the item that begins in the pair's range and ends in a later one
+  ChunkCut* cuts;              // [pairs]
   __half* out;
   float* lse;
   uint32_t* status;
   uint32_t wait_polls;
 };
-constexpr int CHUNK_INFO = 4;
 // What an item costs beside its blocks (queries, outputs or a partial), and the least that a pair of CTAs is given, in blocks.
-constexpr int CHUNK_SEG_COST = 3, CHUNK_LEAST = 2;
+constexpr int CHUNK_SEG_COST = 6, CHUNK_LEAST = 2;
 // (token, head) pairs of a KV head up to which a sequence of a step is the tree attention kernel's, whose tiles are that small: where the call
 // says that no sequence has more; and where it may (the launch's tile is then the limit's, and most such sequences have one token).
 constexpr int CHUNK_SHORT = 32, CHUNK_SHORT_MIXED = 16;
