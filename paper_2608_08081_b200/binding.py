@@ -656,31 +656,48 @@ def iq_make_rotary(rotary_dim: int, interleaved: bool = False, base: float = 100
 
 def _token_rows(x, heads, head_dim):
     """(tokens, stride between tokens, stride between heads) of x fp16 [tokens][heads][d] or [B][T][heads][d] with evenly spaced tokens."""
-    assert x.dtype is torch.float16 and x.shape[-2] == heads and x.shape[-1] == head_dim and x.stride(-1) == 1
-    if x.dim() == 3:
-        return x.shape[0], x.stride(0), x.stride(1)
-    assert x.dim() == 4
-    assert x.shape[0] <= 1 or x.stride(0) == x.shape[1] * x.stride(1)  # the tokens of all sequences as one run
-    return x.shape[0] * x.shape[1], x.stride(1), x.stride(2)
+    size, st = x.shape, x.stride()
+    if len(size) == 3:
+        n, h, d = size
+        s_t, s_h, s_d = st
+    else:
+        B, T, h, d = size
+        s_b, s_t, s_h, s_d = st
+        assert B <= 1 or s_b == T * s_t  # the tokens of all sequences as one run
+        n = B * T
+    assert x.dtype is torch.float16 and h == heads and d == head_dim and s_d == 1
+    return n, s_t, s_h
 
 
 def iq_apply_rotary(shape: Shape, rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream=None) -> None:
     """Rotary positions of queries q [tokens][H_q][d] and keys k [tokens][H_kv][d] (fp16; also [B][T][...]; strided views, last dim contiguous;
     either may be None) into q_out, k_out, or in place where these are None. positions: int32, one per token."""
-    n, sides = None, []
-    for x, y, heads in ((q, q_out, shape.n_q_heads), (k, k_out, shape.n_kv_heads)):
-        if x is None:
-            assert y is None
-            sides += [None, 0, 0, None, 0, 0]
-            continue
-        y = x if y is None else y
-        nx, xt, xh = _token_rows(x, heads, shape.head_dim)
-        ny, yt, yh = _token_rows(y, heads, shape.head_dim)
-        assert nx == ny and n in (None, nx)
-        n = nx
-        sides += [x.data_ptr(), xt, xh, y.data_ptr(), yt, yh]
-    assert n is not None
-    _check(_lib.iq_apply_rotary(ctypes.byref(shape.c()), ctypes.byref(rotary.c()), *sides, _ints(positions, n), n, _stream(stream)), "iq_apply_rotary")
+    qp = kp = qop = kop = n = None
+    qt = qh = qot = qoh = kt = kh = kot = koh = 0
+    d = shape.head_dim
+    if q is not None:
+        n, qt, qh = n_out, qot, qoh = _token_rows(q, shape.n_q_heads, d)
+        qp = qop = q.data_ptr()
+        if q_out is not None:
+            n_out, qot, qoh = _token_rows(q_out, shape.n_q_heads, d)
+            qop = q_out.data_ptr()
+        assert n_out == n
+    else:
+        assert q_out is None
+    if k is not None:
+        m, kt, kh = n_out, kot, koh = _token_rows(k, shape.n_kv_heads, d)
+        kp = kop = k.data_ptr()
+        if k_out is not None:
+            n_out, kot, koh = _token_rows(k_out, shape.n_kv_heads, d)
+            kop = k_out.data_ptr()
+        assert n_out == m and (n is None or n == m)
+        n = m
+    else:
+        assert k_out is None and q is not None
+    rc = _lib.iq_apply_rotary(ctypes.byref(shape.c()), ctypes.byref(rotary.c()), qp, qt, qh, qop, qot, qoh, kp, kt, kh, kop, kot, koh, _ints(positions, n), n,
+                              _stream(stream))
+    if rc:
+        raise IQError(rc, "iq_apply_rotary")
 
 
 def iq_plan_tokens(shape: Shape, ctx_lens_dev, n_new_dev, token_start, positions=None, sequences=None, slots=None, block_table=None, page_rows: int = 0,

@@ -78,24 +78,37 @@ struct ChunkRange {
   long long at, end, total;  // units
   long long seq_at;          // where sequence b, in which the range starts, starts
   int b, pairs;              // pairs of CTAs that have a range
+  ChunkSeq sq;               // sequence b
 };
 // By one converged warp.
 __device__ __forceinline__ ChunkRange chunk_range(const ChunkParams& p, int pair, int lane) {
   ChunkRange r;
-  long long total = 0;
-  for (int b = lane; b < p.batch; b += 32) total += chunk_seq_units(p, chunk_seq(p, b));
+  ChunkSeq s = {};
+  long long total = 0, w = 0;
+  for (int b = lane; b < p.batch; b += 32) {
+    s = chunk_seq(p, b);
+    w = chunk_seq_units(p, s);
+    total += w;
+  }
 #pragma unroll 1
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(FULL, total, o);
   r.total = total;
-  r.pairs = (int)max(1ll, min((long long)p.pairs, total / p.least_units));
+  r.pairs = (int)max(1ll, min((long long)p.pairs, chunk_div(total, p.least_units)));
   r.at = r.end = total;
   r.b = 0;
   r.seq_at = 0;
   if (total == 0 || pair >= r.pairs) return r;
   r.at = chunk_cut(total, pair, r.pairs);
   r.end = chunk_cut(total, pair + 1, r.pairs);
+#pragma unroll 1
   for (int b0 = 0;; b0 += 32) {
-    const long long w = b0 + lane < p.batch ? chunk_seq_units(p, chunk_seq(p, b0 + lane)) : 0;
+    if (p.batch > 32) {  // (else they are the lanes' already)
+      w = 0;
+      if (b0 + lane < p.batch) {
+        s = chunk_seq(p, b0 + lane);
+        w = chunk_seq_units(p, s);
+      }
+    }
     long long x = w;
 #pragma unroll 1
     for (int o = 1; o < 32; o <<= 1) {
@@ -107,6 +120,10 @@ __device__ __forceinline__ ChunkRange chunk_range(const ChunkParams& p, int pair
       const int at = __ffs(behind) - 1;
       r.b = b0 + at;
       r.seq_at += __shfl_sync(FULL, x - w, at);
+      r.sq.ctx = __shfl_sync(FULL, s.ctx, at);
+      r.sq.n = __shfl_sync(FULL, s.n, at);
+      r.sq.tiles = __shfl_sync(FULL, s.tiles, at);
+      r.sq.tok0 = __shfl_sync(FULL, s.tok0, at);
       return r;
     }
     r.seq_at += __shfl_sync(FULL, x, 31);
@@ -139,7 +156,7 @@ struct ChunkWalk {
     begun = true;
     if (unit >= end) return;
     b = r.b;
-    sq = chunk_seq(p, b);
+    sq = r.sq;
     const long long head = chunk_units_before(p, sq, sq.tiles);
     long long rest = unit - r.seq_at;
     g = (int)chunk_div(rest, head);

@@ -519,6 +519,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       const float qmax = fmaxf(fmaxf(s.warp_q[count & 3][0], s.warp_q[count & 3][1]), s.warp_q[count & 3][2]);
       const int e2 = qmax > 0.f ? 13 - ((int)(__float_as_uint(qmax) >> 23) - 126 + 4) : 0;  // |q~| <= sqrt(D) max |q|: at most 2^13
       const float q_scale = rsqrtf((float)D) * __uint_as_float((uint32_t)(127 + e2) << 23);
+      q_unit = __uint_as_float((uint32_t)(127 - e2) << 23);
 #pragma unroll 1
       for (int set = set0; set < set1; set += 2) {  // two runs at a time: sums over the even runs of the row plus and minus those over the odd ones
         float v[2][32];
@@ -578,7 +579,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         chunk_arrive(q_ready);
         mbar_arrive(&s.raw_empty);
       }
-      q_unit = __uint_as_float((uint32_t)(127 - e2) << 23);
       return true;
     };
 
@@ -734,18 +734,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       tc_fence_after();
       const uint32_t o_col = tmem + lanes + L::O_COL;
       if (c.slot >= 0) {
-        // ---- a partial
-        float* const dst = p.part_acc + ((size_t)c.slot * CHUNK_ROWS + first_row + row) * D;
-#pragma unroll 1
-        for (int x = half * (D / 2); x < (half + 1) * (D / 2); x += 16) {
-          float o[16];
-          tc_ld16(o_col + x, o);
-          if (valid) {
+        // ---- a partial: eight rows of 32 bytes at a time (rows without a token included: nobody reads them)
+        float* const dst = p.part_acc + ((size_t)c.slot * CHUNK_ROWS + first_row + row2) * D + 2 * (lane & 3);
+#pragma unroll 2
+        for (int x = 0; x < D; x += 32) {
+          uint32_t o[16];
+          chunk_ld_rows(tmem + lanes16 + L::O_COL + x, o);
+          tc_wait_ld();
+          chunk_landed(o);
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-              *reinterpret_cast<float4*>(dst + x + 4 * i) =
-                  make_float4(o[4 * i] * p.value_unit, o[4 * i + 1] * p.value_unit, o[4 * i + 2] * p.value_unit, o[4 * i + 3] * p.value_unit);
-          }
+          for (int i = 0; i < 4; i++)
+#pragma unroll
+            for (int k = 0; k < 2; k++)
+              *reinterpret_cast<float2*>(dst + 8 * k * D + x + 8 * i) =
+                  make_float2(__uint_as_float(o[4 * i + 2 * k]) * p.value_unit, __uint_as_float(o[4 * i + 2 * k + 1]) * p.value_unit);
         }
         if (half == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * ((size_t)c.slot * CHUNK_ROWS + first_row + row)) = make_float2(ref, sum);
       } else {
