@@ -110,7 +110,7 @@ struct ChunkLayout {
   // Warps: softmax, K levels, V levels, products (one, in the first CTA of a pair), queries on their way. Registers of a thread: 96 at
   // launch, 480 over the five groups of warps (two of them softmax, two levels).
   static constexpr int SOFTMAX_WARPS = 8, K_WARP = 8, V_WARP = 12, MMA_WARP = 16, QUERY_WARP = 17, THREADS = 640;
-  static constexpr int SOFTMAX_REGS = 152, LEVEL_REGS = 64, MMA_REGS = 48;
+  static constexpr int SOFTMAX_REGS = 128, LEVEL_REGS = 72, MMA_REGS = 80;
   // tensor memory: Q (D = 128: both terms; 256: the first), two buffers of scores, O. The probabilities of NC columns go over their
   // scores, two to a column.
   static constexpr int Q_COL = 0, S_COL = 128, O_COL = 512 - D;
