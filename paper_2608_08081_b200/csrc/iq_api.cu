@@ -1203,7 +1203,6 @@ int iq_apply_rotary(const iq_shape* shape, const iq_rotary* rotary, const void* 
 
 // Pairs of CTAs of a chunk attention launch, and the sections of its workspace, in bytes from its start.
 namespace {
-constexpr size_t CHUNK_SHORT_ITEMS = 1 << 15;  // (sequence, KV head) pairs of a launch up to which short sequences go their own way: 0.5 GB of partials at head_dim 128
 struct ChunkPlan {
   int pairs;
   int short_tokens;  // sequences of up to so many tokens can be the tree attention kernel's (0: none can)
@@ -1221,8 +1220,10 @@ int chunk_plan(const iq_shape* s, ChunkPlan& w) {
   w.cuts = o; o += (size_t)w.pairs * sizeof(iq::ChunkCut);
   const int group = s->n_q_heads / s->n_kv_heads;
   const size_t items = (size_t)s->batch * s->n_kv_heads;
-  w.short_tokens = items <= CHUNK_SHORT_ITEMS ? iq::CHUNK_SHORT / group : 0;
-  const size_t parts = w.short_tokens ? (items + sm_count() * iq::tree_ctas_per_sm(s->head_dim, iq::CHUNK_SHORT)) * iq::CHUNK_SHORT : 0;
+  // (0.3 GB of partials at most at head_dim 128)
+  const int short_pairs = items <= 1 << 13 ? iq::CHUNK_SHORT : items <= 1 << 15 ? iq::CHUNK_SHORT_MIXED : 0;
+  w.short_tokens = short_pairs / group;
+  const size_t parts = w.short_tokens ? (items + sm_count() * iq::tree_ctas_per_sm(s->head_dim, short_pairs)) * short_pairs : 0;
   w.short_acc = o; o += parts * s->head_dim * 4;
   w.short_ml = o; o += parts * 8;
   w.short_info = o; o += w.short_tokens ? (items + 1) / 2 * 16 : 0;
@@ -1331,12 +1332,12 @@ static int chunk_attention(const iq_shape* shape, const float* rot_dev, const iq
     r.token_start = token_start_dev;
     r.places = n_tokens_max;
     r.n_tokens_max = short_tokens;
-    r.mask_words = 1;
+    r.mask_words = (short_tokens + 31) / 32;
     r.leave_longer = 1;
     r.cross = !causal;
     r.tile = iq::tree_tile(short_tokens * group);
     r.tiles = 1;
-    r.ctas = sm_count() * iq::tree_ctas_per_sm(shape->head_dim, r.tile);  // (as many for all tiles up to CHUNK_SHORT)
+    r.ctas = sm_count() * iq::tree_ctas_per_sm(shape->head_dim, r.tile);
     r.part_acc = reinterpret_cast<float*>(ws + w.short_acc);
     r.part_ml = reinterpret_cast<float*>(ws + w.short_ml);
     r.item_info = reinterpret_cast<int2*>(ws + w.short_info);

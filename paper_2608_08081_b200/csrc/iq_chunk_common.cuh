@@ -138,7 +138,7 @@ struct ChunkPiece {
   int lo, hi;
   int slot;  // of its partial; -1: it is the whole item
 };
-// The pieces of a range, one after the other; every warp walks for itself.
+// The pieces of a range, one after the other; every warp walks for itself, converged.
 struct ChunkWalk {
   ChunkSeq sq;
   int b, g, t;
@@ -199,7 +199,12 @@ struct ChunkWalk {
         t = 0;
         if (++g == p.n_kv_heads) {
           g = 0;
-          do sq = chunk_seq(p, ++b); while (sq.tiles == 0);  // (units are left, so there is such a sequence)
+          for (uint32_t some = 0; !some; b += some ? 0 : 32) {  // the next sequence with tiles (units are left, so there is one), 32 at a time
+            const int x = b + 1 + (threadIdx.x & 31);
+            some = __ballot_sync(FULL, x < p.batch && chunk_seq(p, x).tiles > 0);
+            if (some) b += __ffs(some);
+          }
+          sq = chunk_seq(p, b);
         }
       }
       if (c.hi > c.lo || (c.x.blocks == 0 && first)) return true;

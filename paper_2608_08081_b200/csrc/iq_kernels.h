@@ -282,7 +282,7 @@ struct ChunkParams {
 constexpr int CHUNK_SEG_COST = 6, CHUNK_LEAST = 2;
 // (token, head) pairs of a KV head up to which a sequence of a step is the tree attention kernel's, whose tiles are that small: where the call
 // says that no sequence has more; and where it may (the launch's tile is then the limit's, and most such sequences have one token).
-constexpr int CHUNK_SHORT = 32, CHUNK_SHORT_MIXED = 16;
+constexpr int CHUNK_SHORT = 64, CHUNK_SHORT_MIXED = 16;
 cudaError_t launch_chunk_attention(const ChunkParams& p, int head_dim, cudaStream_t stream);
 
 // ---- a step's tokens: places, positions, cache rows

@@ -23,6 +23,18 @@ def test_one_sequence(iq, d, ctx, tokens):
     Step(iq, 1, H=4, hk=1, d=d, ctx=ctx, tokens=tokens).run()
 
 
+@pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("H,hk", [(1, 1), (4, 1), (9, 3), (64, 8), (40, 1), (72, 1)])
+@pytest.mark.parametrize("cross", [False, True])
+def test_few_tokens(iq, d, H, hk, cross):
+    """Up to 64 (token, head) pairs of a KV head go another way than more do, in a batch up to 16."""
+    G = H // hk
+    for most in (16, 17, 32, 33, 64, 65):
+        n = max(1, most // G)
+        Step(iq, most, B=2, H=H, hk=hk, d=d, ctx=[150, 300], tokens=[n, max(0, n - 1)], cross=cross).run()
+        Step(iq, most, B=4, H=H, hk=hk, d=d, ctx=[150, 0, 300, 40], tokens=[n, 1, 70, 0], cross=cross, packed=True, window=0 if cross else 100, sinks=3).run()
+
+
 @pytest.mark.parametrize("H,hk", [(1, 1), (4, 1), (32, 4), (16, 8), (7, 1), (64, 8), (24, 2)])
 def test_head_layouts(iq, H, hk):
     Step(iq, 2, B=2, H=H, hk=hk, ctx=[260, 31], tokens=[45, 30]).run()
@@ -178,6 +190,15 @@ def test_many_tiles_and_cut_ones(iq, d, kw):
         again, _ = c.outputs()
         c.call(again)
         assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_large_batches(iq, packed):
+    """A few long sequences among many short and empty ones."""
+    tokens = [0] * 500
+    for b, n in ((3, 1), (40, 70), (41, 2), (200, 90), (201, 17), (499, 130)):
+        tokens[b] = n
+    Step(iq, 24, B=500, H=4, hk=2, ctx=[(37 * b) % 130 for b in range(500)], tokens=tokens, packed=packed).run()
 
 
 def test_nothing_to_do(iq):
