@@ -55,11 +55,6 @@ __device__ __forceinline__ void chunk_ld8(uint32_t taddr, uint32_t (&r)[8]) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ void chunk_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-               : "r"(taddr) : "memory");
-}
 // Values that a tcgen05.ld has left in registers are not used before the wait for it.
 template <int C>
 __device__ __forceinline__ void chunk_landed(uint32_t (&r)[C]) {
@@ -520,55 +515,45 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       const int e2 = qmax > 0.f ? 13 - ((int)(__float_as_uint(qmax) >> 23) - 126 + 4) : 0;  // |q~| <= sqrt(D) max |q|: at most 2^13
       const float q_scale = rsqrtf((float)D) * __uint_as_float((uint32_t)(127 + e2) << 23);
       q_unit = __uint_as_float((uint32_t)(127 - e2) << 23);
+      // (A run at a time, in loops: a piece's beginning and end are long code that runs once, and the instructions' way from memory is most of its time.)
 #pragma unroll 1
-      for (int set = set0; set < set1; set += 2) {  // two runs at a time: sums over the even runs of the row plus and minus those over the odd ones
-        float v[2][32];
+      for (int set = set0; set < set1; set++) {
+        float v[32];
 #pragma unroll
-        for (int i = 0; i < 32; i++) v[0][i] = v[1][i] = 0.f;
-#pragma unroll 2
-        for (int r = 0; r < SETS; r += 2) {
-          const float sg = chunk_sign(set >> 1, r >> 1);
+        for (int i = 0; i < 32; i++) v[i] = 0.f;
+#pragma unroll 1
+        for (int r = 0; r < SETS; r++) {
+          const float sg = chunk_sign(set, r);
 #pragma unroll
-          for (int y = 0; y < 2; y++)
+          for (int i = 0; i < 4; i++) {
+            const uint4 x = q(4 * r + i);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-              const uint4 x = q(4 * (r + y) + i);
-              const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-              for (int k = 0; k < 4; k++) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
-                v[y][8 * i + 2 * k] = fmaf(sg, f.x, v[y][8 * i + 2 * k]);
-                v[y][8 * i + 2 * k + 1] = fmaf(sg, f.y, v[y][8 * i + 2 * k + 1]);
-              }
+            for (int k = 0; k < 4; k++) {
+              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[k]));
+              v[8 * i + 2 * k] = fmaf(sg, f.x, v[8 * i + 2 * k]);
+              v[8 * i + 2 * k + 1] = fmaf(sg, f.y, v[8 * i + 2 * k + 1]);
             }
-        }
-#pragma unroll
-        for (int i = 0; i < 32; i++) {
-          const float x = v[0][i], y = v[1][i];
-          v[0][i] = x + y;
-          v[1][i] = x - y;
-        }
-#pragma unroll
-        for (int y = 0; y < 2; y++) {
-          chunk_wht32(v[y]);
-          chunk_so4<false>(m + 32 * (set + y), v[y]);
-          uint32_t hi[16], lo[16];
-#pragma unroll
-          for (int k = 0; k < 16; k++) {
-            const float a0 = v[y][2 * k] * q_scale, a1 = v[y][2 * k + 1] * q_scale;
-            hi[k] = pack_half2(a0, a1);
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[k]));
-            lo[k] = pack_half2(a0 - f.x, a1 - f.y);
           }
-          tc_st16(tmem + lanes + L::Q_COL + (set + y) * 16, hi);
-          if constexpr (D == 128) {
-            tc_st16(tmem + lanes + L::Q_COL + D / 2 + (set + y) * 16, lo);
-          } else {
-            uint8_t* const slab = smem + L::OFF_Q + (set >> 1) * 16384;
+        }
+        chunk_wht32(v);
+        chunk_so4<false>(m + 32 * set, v);
+        uint32_t hi[16], lo[16];
 #pragma unroll
-            for (int k = 0; k < 4; k++)
-              *reinterpret_cast<uint4*>(chunk_swizzled(slab, row, 4 * y + k)) = make_uint4(lo[4 * k], lo[4 * k + 1], lo[4 * k + 2], lo[4 * k + 3]);
-          }
+        for (int k = 0; k < 16; k++) {
+          const float a0 = v[2 * k] * q_scale, a1 = v[2 * k + 1] * q_scale;
+          hi[k] = pack_half2(a0, a1);
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&hi[k]));
+          lo[k] = pack_half2(a0 - f.x, a1 - f.y);
+        }
+        tc_st16(tmem + lanes + L::Q_COL + set * 16, hi);
+        if constexpr (D == 128) {
+          tc_st16(tmem + lanes + L::Q_COL + D / 2 + set * 16, lo);
+        } else {
+          uint8_t* const slab = smem + L::OFF_Q + (set >> 1) * 16384;
+#pragma unroll
+          for (int k = 0; k < 4; k++)
+            *reinterpret_cast<uint4*>(chunk_swizzled(slab, row, 4 * (set & 1) + k)) = make_uint4(lo[4 * k], lo[4 * k + 1], lo[4 * k + 2], lo[4 * k + 3]);
         }
       }
       tc_wait_st();
@@ -636,14 +621,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
           for (int k = 0; k < 2; k++) {
             const int pos = c.sq.ctx + (c.t * CHUNK_ROWS + first_row + row2 + 8 * k) / p.group;
             const int last = p.causal ? min(pos, c.x.end - 1) : c.x.end - 1, from = p.window > 0 ? pos - p.window + 1 : 0;
+            uint32_t seen = 0;  // bit 2 (NI x + i) + e: column NC x + 8 i + 2 (lane % 4) + e
+#pragma unroll 1
+            for (int i = PARTS * NI - 1; i >= 0; i--) {
+              const int r = row0 + 8 * i;
+              const bool a = r <= last && (r >= from || r < p.sinks), b = r + 1 <= last && (r + 1 >= from || r + 1 < p.sinks);
+              seen = seen << 2 | (b ? 2u : 0u) | (a ? 1u : 0u);
+            }
 #pragma unroll
             for (int x = 0; x < PARTS; x++)
 #pragma unroll
-              for (int i = 0; i < NI; i++) {
-                const int r = row0 + NC * x + 8 * i;
-                const bool a = r <= last && (r >= from || r < p.sinks), b = r + 1 <= last && (r + 1 >= from || r + 1 < p.sinks);
-                t[x][k][i] = f32x2(a ? t[x][k][i].lo() : -INFINITY, b ? t[x][k][i].hi() : -INFINITY);
-              }
+              for (int i = 0; i < NI; i++)
+                t[x][k][i] = f32x2(seen >> (2 * (NI * x + i)) & 1u ? t[x][k][i].lo() : -INFINITY, seen >> (2 * (NI * x + i)) & 2u ? t[x][k][i].hi() : -INFINITY);
           }
         }
         float top[2];
@@ -755,47 +744,33 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         const float4* const m = s.m[pieces % 3];
         const float unit = sum == 0.f ? 0.f : p.value_unit * rsqrtf((float)D) / sum;
 #pragma unroll 1
-        for (int set = set0; set < set1; set += 2) {
-          float v[2][32];
-          {
-            uint32_t r[2][32];
-            chunk_ld32(o_col + 32 * set, r[0]);
-            chunk_ld32(o_col + 32 * set + 32, r[1]);
-            tc_wait_ld();
-            chunk_landed(r[0]);
-            chunk_landed(r[1]);
+        for (int set = set0; set < set1; set++) {
+          uint32_t r[32];
+          float v[32];
+          tc_ld32(o_col + 32 * set, r);
+          chunk_landed(r);
 #pragma unroll
-            for (int k = 0; k < 32; k++) {
-              v[0][k] = __uint_as_float(r[0][k]) * unit;
-              v[1][k] = __uint_as_float(r[1][k]) * unit;
-            }
-          }
+          for (int k = 0; k < 32; k++) v[k] = __uint_as_float(r[k]) * unit;
+          chunk_so4<true>(m + 32 * set, v);
+          chunk_wht32(v);
 #pragma unroll
-          for (int y = 0; y < 2; y++) {
-            chunk_so4<true>(m + 32 * (set + y), v[y]);
-            chunk_wht32(v[y]);
+          for (int i = 0; i < 2; i++) {
+            uint32_t y[16];
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-              uint32_t z[16];
-#pragma unroll
-              for (int k = 0; k < 16; k++) z[k] = __float_as_uint(v[y][16 * i + k]);
-              tc_st16(o_col + 32 * (set + y) + 16 * i, z);
-            }
+            for (int k = 0; k < 16; k++) y[k] = __float_as_uint(v[16 * i + k]);
+            tc_st16(o_col + 32 * set + 16 * i, y);
           }
         }
         tc_wait_st();
         tc_fence_before();
         cta_bar_sync_n(pair_bar, 64);
         tc_fence_after();
-        constexpr int XC = D == 128 ? 16 : 8;  // columns of a run at a time
+        constexpr int XC = 8;  // columns of a run at a time
 #pragma unroll 1
         for (int x = 0; x < 32; x += XC) {
           uint32_t u[SETS][XC];
 #pragma unroll
-          for (int r = 0; r < SETS; r++) {
-            if constexpr (XC == 16) tc_ld16_issue(o_col + 32 * r + x, u[r]);
-            else chunk_ld8(o_col + 32 * r + x, u[r]);
-          }
+          for (int r = 0; r < SETS; r++) chunk_ld8(o_col + 32 * r + x, u[r]);
           tc_wait_ld();
 #pragma unroll
           for (int r = 0; r < SETS; r++) chunk_landed(u[r]);
