@@ -363,16 +363,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       const uint64_t k_desc = smem_desc_k128(smem_u32(smem + L::OFF_K)), v_desc = smem_desc_k128(smem_u32(smem + L::OFF_V));
       const uint64_t q_desc = smem_desc_k128(smem_u32(smem + L::OFF_Q));
       const uint32_t s_full_1[2] = {chunk_at(&s.s_full[0], 1), chunk_at(&s.s_full[1], 1)};
+      constexpr int ROLL = D == 256 ? 8 : 1;  // (a product of 64 columns takes half as long as the loop around four of them allows for)
       auto scores = [&](uint32_t i) {  // S = Q K^T of step i, whose levels are there; the second terms first
         const uint32_t o = i & 1, st = i % ST;
         const uint64_t b = k_desc + st * (L::OPERAND >> 4);
         const uint32_t d = tmem + L::S_COL + o * NB;
         if (elect_one()) {
+#pragma unroll ROLL
+          for (int k = 0; k < 2 * (D / 64); k++) {  // 64 coordinates: of the second terms, then of the first
+            const int hi = k / (D / 64), slab = k % (D / 64);
+            const uint64_t bs = b + slab * (NB / 2 * 128 >> 4);
 #pragma unroll
-          for (int k = 0; k < 2 * (D / 16); k++) {
-            const int kk = k % (D / 16), hi = k / (D / 16), at = ((kk >> 2) * (NB / 2 * 128) + (kk & 3) * 32) >> 4;
-            if (D == 256 && !hi) chunk_mma_ss(d, q_desc + (((kk >> 2) * 16384 + (kk & 3) * 32) >> 4), b + at, L::IDESC_QK, k != 0);
-            else chunk_mma(d, tmem + L::Q_COL + (hi ? 0 : D / 2) + kk * 8, b + at, L::IDESC_QK, k != 0);
+            for (int i = 0; i < 4; i++) {
+              if (D == 256 && !hi) chunk_mma_ss(d, q_desc + ((slab * 16384 + i * 32) >> 4), bs + (i * 32 >> 4), L::IDESC_QK, k + i != 0);
+              else chunk_mma(d, tmem + L::Q_COL + (hi ? 0 : D / 2) + (4 * slab + i) * 8, bs + (i * 32 >> 4), L::IDESC_QK, k + i != 0);
+            }
           }
           chunk_commit(&s.s_full[o]);
           chunk_commit(&s.k_empty[st]);
@@ -385,11 +390,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         const uint32_t o = i & 1, st = i % ST;
         const uint64_t b = v_desc + st * (L::OPERAND >> 4);
         if (elect_one()) {
+#pragma unroll 1
+          for (int k = 0; k < NB / 64; k++)  // 64 rows: two parts of weights
 #pragma unroll
-          for (int k = 0; k < NB / 16; k++) {
-            const uint32_t a = tmem + L::S_COL + o * NB + (k / (NC / 16)) * NC + (k % (NC / 16)) * 8;
-            chunk_mma(tmem + L::O_COL, a, b + (((k >> 2) * (D / 2 * 128) + (k & 3) * 32) >> 4), L::IDESC_PV, !(first && k == 0));
-          }
+            for (int i = 0; i < 4; i++)
+              chunk_mma(tmem + L::O_COL, tmem + L::S_COL + o * NB + (2 * k + (i >> 1)) * NC + (i & 1) * 8, b + ((k * (D / 2 * 128) + i * 32) >> 4), L::IDESC_PV, !(first && k + i == 0));
           chunk_commit(&s.o_done[o]);
           chunk_commit(&s.v_empty[st]);
         }
@@ -419,50 +424,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         }
       }
     }
-  } else if (warp >= L::V_WARP) {
-    // ================================================================ V levels: a thread 64 rows of a coordinate, half of its record
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::LEVEL_REGS));
-    const int t = tid - 32 * L::V_WARP;
-    const int coord = D == 128 ? t & 63 : t, part = D == 128 ? t >> 6 : 0;
-    const uint8_t* const src = p.v_codes + (rank * (D / 2) + coord) * R + part * (R / 2);
-    uint8_t* const slab = smem + L::OFF_V + part * (D / 2 * 128);
-    const uint32_t v_full = chunk_at(s.v_full, 0);
-    ChunkSteps steps;
-    steps.start(p, s.range);
-    uint32_t raw[2 * BITS];
-    auto load = [&]() { chunk_load<BITS>(src + steps.row0 * P + (SUB > 1 ? (steps.j & 1) * (R / 2) : 0), raw); };
-    bool have = steps.next<SUB>(p, lane, nullptr);
-    if (have) load();
-    while (have) {
-      const uint32_t st = n % ST;
-      if (n >= ST) chunk_wait(&s.v_empty[st], ((n / ST) - 1) & 1, p.wait_polls, &s.failed);
-      chunk_levels<BITS>(raw, p.lut_v_lo, p.lut_v_hi, p.lookup, slab + st * L::OPERAND, coord);
-      have = steps.next<SUB>(p, lane, nullptr);
-      if (have) load();
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) chunk_arrive(v_full + 8 * st);
-      n++;
-    }
   } else if (warp >= L::K_WARP) {
-    // ================================================================ K levels, a thread 64 coordinates of a row; factors of all rows
+    // ================================================================ levels: of K, a thread 64 coordinates of a row, and the factors of the
+    // rows; of V, 64 rows of a coordinate. One code for both: instructions that are not at hand are what a warp here waits for most.
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::LEVEL_REGS));
-    const int t = tid - 32 * L::K_WARP;
-    const int r = t % (NB / 2), part = t / (NB / 2);
-    uint8_t* const slab = smem + L::OFF_K + part * (NB / 2 * 128);
-    const uint32_t k_full = chunk_at(s.k_full, 0);
+    const bool is_v = warp >= L::V_WARP;
+    const int t = tid - 32 * (is_v ? L::V_WARP : L::K_WARP);
+    constexpr int KR = NB / 2, VR = D / 2;  // rows of the CTA's operand: of K, coordinates of V
+    const int r = is_v ? t % VR : t % KR, part = is_v ? t / VR : t / KR;
+    const uint8_t* const src = is_v ? p.v_codes + (rank * VR + r) * R + part * (R / 2) : p.k_codes + (rank * KR + r) * P + part * (8 * BITS);
+    const int sub_bytes = is_v ? R / 2 : NB * P;  // from a block's first step to its second
+    uint8_t* const slab = smem + (is_v ? L::OFF_V + part * (VR * 128) : L::OFF_K + part * (KR * 128));
+    uint64_t* const empty = is_v ? s.v_empty : s.k_empty;
+    const uint32_t full = chunk_at(is_v ? s.v_full : s.k_full, 0);
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      lo[i] = is_v ? p.lut_v_lo[i] : p.lut_lo[i];
+      hi[i] = is_v ? p.lut_v_hi[i] : p.lut_hi[i];
+    }
+    const bool factors = !is_v && t < NB;
     ChunkSteps steps;
     steps.start(p, s.range);
     uint32_t raw[2 * BITS];
     float ks = 0.f, vs = 0.f;
     auto load = [&]() {
-      const size_t first = steps.row0 + (SUB > 1 ? (steps.j & 1) * NB : 0);  // the step's first row
-      chunk_load<BITS>(p.k_codes + (first + rank * (NB / 2) + r) * P + part * (8 * BITS), raw);
-      ks = vs = 0.f;
-      const int row = steps.c.x.block(steps.c.lo + steps.j / SUB) * 128 + (SUB > 1 ? (steps.j & 1) * NB : 0) + t;
-      if (t < NB && row < steps.c.x.end) {  // (rows that no token sees may hold anything)
-        ks = load_scale(p.k_scales, first + t, p.scale_f16);
-        vs = load_scale(p.v_scales, first + t, p.scale_f16);
+      chunk_load<BITS>(src + steps.row0 * P + (SUB > 1 ? (steps.j & 1) * sub_bytes : 0), raw);
+      if (factors) {
+        const int first = SUB > 1 ? (steps.j & 1) * NB : 0, row = steps.c.x.block(steps.c.lo + steps.j / SUB) * 128 + first + t;
+        ks = vs = 0.f;
+        if (row < steps.c.x.end) {  // (rows that no token sees may hold anything)
+          ks = load_scale(p.k_scales, steps.row0 + first + t, p.scale_f16);
+          vs = load_scale(p.v_scales, steps.row0 + first + t, p.scale_f16);
+        }
       }
     };
     uint32_t* const status = warp == L::K_WARP && rank == 0 ? p.status : nullptr;
@@ -470,20 +464,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
     if (have) load();
     while (have) {
       const uint32_t st = n % ST;
-      if (n >= ST) chunk_wait(&s.k_empty[st], ((n / ST) - 1) & 1, p.wait_polls, &s.failed);
-      if (t < NB) {
+      if (n >= ST) chunk_wait(&empty[st], ((n / ST) - 1) & 1, p.wait_polls, &s.failed);
+      if (factors) {
         float* const col = reinterpret_cast<float*>(&s.column[n % L::COLUMNS][t >> 1]) + (t & 1);
         vs = vs < CHUNK_LEAST_SCALE ? CHUNK_LEAST_SCALE : vs;
         col[0] = ks * p.score_unit;
         col[2] = log2f(vs);
         s.weight[n % L::COLUMNS][t] = vs < INFINITY ? 1.f / vs : 1.f;  // (finite: tokens that do not see the row multiply it by 0)
       }
-      chunk_levels<BITS>(raw, p.lut_lo, p.lut_hi, p.lookup, slab + st * L::OPERAND, r);
+      chunk_levels<BITS>(raw, lo, hi, p.lookup, slab + st * L::OPERAND, r);
       have = steps.next<SUB>(p, lane, status);
       if (have) load();
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) chunk_arrive(k_full + 8 * st);
+      if (lane == 0) chunk_arrive(full + 8 * st);
       n++;
     }
   } else {
