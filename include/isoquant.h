@@ -24,8 +24,8 @@
  *     `status_dev` array of 4 uint32 (zeroed by the caller): [0] bit mask of IQ_STATUS_* flags,
  *     [1] rows whose codes were re-decided in fp64 (see iq_quantize_append), [2] rows skipped because they fell outside the
  *     cache (the page pool's calls: entries or forks that they could not serve), [3] reserved. Nothing on the device traps or spins without a bound: the waits of the
- *     decode, tree attention, bulk append and reconstruction kernels on asynchronous copies and tensor-core results give up after 65536 polls
- *     of at most 20 us each (about a second at worst; a wait that works lasts microseconds). Decode, tree attention and append then flag
+ *     decode, tree, chunk and cross attention, bulk append and reconstruction kernels on asynchronous copies and tensor-core results give up after 65536 polls
+ *     of at most 20 us each (about a second at worst; a wait that works lasts microseconds). All but the last then flag
  *     IQ_STATUS_WAIT_TIMEOUT and return with invalid results; iq_reconstruct_rows, which has no status array, writes NaN
  *     to the rows concerned.
  *
@@ -94,11 +94,11 @@ enum {
 
 enum {
   IQ_STATUS_ROW_OUT_OF_RANGE = 1u, /* quantize-append: append_pos + i >= t_cap, row skipped */
-  IQ_STATUS_WAIT_TIMEOUT = 2u,     /* decode, tree attention, bulk append: a bounded wait on an asynchronous copy or tensor-core result ran out; results invalid */
+  IQ_STATUS_WAIT_TIMEOUT = 2u,     /* decode, tree, chunk and cross attention, bulk append: a bounded wait on an asynchronous copy or tensor-core result ran out; results invalid */
   IQ_STATUS_SCALE_OVERFLOW = 8u,   /* binary16 scales: a row norm above 65504 was stored as 65504 */
   IQ_STATUS_BAD_PAGE = 4u,         /* paged cache: a block-table entry outside [0, num_pages) was met: read as page 0 by
-                                      decode / tree attention / reconstruct, the rows skipped (and counted in [2]) by quantize-append
-                                      and iq_keep_rows; see the page pool's calls for theirs */
+                                      decode / tree, chunk and cross attention / reconstruct, the rows skipped (and counted in [2]) by quantize-append
+                                      and iq_keep_rows, a slot of -1 from iq_plan_tokens; see the page pool's calls for theirs */
   IQ_STATUS_NO_PAGE = 16u,         /* page pool: fewer free pages than a call needed; the entries that got none hold -1, counted in [2] */
   IQ_STATUS_BAD_SEQUENCE = 32u     /* iq_fork_sequences: a fork whose numbers are out of range or that conflicts with another, skipped, counted in [2] */
 };
@@ -564,7 +564,7 @@ int iq_copy_pages(const iq_shape* shape, const iq_cache* cache, const int32_t* s
  * A step over requests of any lengths: prompts, pieces of prompts and single tokens together (the paper decodes one token at a time).
  * Its tokens may come padded, n_tokens_max places per sequence, or packed, one request after the other: token_start_dev, device int32
  * [batch + 1], then says where each sequence's tokens start among the n_tokens_max places of the step (clamped to [0, n_tokens_max]; a start
- * behind the next counts as no tokens). The calls below take them in either form.
+ * behind the next counts as no tokens; places of two sequences hold the results of either). The calls below take them in either form.
  *
  * iq_plan_tokens lays out a packed step from the requests' lengths: token_start[b] = sum of n_new[0 .. b - 1] (negative counts as 0), and
  * for place i, which is token j of sequence b: positions[i] = ctx_lens[b] + j, sequences[i] = b, slots[i] = the cache row that holds the token:
@@ -577,7 +577,7 @@ int iq_copy_pages(const iq_shape* shape, const iq_cache* cache, const int32_t* s
  *                             for the new rows are reserved before (iq_reserve_pages).
  *   token_start_dev           device int32 [batch + 1]; positions_dev, sequences_dev device int32 [n_tokens_max], slots_dev device
  *                             int64 [n_tokens_max], each of the three may be NULL. Nothing may overlap the inputs.
- * shape: its batch and t_cap are read. batch up to 65535 (IQ_ERR_LIMIT).
+ * shape: its batch (up to 65535, as everywhere) and t_cap are read.
  */
 #define IQ_NO_POSITION INT32_MIN
 int iq_plan_tokens(const iq_shape* shape, const int32_t* ctx_lens_dev, const int32_t* n_new_dev, const int32_t* block_table_dev,
@@ -652,11 +652,13 @@ int iq_quantize_append_packed(const iq_shape* shape, const float* rot_dev, const
  *   status_dev     optional (see top). Pages whose rows no token sees need not be in the block table.
  * Codebooks as for iq_decode_attention; scales must not be negative. A token that sees no row yields out = 0, lse = -inf.
  * Arithmetic: q~ as two binary16 terms (22 bits of the largest element of 128 (token, head) pairs), levels exact; a row's weight times its V
- * scale, relative to the largest such of its token, as one binary16 value (2^-12 of it, or 2^-30 of the largest); tensor-core sums
- * over a CTA's share of the rows, joined in fp32. V scales below 2^-60 count as 2^-60. The same inputs give the same bits in every call on
- * the same kind of device.
+ * scale, relative to the largest such of its token, as one binary16 value (off by 2^-11 of itself, or 2^-30 of the largest); tensor-core
+ * sums over a share of the rows, joined in fp32. V scales below 2^-60 count as 2^-60. Sequences of few tokens (64 / heads per KV head where
+ * n_tokens_max says that there are no longer ones, else 16 / heads per KV head in batches of two or more, of up to 2^13 and 2^15 sequences times KV
+ * heads) go through iq_tree_attention's kernel, with its arithmetic. The same call with the same inputs gives the same bits every time on the same kind of
+ * device; a sequence's bits can depend on which others are in the call, within these roundings.
  * Limits (IQ_ERR_LIMIT): n_tokens_max as above and times the heads per KV head below 2^31 - 128; t_cap at most 2^31 - 2^21; heads per KV head times
- * t_cap times all tiles of 128 (token, head) pairs below about 2^53.
+ * (t_cap + n_tokens_max) times n_kv_heads * batch * (n_tokens_max * heads per KV head / 128 + 1) tiles below about 2^53, also where packed.
  */
 #define IQ_CHUNK_MAX_TOKENS (1 << 20)
 size_t iq_chunk_workspace_bytes(const iq_shape* shape); /* 0: a shape that the calls refuse */

@@ -1257,8 +1257,8 @@ static int chunk_attention(const iq_shape* shape, const float* rot_dev, const iq
   if (token_start_dev && n_tokens_dev) return IQ_ERR_SHAPE;
   const int group = shape->n_q_heads / shape->n_kv_heads;
   if (n_tokens_max > IQ_CHUNK_MAX_TOKENS || (long long)n_tokens_max * group >= (1ll << 31) - 128) return IQ_ERR_LIMIT;
-  const double tokens = token_start_dev ? (double)n_tokens_max : (double)n_tokens_max * shape->batch;
-  // units of the launch (chunk_units): tiles times what one can count
+  // units of the launch (chunk_units): tiles times what one can count; nothing says that packed sequences do not overlap, so they count as padded ones
+  const double tokens = (double)n_tokens_max * shape->batch;
   const double tiles = shape->n_kv_heads * (tokens * group / 128.0 + shape->batch);
   if (tiles * ((double)group * ((double)shape->t_cap + n_tokens_max + 1024.0) + 256.0) >= 9007199254740992.0) return IQ_ERR_LIMIT;
   if (shape->batch == 0 || n_tokens_max == 0) return IQ_OK;

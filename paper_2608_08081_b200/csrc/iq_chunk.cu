@@ -8,7 +8,7 @@ namespace {
 constexpr int CHUNK_MERGE_WARPS = 4;
 // CTA (c, y): rows 4 y ... of the tile that begins in the range of pair c of the launch and ends in a later one, a warp to a row: the tile's
 // partials, from consecutive pairs, then o = R^T o~. All that is read hangs on the pairs' notes alone, so it takes three trips to memory one after
-// the other. (With the pieces worked out again from the lengths, two rows to a warp: 12 us for 8 tiles, 44 for 40 at head_dim 256.)
+// the other. (With the pieces worked out again from the lengths, two rows to a warp: 12 us for 8 tiles, 44 for 40 at head_dim 256; now 7 and 20.)
 template <int D>
 __global__ void __launch_bounds__(CHUNK_MERGE_WARPS * 32) chunk_merge_kernel(const __grid_constant__ ChunkParams p) {
   constexpr int E = D / 32, NF = 4;

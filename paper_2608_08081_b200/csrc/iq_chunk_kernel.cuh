@@ -1,15 +1,33 @@
-// Attention of any number of new tokens over the packed cache: tiles of 128 (token, query head) pairs of a KV head, one pass over the
-// blocks that they see.
+// Attention of any number of new tokens over the packed cache: tiles of 256 (token, query head) pairs of a KV head, shared by a pair of CTAs, one
+// pass over the blocks that they see.
 //
-// A step of NB cached rows: S[pair][row] = Q K^T, Q the rotated queries as two binary16 terms, K the levels of the codes; w = S scale_K + log2(scale_V)
-// in units of log2; p = 2^(w - reference_pair); O[pair][coordinate] += p V, V the levels; l_pair += p / scale_V. The output is R^T O / l.
+// A step of NB cached rows: S[pair][row] = Q K^T, Q the rotated queries as two binary16 terms, K the levels of the codes;
+// t = S scale_K + log2(scale_V) - reference_pair in units of log2; p = 2^t; O[pair][coordinate] += p V, V the levels; l_pair += p / scale_V. The
+// output is R^T O / l.
 // A row's V scale is part of its exponent, so p is the row's weight in the OUTPUT, and the reference follows the largest of those: p
 // goes to the tensor cores as one binary16 value, whose 11 bits hold down to 2^-19 of it and which leaves out less than 2^-30 of it, also where
 // a row with most of the weight has next to no value. One term's rounding is as much error as that of the binary16 output; the queries' would
-// grow with the scores, so they have two (22 bits; of the tile's largest element, as one power of two scales all of them).
-// References are raised only when a weight passes 2^15: then sums and O are scaled (a raised reference lies 5 log2 units below the block's
+// grow with the scores, so they have two (22 bits; of the largest element of the CTA's 128 pairs, as one power of two scales all of them).
+// References are raised only when a weight passes 2^15: then sums and O are scaled (a raised reference lies 5 log2 units below the step's
 // maximum).
 //
+// Work split. The two CTAs of a pair have 128 rows of Q, S and O each in their tensor memory, and half of the levels of a step each in shared memory: one
+// product of both (cta_group::2, M = 256) reads the operand once from either, and each block is dequantised once for 256 pairs. Warps of a
+// CTA: eight softmax, 16 rows each; four that make K levels, four V levels; one that issues the products of the pair; three that bring the next
+// tile's queries. Softmax warps meet nobody in the loop over the steps. Items (sequence, KV head, tile) are laid end to end and cut into
+// equal ranges, one per pair of CTAs; tiles that two or more pairs share are merged by a second launch.
+//
+// What bounds it. 4096 tokens behind 28 000 rows, 64/8 heads, 3 bits: 5.3 ms = 0.76 PFLOP/s of the 4 d a (pair, row) needs; the two terms of Q make it
+// 6 d, 1.14 PFLOP/s on the tensor pipe. A step of 128 rows takes the pipe 1536 cycles and a softmax warp some 2700, one instruction after the
+// other: barrier 210, scores 250, exponents 850, exponentials and sums 1150, weights handed over 110, loop 150. Two buffers of scores
+// and a trip of 2100 cycles from weights to the scores that take their place keep the steps from overlapping further. The schedulers issue in 0.49 of
+// the cycles, the special-function pipe is busy 0.32, shift/logic 0.33, the tensor pipe 0.47 (1000 tokens behind 6000 rows, 171 us, of
+// which the beginning and end of a piece take 6 us each).
+// Built and slower: one CTA to a tile (issue 0.55 of the cycles, half of it for levels: 5.9 ms for 5.1); four softmax warps to 32 rows, a quarter of the
+// columns each, which meet once a step (3200 cycles a step); a fourth to three quarters of the exponentials as polynomials of degree 4 on the
+// multiply-add pipe (215 us: 221, 228, 239); the next step's scores asked for before the weights are handed over (175 us: 185). Code that is
+// not at hand costs as much as any pipe: with a piece's rotations in long unrolled code and K and V levels in code of their own, 10 % of the
+// instruction fetches missed (now 3.6 %) and 64 tokens behind 1000 rows took 29.9 us instead of 26.7.
 #pragma once
 #include <type_traits>
 
@@ -19,8 +37,8 @@
 
 namespace iq {
 
-constexpr float CHUNK_LIMIT = 15.f;                // log2 of the largest p ...
-constexpr float CHUNK_START = 5.f;                 // ... and of the block's largest behind a raise
+constexpr float CHUNK_LIMIT = 15.f;                   // log2 of the largest p ...
+constexpr float CHUNK_START = 5.f;                    // ... and of the step's largest behind a raise
 constexpr float CHUNK_LEAST_SCALE = 8.67361738e-19f;  // 2^-60: V scales below it count as this
 
 // Layouts of the loads: 16x256b leaves rows lane / 4 and lane / 4 + 8 of 16 and columns 2 (lane % 4), + 1 of every 8 with a thread (so that it needs the
@@ -103,7 +121,7 @@ struct ChunkLayout {
   static constexpr int PARTS = NB / NC;
   static constexpr int SETS = D / 32;              // runs of 32 coordinates
   // Warps: softmax, K levels, V levels, products (one, in the first CTA of a pair), queries on their way. Registers of a thread: 96 at
-  // launch, 480 over the five groups of warps (two of them softmax, two levels).
+  // launch, 480 over the five groups of warps (two of them softmax, two levels): as many as none of them spills with (152, 64 and 48: 2 - 8 % slower).
   static constexpr int SOFTMAX_WARPS = 8, K_WARP = 8, V_WARP = 12, MMA_WARP = 16, QUERY_WARP = 17, THREADS = 640;
   static constexpr int SOFTMAX_REGS = 128, LEVEL_REGS = 72, MMA_REGS = 80;
   // tensor memory: Q (D = 128: both terms; 256: the first), two buffers of scores, O. The probabilities of NC columns go over their
@@ -343,9 +361,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
             const uint4 x = *reinterpret_cast<const uint4*>(smem + L::OFF_RAW + r * (2 * D) + ((k ^ (r & 7)) << 4));
             const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-            for (int k2 = 0; k2 < 4; k2++) top = __hmax2(top, __habs2(*reinterpret_cast<const __half2*>(&w[k2])));
+            for (int k2 = 0; k2 < 4; k2++) {
+              const uint32_t a = w[k2] & 0x7FFF7FFFu;
+              const __half2 h = *reinterpret_cast<const __half2*>(&a);
+              const uint32_t kept = a & ~__heq2_mask(h, __half2half2(__ushort_as_half(0x7C00)));  // (an infinite query is its own affair, as NaN)
+              top = __hmax2(top, *reinterpret_cast<const __half2*>(&kept));
+            }
           }
-          const float most = warp_max(fminf(fmaxf(__low2float(top), __high2float(top)), 65504.f));  // (an infinite query is its own affair)
+          const float most = warp_max(fmaxf(__low2float(top), __high2float(top)));
           if (lane == 0) s.warp_q[pieces & 3][warp - L::QUERY_WARP] = most;
         }
         __syncwarp();
@@ -482,9 +505,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
     }
   } else {
     // ================================================================ queries, softmax, outputs
-    // A warp has 16 rows and all columns of S: its references and sums are nobody else's, so it meets no other in the loop over the steps, and the
-    // exponentials of one warp of a scheduler run under the waits of the other. (Four warps to 32 rows, a quarter of the columns each, met once a
-    // step and took 3200 cycles for it, the two barriers' latencies one after the other.)
+    // A warp has 16 rows and all columns of S: its references and sums are nobody else's, so it meets no other in the loop over the steps.
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
     const int quad = warp & 3, half = warp >> 2;           // rows 32 quad + 16 half ...; half of the coordinates of rows 32 quad ...
     const uint32_t lanes = (uint32_t)quad << 21;           // the quarter of the tensor-memory lanes

@@ -130,6 +130,24 @@ def test_a_query_that_is_not_finite_concerns_its_own_output(iq, d):
 
 
 @pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("x", [np.inf, -np.inf, np.nan])
+def test_a_query_that_is_not_finite_changes_no_bit_of_the_others(iq, d, x):
+    c = Step(iq, 12, H=4, hk=1, d=d, ctx=100, tokens=70)
+    res = []
+    for y in (0.0, x):
+        c.q[0][7, 2, 5] = c.q[0][66, 1, d - 1] = y
+        c.upload()
+        out, lse = c.outputs()
+        c.call(out, lse)
+        res.append((out, lse))
+    ok = torch.ones((70, 4), dtype=torch.bool)
+    ok[7, 2] = ok[66, 1] = False
+    assert torch.equal(res[0][0][0].cpu()[ok], res[1][0][0].cpu()[ok])
+    assert torch.equal(res[0][1][0].cpu()[ok], res[1][1][0].cpu()[ok])
+    assert bool(torch.isnan(res[1][0][0].cpu()[~ok]).any(-1).all())
+
+
+@pytest.mark.parametrize("d", [128, 256])
 def test_tokens_behind_the_cache(iq, d):
     """Rows from t_cap on are not there: their tokens see the cache, and those with a window behind it nothing."""
     Step(iq, 12, H=4, hk=1, d=d, ctx=200, tokens=150, t_cap=256).run()
