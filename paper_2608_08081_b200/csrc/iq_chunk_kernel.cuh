@@ -5,11 +5,12 @@
 // t = S scale_K + log2(scale_V) - reference_pair in units of log2; p = 2^t; O[pair][coordinate] += p V, V the levels; l_pair += p / scale_V. The
 // output is R^T O / l.
 // A row's V scale is part of its exponent, so p is the row's weight in the OUTPUT, and the reference follows the largest of those: p
-// goes to the tensor cores as one binary16 value, whose 11 bits hold down to 2^-19 of it and which leaves out less than 2^-30 of it, also where
+// goes to the tensor cores as one binary16 value, whose 11 bits hold down to 2^-14 of it and which leaves out less than 2^-25 of it, also where
 // a row with most of the weight has next to no value. One term's rounding is as much error as that of the binary16 output; the queries' would
 // grow with the scores, so they have two (22 bits; of the largest element of the CTA's 128 pairs, as one power of two scales all of them).
-// References are raised only when a weight passes 2^15: then sums and O are scaled (a raised reference lies 5 log2 units below the step's
-// maximum).
+// References are raised only when a weight passes 2^15: then sums and O are scaled, which waits for the values of the step before (a raised
+// reference is the step's maximum; 5 log2 units below it, which would hold 5 bits more of the smallest weights, cost 172 us for 162 with 1000 tokens behind 6000 rows;
+// 3 units above it 161).
 //
 // Work split. The two CTAs of a pair have 128 rows of Q, S and O each in their tensor memory, and half of the levels of a step each in shared memory: one
 // product of both (cta_group::2, M = 256) reads the operand once from either, and each block is dequantised once for 256 pairs. Warps of a
@@ -38,7 +39,7 @@
 namespace iq {
 
 constexpr float CHUNK_LIMIT = 15.f;                   // log2 of the largest p ...
-constexpr float CHUNK_START = 5.f;                    // ... and of the step's largest behind a raise
+constexpr float CHUNK_START = 0.f;                    // ... and of the step's largest behind a raise
 constexpr float CHUNK_LEAST_SCALE = 8.67361738e-19f;  // 2^-60: V scales below it count as this
 
 // Layouts of the loads: 16x256b leaves rows lane / 4 and lane / 4 + 8 of 16 and columns 2 (lane % 4), + 1 of every 8 with a thread (so that it needs the
