@@ -42,6 +42,18 @@ constexpr float CHUNK_LIMIT = 15.f;                   // log2 of the largest p .
 constexpr float CHUNK_START = 0.f;                    // ... and of the step's largest behind a raise
 constexpr float CHUNK_LEAST_SCALE = 8.67361738e-19f;  // 2^-60: V scales below it count as this
 
+// (Off by 2^-22 of the logarithm, and by one unit in the last place. log2f and a division: 1 % more time.)
+__device__ __forceinline__ float chunk_log2(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float chunk_inverse(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Layouts of the loads: 16x256b leaves rows lane / 4 and lane / 4 + 8 of 16 and columns 2 (lane % 4), + 1 of every 8 with a thread (so that it needs the
 // factors of 16 columns, not of all), 16x128b takes back the same as pairs of binary16 values, one to a column.
 __device__ __forceinline__ void chunk_ld_rows(uint32_t taddr, uint32_t (&r)[16]) {
@@ -493,8 +505,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         float* const col = reinterpret_cast<float*>(&s.column[n % L::COLUMNS][t >> 1]) + (t & 1);
         vs = vs < CHUNK_LEAST_SCALE ? CHUNK_LEAST_SCALE : vs;
         col[0] = ks * p.score_unit;
-        col[2] = log2f(vs);
-        s.weight[n % L::COLUMNS][t] = vs < INFINITY ? 1.f / vs : 1.f;  // (finite: tokens that do not see the row multiply it by 0)
+        col[2] = chunk_log2(vs);
+        s.weight[n % L::COLUMNS][t] = vs < INFINITY ? chunk_inverse(vs) : 1.f;  // (finite: tokens that do not see the row multiply it by 0)
       }
       chunk_levels<BITS>(raw, lo, hi, p.lookup, slab + st * L::OPERAND, r);
       have = steps.next<SUB>(p, lane, status);

@@ -15,7 +15,8 @@ def attention(rows, table, page_rows, quats, levels_k, levels_v, q, ctx, tokens,
 
     The bounds. A score: as in branching.attention, (d / 16 + 2) cuts of a tensor-core sum, twice, of 2^-24 of |q| |k| sm each, and as much
     again for the rounding of q~ (22 bits) and the products with scales. An exponent is the sum of the score, the logarithm of the V scale
-    and the reference in 32 bits: three roundings of 2^-24 of its parts' size (log2 units). exp2, products and sums: (rows / 128 + 64)
+    and the reference in 32 bits: three roundings of 2^-24 of its parts' size (log2 units), and the logarithm is
+    off by 2^-22 of itself (lg2.approx: four more). exp2, products and sums: (rows / 128 + 64)
     roundings of 2^-22. A weight's rounding to binary16: half a step is 2^-11 of it, independent between rows, so their sum is 2^-11
     sqrt(sum (p |v|)^2 / 3) in the mean; three and a half times that is allowed. What binary16 leaves out below its normal numbers (2^-14): half a step there
     is 2^-25, and the largest weight times value of a row of queries is 1 or more, as a new reference is the largest so far: 2^-25 of it, per row. The tensor core's running sums over the rows: a cut of 2^-23 of the sum so far every 16 rows, by halves."""
@@ -58,7 +59,7 @@ def attention(rows, table, page_rows, quats, levels_k, levels_v, q, ctx, tokens,
             count = on.sum(1)[:, None].double()
             dz = 4 * (d / 16 + 2) * 2.0 ** -24 * qr.norm(dim=-1) * kn.max() * sm
             size = z.masked_fill(~on[:, None], 0.0).abs().amax(-1) / math.log(2) + abs(np.log2(max(float(vn.max()), 1e-18))) + 64
-            dw = dz + 3 * 2.0 ** -24 * size * math.log(2) + (count / 128 + 64) * 2.0 ** -22
+            dw = dz + 7 * 2.0 ** -24 * size * math.log(2) + (count / 128 + 64) * 2.0 ** -22
             pv = p * vn
             tol[:, hs] = torch.where(some, 2 * dw * torch.where(on[:, None], vn, 0.0).amax(-1) + 3.5 * 2.0 ** -11 * pv.square().sum(-1).div(3).sqrt() / l
                                      + count * 2.0 ** -25 * pv.amax(-1) / l + count / 16 * 2.0 ** -24 * pv.sum(-1) / l, 0.0)
