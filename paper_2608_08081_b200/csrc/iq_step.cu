@@ -97,7 +97,7 @@ constexpr int ROTARY_TOKENS = 16;  // most tokens of a CTA
 // A CTA: `tokens` tokens, the angles of each once for all heads. An angle is position times frequency in turns, a 64-bit fraction: the
 // product modulo 2^64 is the turn's fraction, exactly, however far the position. A thread takes 16 elements of a head, 8 pairs.
 // Bound by memory: 8192 tokens, 64/8 heads of 128: 55.6 us = 5.4 TB/s read and written (one token 2.9). Two tasks of a thread in flight: slower;
-// the first one's elements asked for before the angles are worked out: 60.5 us (2107 tokens, 16/8 heads of 256, a quarter turned: 10.6 for 11.7).
+// as many threads as fill all rounds: 57.4 us (1000 tokens, 32/8 heads: 6.05 for 6.75); the first elements asked for before the angles are worked out: 60.5 us (2107 tokens, 16/8 heads of 256, a quarter turned: 10.6 for 11.7).
 __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(const __grid_constant__ RotaryParams p, int tokens) {
   __shared__ float2 turn[ROTARY_TOKENS * IQ_ROTARY_MAX_PAIRS];  // cosines and sines times the magnitude, [token][pair]
   __shared__ int position[ROTARY_TOKENS];
@@ -182,7 +182,7 @@ cudaError_t launch_apply_rotary(const RotaryParams& p, cudaStream_t stream) {
   const int tasks = (p.side[0].heads + p.side[1].heads) * (p.head_dim / 16);
   const int tokens = min(ROTARY_TOKENS, max(1, 2 * ROTARY_THREADS / tasks));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((p.n_tokens + tokens - 1) / tokens));
+  cfg.gridDim = dim3((unsigned)((p.n_tokens - 1) / tokens + 1));
   cfg.blockDim = dim3(ROTARY_THREADS);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
