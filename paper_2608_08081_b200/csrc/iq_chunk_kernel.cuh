@@ -18,15 +18,16 @@
 // tile's queries. Softmax warps meet nobody in the loop over the steps. Items (sequence, KV head, tile) are laid end to end and cut into
 // equal ranges, one per pair of CTAs; tiles that two or more pairs share are merged by a second launch.
 //
-// What bounds it. 4096 tokens behind 28 000 rows, 64/8 heads, 3 bits: 5.3 ms = 0.76 PFLOP/s of the 4 d a (pair, row) needs; the two terms of Q make it
-// 6 d, 1.14 PFLOP/s on the tensor pipe. A step of 128 rows takes the pipe 1536 cycles and a softmax warp some 2700, one instruction after the
-// other: barrier 210, scores 250, exponents 850, exponentials and sums 1150, weights handed over 110, loop 150. Two buffers of scores
+// What bounds it. 4096 tokens behind 28 000 rows, 64/8 heads, 3 bits: 5.1 ms = 0.79 PFLOP/s of the 4 d a (pair, row) needs; the two terms of Q make it
+// 6 d, 1.19 PFLOP/s on the tensor pipe. A step of 128 rows takes the pipe 1536 cycles and a softmax warp some 2600, one instruction after the
+// other (of 2700 before the last changes: barrier 210, scores 250, exponents 850, exponentials and sums 1150, weights handed over 110, loop 150). Two buffers of scores
 // and a trip of 2100 cycles from weights to the scores that take their place keep the steps from overlapping further. The schedulers issue in 0.49 of
-// the cycles, the special-function pipe is busy 0.32, shift/logic 0.33, the tensor pipe 0.47 (1000 tokens behind 6000 rows, 171 us, of
+// the cycles, the special-function pipe is busy 0.32, shift/logic 0.33, the tensor pipe 0.47 (1000 tokens behind 6000 rows, then 171 us, now 162, of
 // which the beginning and end of a piece take 6 us each).
 // Built and slower: one CTA to a tile (issue 0.55 of the cycles, half of it for levels: 5.9 ms for 5.1); four softmax warps to 32 rows, a quarter of the
 // columns each, which meet once a step (3200 cycles a step); a fourth to three quarters of the exponentials as polynomials of degree 4 on the
-// multiply-add pipe (215 us: 221, 228, 239); the next step's scores asked for before the weights are handed over (175 us: 185). Code that is
+// multiply-add pipe (215 us: 221, 228, 239); the next step's scores asked for before the weights are handed over (175 us: 185); the look at
+// the references behind the exponentials, which then run beside the exponents (no gain). Code that is
 // not at hand costs as much as any pipe: with a piece's rotations in long unrolled code and K and V levels in code of their own, 10 % of the
 // instruction fetches missed (now 3.6 %) and 64 tokens behind 1000 rows took 29.9 us instead of 26.7.
 #pragma once
