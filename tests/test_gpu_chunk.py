@@ -270,6 +270,27 @@ def test_streams_and_graphs(iq):
     c.check(out, lse)
 
 
+@pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("tokens", [3, 70])
+def test_rows_behind_4_gib(iq, d, tokens):
+    """Pages at the end of a pool whose arrays of codes pass 2^32 bytes: the same bits as from a small pool."""
+    c = Step(iq, 29, H=4, hk=1, d=d, ctx=300, tokens=tokens, page_rows=128)
+    want = c.run()
+    small = (c.cache.k_codes, c.cache.k_scales, c.cache.v_codes, c.cache.v_scales)
+    n = small[0].shape[0]
+    pages = (1 << 32) // (small[0].nbytes // n) + n + 1
+    big = []
+    for x in small:
+        y = torch.empty((pages,) + x.shape[1:], dtype=x.dtype, device="cuda")
+        y[pages - n:] = x
+        big.append(y)
+    c.cache = iq.Cache(*big, c.cache.block_table + (pages - n), 128)
+    out, _ = c.outputs()
+    c.call(out)
+    assert c.status.tolist() == [0, 0, 0, 0]
+    assert torch.equal(out, want)
+
+
 def test_two_calls_at_once(iq):
     a, b = Step(iq, 21, H=32, hk=8, ctx=1500, tokens=200).upload(), Step(iq, 22, B=3, H=16, hk=8, d=256, ctx=700, tokens=60).upload()
     oa, ob = a.outputs(), b.outputs()
