@@ -318,6 +318,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
   chunk_pair_sync();
   tc_fence_after();
   const uint32_t tmem = __shfl_sync(FULL, s.tmem, 0);
+  if (s.range.total == 0) {  // (a step whose sequences are all the other kernel's: nothing but the note for the merge)
+    allow_dependent_launch();
+    if (tid == 0 && rank == 0) p.cuts[pair].last = -1;
+    if (warp == L::MMA_WARP) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512));
+    return;
+  }
   uint32_t n = 0;  // steps so far
 
   if (warp >= L::MMA_WARP) {
