@@ -208,7 +208,9 @@ __device__ __forceinline__ void chunk_mma_ss(uint32_t d_tmem, uint64_t adesc, ui
                : "memory");
 }
 // Bounded wait of a converged warp. A wait that gives up is noted in `failed` of both CTAs, and from then on no wait of theirs lasts: every
-// thread goes on through the same loops and barriers over whatever is there, so that the pair ends together.
+// thread goes on through the same loops and barriers over whatever is there, so that the pair ends together. Other warps may note it at any
+// moment, so warps that share a barrier never go by their own reading of it: the query warps by the OR of all of theirs, the softmax warps by
+// one thread's (`go`).
 __device__ __forceinline__ void chunk_wait(uint64_t* bar, uint32_t parity, uint32_t limit, uint32_t* failed) {
   for (uint32_t i = 0; !mbar_try_wait(bar, parity); i++)
     if (i >= limit || *(volatile uint32_t*)failed) {
@@ -349,7 +351,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
           continue;
         }
         if (pieces > 0) chunk_wait(&s.raw_empty, (pieces - 1) & 1, p.wait_polls, &s.failed);
-        if (__any_sync(FULL, *(volatile uint32_t*)&s.failed != 0)) break;  // (what is there may still be read)
+        // One finding for the three warps, which meet at barriers below (where a wait has given up, what is there may still be read).
+        if (cta_bar_or_n(query_bar, 96, *(volatile uint32_t*)&s.failed != 0)) break;
         if (!more) c.hi = c.lo = 0;
         if (t == 0) s.piece[pieces & 3] = c;
         if (more) {
