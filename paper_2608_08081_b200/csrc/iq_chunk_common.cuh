@@ -15,9 +15,8 @@ __device__ __forceinline__ ChunkSeq chunk_seq(const ChunkParams& p, int b) {
   ChunkSeq s;
   s.ctx = max(0, min(p.ctx_lens[b], p.t_cap));
   if (p.token_start) {
-    const int first = max(0, min(p.token_start[b], p.n_tokens_max));
-    s.n = max(0, min(p.token_start[b + 1], p.n_tokens_max) - first);
-    s.tok0 = first;
+    s.n = packed_tokens(p.token_start, b, p.n_tokens_max);
+    s.tok0 = packed_start(p.token_start, b, p.n_tokens_max);
   } else {
     s.n = p.n_tokens ? max(0, min(p.n_tokens[b], p.n_tokens_max)) : p.n_tokens_max;
     s.tok0 = (long long)b * p.n_tokens_max;

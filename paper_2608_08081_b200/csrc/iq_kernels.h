@@ -49,14 +49,19 @@ struct QuantizeParams {
   uint32_t wait_polls;      // bulk: limit of the waits for tensor-core results: DEC_WAIT_LIMIT, or what the self-test asks for
 };
 #ifdef __CUDACC__
+// Where packed sequence b starts among `places` places, and how many tokens it has. (Both starts are brought into range before their
+// difference is taken, which then fits whatever they hold.)
+__device__ __forceinline__ int packed_start(const int32_t* token_start, int b, int places) { return max(0, min(token_start[b], places)); }
+__device__ __forceinline__ int packed_tokens(const int32_t* token_start, int b, int places) {
+  return max(0, packed_start(token_start, b + 1, places) - packed_start(token_start, b, places));
+}
 // New rows of sequence b, and where its first one starts, in elements from k_new or v_new.
 __device__ __forceinline__ int append_rows(const QuantizeParams& p, int b) {
-  int n = p.n_new ? p.n_new[b] : p.n_new_max;
-  if (p.token_start) n = min(p.token_start[b + 1], p.n_rows) - max(0, min(p.token_start[b], p.n_rows));
+  const int n = p.token_start ? packed_tokens(p.token_start, b, p.n_rows) : p.n_new ? p.n_new[b] : p.n_new_max;
   return min(n, p.n_new_max);
 }
 __device__ __forceinline__ size_t append_source(const QuantizeParams& p, int b) {
-  return p.token_start ? (size_t)max(0, min(p.token_start[b], p.n_rows)) * p.stride_t : (size_t)b * p.stride_b;
+  return p.token_start ? (size_t)packed_start(p.token_start, b, p.n_rows) * p.stride_t : (size_t)b * p.stride_b;
 }
 #endif
 cudaError_t launch_quantize_append(const QuantizeParams& p, int head_dim, int batch, cudaStream_t stream);

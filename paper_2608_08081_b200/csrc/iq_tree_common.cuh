@@ -34,9 +34,8 @@ __device__ __forceinline__ int tree_position(const TreeParams& p, int b, int t, 
 __device__ __forceinline__ int tree_tokens(const TreeParams& p, int b, long long& tok0) {
   int n;
   if (p.token_start) {
-    const int first = max(0, min(p.token_start[b], p.places));
-    n = max(0, min(p.token_start[b + 1], p.places) - first);
-    tok0 = first;
+    n = packed_tokens(p.token_start, b, p.places);
+    tok0 = packed_start(p.token_start, b, p.places);
   } else {
     n = p.n_tokens ? max(0, min(p.n_tokens[b], p.places)) : p.places;
     tok0 = (long long)b * p.places;
