@@ -657,8 +657,9 @@ int iq_quantize_append_packed(const iq_shape* shape, const float* rot_dev, const
  * n_tokens_max says that there are no longer ones, else 16 / heads per KV head in batches of two or more, of up to 2^13 and 2^15 sequences times KV
  * heads) go through iq_tree_attention's kernel, with its arithmetic. The same call with the same inputs gives the same bits every time on the same kind of
  * device; a sequence's bits can depend on which others are in the call, within these roundings.
- * Limits (IQ_ERR_LIMIT): n_tokens_max as above and times the heads per KV head below 2^31 - 128; t_cap at most 2^31 - 2^21; heads per KV head times
- * (t_cap + n_tokens_max) times n_kv_heads * batch * (n_tokens_max * heads per KV head / 128 + 1) tiles below about 2^53, also where packed.
+ * Limits (IQ_ERR_LIMIT): n_tokens_max as above and times the heads per KV head below 2^31 - 128; t_cap below 2^31 - 2^21; heads per KV head times
+ * (t_cap + n_tokens_max) times n_kv_heads * batch * (n_tokens_max * heads per KV head / 128 + 1) tiles below about 2^53, also where packed, and
+ * times t_cap / 128 below about 2^62.
  */
 #define IQ_CHUNK_MAX_TOKENS (1 << 20)
 size_t iq_chunk_workspace_bytes(const iq_shape* shape); /* 0: a shape that the calls refuse */

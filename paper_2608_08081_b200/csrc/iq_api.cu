@@ -1260,7 +1260,9 @@ static int chunk_attention(const iq_shape* shape, const float* rot_dev, const iq
   // units of the launch (chunk_units): tiles times what one can count; nothing says that packed sequences do not overlap, so they count as padded ones
   const double tokens = (double)n_tokens_max * shape->batch;
   const double tiles = shape->n_kv_heads * (tokens * group / 128.0 + shape->batch);
-  if (tiles * ((double)group * ((double)shape->t_cap + n_tokens_max + 1024.0) + 256.0) >= 9007199254740992.0) return IQ_ERR_LIMIT;
+  const double units = (double)group * ((double)shape->t_cap + n_tokens_max + 1024.0) + 256.0;
+  if (tiles * units >= 9007199254740992.0) return IQ_ERR_LIMIT;
+  if (units * ((double)shape->t_cap / 128.0 + 1.0) >= 4611686018427387904.0) return IQ_ERR_LIMIT;  // a share of a tile's blocks (chunk_blocks_before): 2^62
   if (shape->batch == 0 || n_tokens_max == 0) return IQ_OK;
   if (!q || !workspace_dev || !out) return IQ_ERR_NULL;
   if (!aligned16(q) || !aligned16(rot_dev) || !aligned16(workspace_dev) || !aligned16(out)) return IQ_ERR_ALIGN;

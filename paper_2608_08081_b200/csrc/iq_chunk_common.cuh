@@ -66,7 +66,7 @@ __device__ __forceinline__ ChunkTile chunk_tile(const ChunkParams& p, const Chun
   x.blocks = total - x.first + x.sink_blocks;
   return x;
 }
-// Blocks of an item before its unit o.
+// Blocks of an item before its unit o. (units * blocks < 2^62: the host's limit.)
 __device__ __forceinline__ int chunk_blocks_before(const ChunkParams& p, long long o, long long units, int blocks) {
   if (o >= units) return blocks;
   return o <= p.seg_units ? 0 : (int)chunk_div((o - p.seg_units) * blocks, units - p.seg_units);
