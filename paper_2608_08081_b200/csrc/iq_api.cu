@@ -1206,7 +1206,7 @@ namespace {
 struct ChunkPlan {
   int pairs;
   int short_tokens;  // sequences of up to so many tokens can be the tree attention kernel's (0: none can)
-  size_t part_acc, part_ml, cuts, short_acc, short_ml, short_info, total;
+  size_t part_acc, part_ml, cuts, kept, short_acc, short_ml, short_info, total;
 };
 int chunk_plan(const iq_shape* s, ChunkPlan& w) {
   const int rc = check_shape(s);
@@ -1218,6 +1218,7 @@ int chunk_plan(const iq_shape* s, ChunkPlan& w) {
   w.part_acc = o; o += rows * s->head_dim * 4;
   w.part_ml = o; o += rows * 8;
   w.cuts = o; o += (size_t)w.pairs * sizeof(iq::ChunkCut);
+  w.kept = o; o += 2 * (size_t)w.pairs * iq::chunk_kept(s->head_dim) * 16;
   const int group = s->n_q_heads / s->n_kv_heads;
   const size_t items = (size_t)s->batch * s->n_kv_heads;
   // (0.3 GB of partials at most at head_dim 128)
@@ -1316,6 +1317,7 @@ static int chunk_attention(const iq_shape* shape, const float* rot_dev, const iq
   p.part_acc = reinterpret_cast<float*>(ws + w.part_acc);
   p.part_ml = reinterpret_cast<float*>(ws + w.part_ml);
   p.cuts = reinterpret_cast<iq::ChunkCut*>(ws + w.cuts);
+  p.kept = reinterpret_cast<float4*>(ws + w.kept);
   p.out = static_cast<__half*>(out);
   p.lse = lse_out;
   p.status = status_dev;

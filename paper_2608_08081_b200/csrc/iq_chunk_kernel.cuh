@@ -5,12 +5,17 @@
 // t = S scale_K + log2(scale_V) - reference_pair in units of log2; p = 2^t; O[pair][coordinate] += p V, V the levels; l_pair += p / scale_V. The
 // output is R^T O / l.
 // A row's V scale is part of its exponent, so p is the row's weight in the OUTPUT, and the reference follows the largest of those: p
-// goes to the tensor cores as one binary16 value, whose 11 bits hold down to 2^-14 of it and which leaves out less than 2^-25 of it, also where
+// goes to the tensor cores as one binary16 value, whose 11 bits hold down to 2^-14 of it and which leaves out less than 2^-25 of it a row, also where
 // a row with most of the weight has next to no value. One term's rounding is as much error as that of the binary16 output; the queries' would
 // grow with the scores, so they have two (22 bits; of the largest element of the CTA's 128 pairs, as one power of two scales all of them).
 // References are raised only when a weight passes 2^15: then sums and O are scaled, which waits for the values of the step before (a raised
 // reference is the step's maximum; 5 log2 units below it, which would hold 5 bits more of the smallest weights, cost 172 us for 162 with 1000 tokens behind 6000 rows;
 // 3 units above it 161).
+//
+// Segments. The tensor core cuts its running sum towards zero with each product of 16 rows (measured: 1e-7 of the final sum, all in one direction), and
+// weights below 2^-25 of the reference are left out of O though not of l: both would grow with the rows, to 8e-4 and up to 2^-8 of an output behind 128 K of them.
+// So a piece is worked in segments of at most 8192 rows with references and sums of their own, joined in fp32 through each thread's own
+// places of the workspace: at most 5e-5 and 2^-12, however many rows there are.
 //
 // Work split. The two CTAs of a pair have 128 rows of Q, S and O each in their tensor memory, and half of the levels of a step each in shared memory: one
 // product of both (cta_group::2, M = 256) reads the operand once from either, and each block is dequantised once for 256 pairs. Warps of a
@@ -41,6 +46,9 @@ namespace iq {
 
 constexpr float CHUNK_LIMIT = 15.f;                   // log2 of the largest p ...
 constexpr float CHUNK_START = 0.f;                    // ... and of the step's largest behind a raise
+// Blocks of a segment (a power of two). 16, 32 and 64 blocks and no segments: 5.19, 5.18, 5.07 and 5.05 ms for 4096 tokens behind 28 000 rows; 175, 166, 159 and
+// 161 us for 1000 behind 6000.
+constexpr int CHUNK_SEGMENT = 64;
 constexpr float CHUNK_LEAST_SCALE = 8.67361738e-19f;  // 2^-60: V scales below it count as this
 
 // (Off by 2^-22 of the logarithm, and by one unit in the last place. log2f and a division: 1 % more time.)
@@ -70,6 +78,12 @@ __device__ __forceinline__ void chunk_ld_rows(uint32_t taddr, uint32_t (&r)[8]) 
 __device__ __forceinline__ void chunk_st_rows(uint32_t taddr, const uint32_t (&r)[8]) {
   asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr),
                "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+__device__ __forceinline__ void chunk_st_rows(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+               "r"(r[13]), "r"(r[14]), "r"(r[15])
                : "memory");
 }
 __device__ __forceinline__ void chunk_st_pairs(uint32_t taddr, const uint32_t (&r)[8]) {
@@ -134,6 +148,8 @@ struct ChunkLayout {
   static constexpr int NC = 32, NI = NC / 8;       // columns of S that a softmax warp takes at a time (of its 16 rows); groups of 8
   static constexpr int PARTS = NB / NC;
   static constexpr int SETS = D / 32;              // runs of 32 coordinates
+  static constexpr int SEGMENT = CHUNK_SEGMENT * SUB;  // steps of a segment (a power of two)
+  static constexpr size_t KEPT = chunk_kept(D);
   // Warps: softmax, K levels, V levels, products (one, in the first CTA of a pair), queries on their way. Registers of a thread: 96 at
   // launch, 480 over the five groups of warps (two of them softmax, two levels): as many as none of them spills with (152, 64 and 48: 2 - 8 % slower).
   static constexpr int SOFTMAX_WARPS = 8, K_WARP = 8, V_WARP = 12, MMA_WARP = 16, QUERY_WARP = 17, THREADS = 640;
@@ -465,7 +481,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
           if (j + 2 < steps) wait_k(n + 2);
           chunk_wait(&s.p_full[n & 1], (n >> 1) & 1, p.wait_polls, &s.failed);
           tc_fence_after();
-          values(n, j == 0);
+          values(n, (j & (L::SEGMENT - 1)) == 0);
           if (j + 2 < steps) scores(n + 2);
         }
       }
@@ -605,19 +621,80 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       return true;
     };
 
+    // What the segments of a piece before the present one have come to, in the thread's own places of the workspace: references and sums of its two
+    // rows, then O. Its factors for what is there (`had`) and for the present segment, and their references and sums joined.
+    float4* const kept = p.kept + (size_t)blockIdx.x * L::KEPT + tid;
+    auto join = [&](bool first, const float (&ref)[2], const float (&sum)[2], float (&had)[2], float (&now)[2]) {
+      const float4 x = first ? make_float4(-INFINITY, -INFINITY, 0.f, 0.f) : kept[0];
+      float4 y;
+      auto both = [](float r0, float l0, float r1, float l1, float& f0, float& f1, float& r, float& l) {
+        r = fmaxf(r0, r1);
+        f0 = r0 > -INFINITY ? ex2f(r0 - r) : 0.f;  // (nothing seen)
+        f1 = r1 > -INFINITY ? ex2f(r1 - r) : 0.f;
+        l = fmaf(l0, f0, l1 * f1);
+      };
+      both(x.x, x.z, ref[0], sum[0], had[0], now[0], y.x, y.z);
+      both(x.y, x.w, ref[1], sum[1], had[1], now[1], y.y, y.w);
+      return y;
+    };
+    // O so far = what is there and the present segment's, to the workspace, or (the last segment) back to tensor memory.
+    auto join_values = [&](bool first, bool last, const float (&had)[2], const float (&now)[2]) {
+#pragma unroll 1
+      for (int x = 0; x < D; x += 32) {
+        uint32_t o[16];
+        float4 y[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) y[i] = first ? make_float4(0.f, 0.f, 0.f, 0.f) : kept[256 * (1 + x / 8 + i)];
+        chunk_ld_rows(tmem + lanes16 + L::O_COL + x, o);
+        tc_wait_ld();
+        chunk_landed(o);
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          y[i].x = fmaf(__uint_as_float(o[4 * i]), now[0], y[i].x * had[0]);
+          y[i].y = fmaf(__uint_as_float(o[4 * i + 1]), now[0], y[i].y * had[0]);
+          y[i].z = fmaf(__uint_as_float(o[4 * i + 2]), now[1], y[i].z * had[1]);
+          y[i].w = fmaf(__uint_as_float(o[4 * i + 3]), now[1], y[i].w * had[1]);
+        }
+        if (last) {
+#pragma unroll
+          for (int i = 0; i < 4; i++) {
+            o[4 * i] = __float_as_uint(y[i].x);
+            o[4 * i + 1] = __float_as_uint(y[i].y);
+            o[4 * i + 2] = __float_as_uint(y[i].z);
+            o[4 * i + 3] = __float_as_uint(y[i].w);
+          }
+          chunk_st_rows(tmem + lanes16 + L::O_COL + x, o);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; i++) kept[256 * (1 + x / 8 + i)] = y[i];
+        }
+      }
+    };
+
     uint32_t pieces = 0;
     bool more = queries(0);
     while (more) {
       const ChunkPiece& c = s.piece[pieces & 3];
       const int steps = (c.hi - c.lo) * SUB;
-      float neg_ref[2], limit[2];  // minus the reference; what an exponent may be beside it (-inf: the pair has seen no row)
+      float neg_ref[2], limit[2];  // minus the reference; what an exponent may be beside it (-inf: the pair has seen no row of the segment)
       F32x2 l[2];
+      auto segment = [&]() {
 #pragma unroll
-      for (int k = 0; k < 2; k++) {
-        neg_ref[k] = 0.f;
-        limit[k] = -INFINITY;
-        l[k] = f32x2(0.f, 0.f);
-      }
+        for (int k = 0; k < 2; k++) {
+          neg_ref[k] = 0.f;
+          limit[k] = -INFINITY;
+          l[k] = f32x2(0.f, 0.f);
+        }
+      };
+      // References and sums of the segment.
+      auto sums = [&](float (&ref)[2], float (&sum)[2]) {
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+          ref[k] = limit[k] > -INFINITY ? -neg_ref[k] : -INFINITY;
+          sum[k] = l[k].lo() + l[k].hi();
+        }
+      };
+      segment();
       uint32_t whole_steps = 0;  // of 32 steps, those that all of the CTA's rows see whole: a lane looks at one
       auto first_of = [&](int j) { return c.x.block(c.lo + j / SUB) * 128 + (SUB > 1 ? (j & 1) * NB : 0); };  // a step's first row
       for (int j = 0; j < steps; j++, n++) {
@@ -626,6 +703,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
           const int r = first_of(min(j + lane, steps - 1));
           const int first_pos = c.sq.ctx + at / p.group, last_from = p.window > 0 ? c.sq.ctx + (at + 127) / p.group - p.window + 1 : 0;
           whole_steps = __ballot_sync(FULL, r + NB <= c.x.end && (!p.causal || r + NB - 1 <= first_pos) && (r >= last_from || r + NB <= p.sinks));
+        }
+        const bool begins = (j & (L::SEGMENT - 1)) == 0;
+        if (begins && j > 0) {  // ---- the segment that has ended is added to those before it
+          float ref[2], sum[2], had[2], now[2];
+          sums(ref, sum);
+          const bool first = j == L::SEGMENT;
+          const float4 y = join(first, ref, sum, had, now);
+          kept[0] = y;
+          chunk_wait(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1, p.wait_polls, &s.failed);
+          tc_fence_after();
+          join_values(first, false, had, now);
+          segment();
         }
         const bool whole = whole_steps >> (j & 31) & 1u;
         const uint32_t s_col = tmem + lanes16 + L::S_COL + (n & 1) * NB;
@@ -702,7 +791,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
                 for (int i = 0; i < NI; i++) t[x][k][i] = add2(t[x][k][i], f32x2(less, less));
             }
           }
-          if (j > 0) {
+          if (!begins) {
             chunk_wait(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1, p.wait_polls, &s.failed);
             tc_fence_after();
 #pragma unroll 1
@@ -740,14 +829,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       }
 
       // ---- sums and references of the rows
+      const bool joined = steps > L::SEGMENT;
+      float had[2], now[2];
+      {
+        float ref[2], sum[2];
+        sums(ref, sum);
+        if (joined) {
+          const float4 y = join(false, ref, sum, had, now);
+          ref[0] = y.x;
+          ref[1] = y.y;
+          sum[0] = y.z;
+          sum[1] = y.w;
+        }
 #pragma unroll
-      for (int k = 0; k < 2; k++) {
-        float all = l[k].lo() + l[k].hi();
-        all += __shfl_xor_sync(FULL, all, 1);
-        all += __shfl_xor_sync(FULL, all, 2);
-        if ((lane & 3) == 0) {
-          s.row_sum[row2 + 8 * k] = all;
-          s.row_ref[row2 + 8 * k] = limit[k] > -INFINITY ? -neg_ref[k] : -INFINITY;
+        for (int k = 0; k < 2; k++) {
+          float all = sum[k];
+          all += __shfl_xor_sync(FULL, all, 1);
+          all += __shfl_xor_sync(FULL, all, 2);
+          if ((lane & 3) == 0) {
+            s.row_sum[row2 + 8 * k] = all;
+            s.row_ref[row2 + 8 * k] = ref[k];
+          }
         }
       }
       // ---- the next piece's queries come first: its first products run under this one's outputs
@@ -759,6 +861,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       const float sum = s.row_sum[row], ref = s.row_ref[row];
       chunk_wait(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1, p.wait_polls, &s.failed);
       tc_fence_after();
+      if (joined) {
+        join_values(false, true, had, now);
+        tc_wait_st();
+        tc_fence_before();
+        cta_bar_sync_n(pair_bar, 64);
+        tc_fence_after();
+      }
       const uint32_t o_col = tmem + lanes + L::O_COL;
       if (c.slot >= 0) {
         // ---- a partial: eight rows of 32 bytes at a time (rows without a token included: nobody reads them)

@@ -278,6 +278,7 @@ struct ChunkParams {
   float* part_acc;             // [2 pairs][256][head_dim], rotated space
   float* part_ml;              // [2 pairs][256][2]: reference (log2 units), sum
   ChunkCut* cuts;              // [pairs]
+  float4* kept;                // [2 pairs][chunk_kept]: of the segments of a CTA's piece so far
   __half* out;
   float* lse;
   uint32_t* status;
@@ -292,6 +293,8 @@ constexpr int CHUNK_SEG_COST = 6, CHUNK_LEAST = 2;
 // one may (a launch of its own for them, with the limit's tile; most such sequences have one token. 28 sequences of one token beside four of 500: 0.59
 // ms, all of them here 0.96).
 constexpr int CHUNK_SHORT = 64, CHUNK_SHORT_MIXED = 16;
+// Places of a CTA's segments: references and sums, then O, a softmax thread's (256 of them) next to another's.
+constexpr size_t chunk_kept(int head_dim) { return 256 * (size_t)(1 + head_dim / 8); }
 cudaError_t launch_chunk_attention(const ChunkParams& p, int head_dim, cudaStream_t stream);
 
 // ---- a step's tokens: places, positions, cache rows

@@ -14,7 +14,8 @@ def iq():
 
 
 @pytest.mark.parametrize("d", [128, 256])
-@pytest.mark.parametrize("kw", [dict(H=8, hk=2, ctx=900, tokens=100), dict(B=3, H=16, hk=4, ctx=[3000, 0, 700], tokens=[600, 400, 90]), dict(H=4, hk=1, ctx=6000, tokens=70)])
+@pytest.mark.parametrize("kw", [dict(H=8, hk=2, ctx=900, tokens=100), dict(B=3, H=16, hk=4, ctx=[3000, 0, 700], tokens=[600, 400, 90]), dict(H=4, hk=1, ctx=6000, tokens=70),
+                                dict(H=16, hk=1, ctx=20000, tokens=600)])
 def test_waits_that_give_up_at_any_place(iq, d, kw):
     """Limits from no poll at all upwards run out in different roles and pieces. The outputs are then invalid; the call returns, with the flag
     where a wait ran out, and the same call without a limit of that kind is right behind it."""
