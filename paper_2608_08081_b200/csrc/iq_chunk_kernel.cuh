@@ -5,12 +5,13 @@
 // t = S scale_K + log2(scale_V) - reference_pair in units of log2; p = 2^t; O[pair][coordinate] += p V, V the levels; l_pair += p / scale_V. The
 // output is R^T O / l.
 // A row's V scale is part of its exponent, so p is the row's weight in the OUTPUT, and the reference follows the largest of those: p
-// goes to the tensor cores as one binary16 value, whose 11 bits hold down to 2^-14 of it and which leaves out less than 2^-25 of it a row, also where
-// a row with most of the weight has next to no value. One term's rounding is as much error as that of the binary16 output; the queries' would
-// grow with the scores, so they have two (22 bits; of the largest element of the CTA's 128 pairs, as one power of two scales all of them).
+// goes to the tensor cores as two binary16 terms (22 bits, or 2^-25 of the reference), also where a row with most of the weight has next to no
+// value. One term would add as much error as the binary16 output's own rounding (outputs 2.6e-4 - 2.8e-4 off in norm instead of 2.07e-4, which the rounding alone
+// makes), and a token's precision would hang on whether enough others come with it to take this kernel; it took 5.0 ms for 5.9 with 4096 tokens behind 28 000 rows, 159
+// us for 180 with 1000 behind 6000, half of the difference instructions, half products. The queries have two terms as well (22 bits), as their
+// error would grow with the scores.
 // References are raised only when a weight passes 2^15: then sums and O are scaled, which waits for the values of the step before (a raised
-// reference is the step's maximum; 5 log2 units below it, which would hold 5 bits more of the smallest weights, cost 172 us for 162 with 1000 tokens behind 6000 rows;
-// 3 units above it 161).
+// reference is the step's maximum; with it 5 log2 units lower, raises took 6 % of the time).
 //
 // Segments. The tensor core cuts its running sum towards zero with each product of 16 rows (measured: 1e-7 of the final sum, all in one direction), and
 // weights below 2^-25 of the reference are left out of O though not of l: both would grow with the rows, to 8e-4 and up to 2^-8 of an output behind 128 K of them.
@@ -23,13 +24,13 @@
 // tile's queries. Softmax warps meet nobody in the loop over the steps. Items (sequence, KV head, tile) are laid end to end and cut into
 // equal ranges, one per pair of CTAs; tiles that two or more pairs share are merged by a second launch.
 //
-// What bounds it. 4096 tokens behind 28 000 rows, 64/8 heads, 3 bits: 5.1 ms = 0.79 PFLOP/s of the 4 d a (pair, row) needs; the two terms of Q make it
-// 6 d, 1.19 PFLOP/s on the tensor pipe. A step of 128 rows takes the pipe 1536 cycles and a softmax warp some 2600, one instruction after the
-// other (of 2700 before the last changes: barrier 210, scores 250, exponents 850, exponentials and sums 1150, weights handed over 110, loop 150). Two buffers of scores
-// and a trip of 2100 cycles from weights to the scores that take their place keep the steps from overlapping further. The schedulers issue in 0.49 of
-// the cycles, the special-function pipe is busy 0.32, shift/logic 0.33, the tensor pipe 0.47 (1000 tokens behind 6000 rows, then 171 us, now 162, of
+// What bounds it. 4096 tokens behind 28 000 rows, 64/8 heads, 3 bits: 5.9 ms = 0.67 PFLOP/s of the 4 d a (pair, row) needs; the two terms of Q and of the
+// weights make it 8 d, 1.35 PFLOP/s on the tensor pipe. A step of 128 rows takes the pipe 2048 cycles and a softmax warp some 3000, one instruction after the
+// other (with one term to a weight 2600 - 2700: barrier 210, scores 250, exponents 850, exponentials and sums 1150, weights handed over 110, loop 150). Two buffers of
+// scores and the trip from weights to the scores that take their place (2100 cycles with one term) keep the steps from overlapping further. The schedulers issue
+// in 0.52 of the cycles, the special-function pipe is busy 0.31, shift/logic 0.35, the tensor pipe 0.60 (1000 tokens behind 6000 rows, 180 us, of
 // which the beginning and end of a piece take 6 us each).
-// Built and slower: one CTA to a tile (issue 0.55 of the cycles, half of it for levels: 5.9 ms for 5.1); four softmax warps to 32 rows, a quarter of the
+// Built and slower, with one term to a weight: one CTA to a tile (issue 0.55 of the cycles, half of it for levels: 5.9 ms for 5.1); four softmax warps to 32 rows, a quarter of the
 // columns each, which meet once a step (3200 cycles a step); a fourth to three quarters of the exponentials as polynomials of degree 4 on the
 // multiply-add pipe (215 us: 221, 228, 239); the next step's scores asked for before the weights are handed over (175 us: 185); the look at
 // the references behind the exponentials, which then run beside the exponents (no gain). Code that is
@@ -101,6 +102,15 @@ __device__ __forceinline__ void chunk_ld8(uint32_t taddr, uint32_t (&r)[8]) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                : "r"(taddr) : "memory");
 }
+// What two binary16 values have left of x and y, as two binary16 values. (A multiply-add that takes binary16 factors as they are: with conversions
+// before it, 1 % more time.)
+__device__ __forceinline__ uint32_t chunk_rest(uint32_t first, float x, float y) {
+  float a, b;
+  asm("{\n\t.reg .f16 u, v, m;\n\tmov.b16 m, 0xBC00;\n\tmov.b32 {u, v}, %2;\n\tfma.rn.f32.f16 %0, u, m, %3;\n\tfma.rn.f32.f16 %1, v, m, %4;\n\t}"
+      : "=f"(a), "=f"(b)
+      : "r"(first), "f"(x), "f"(y));
+  return pack_half2(a, b);
+}
 // Values that a tcgen05.ld has left in registers are not used before the wait for it.
 template <int C>
 __device__ __forceinline__ void chunk_landed(uint32_t (&r)[C]) {
@@ -154,8 +164,8 @@ struct ChunkLayout {
   // launch, 480 over the five groups of warps (two of them softmax, two levels): as many as none of them spills with (152, 64 and 48: 2 - 8 % slower).
   static constexpr int SOFTMAX_WARPS = 8, K_WARP = 8, V_WARP = 12, MMA_WARP = 16, QUERY_WARP = 17, THREADS = 640;
   static constexpr int SOFTMAX_REGS = 128, LEVEL_REGS = 72, MMA_REGS = 80;
-  // tensor memory: Q (D = 128: both terms; 256: the first), two buffers of scores, O. The probabilities of NC columns go over their
-  // scores, two to a column.
+  // tensor memory: Q (D = 128: both terms; 256: the first), two buffers of scores, O. The weights of NC columns go over their
+  // scores: the first terms in the first half of the columns, two to a column, the second terms in the second.
   static constexpr int Q_COL = 0, S_COL = 128, O_COL = 512 - D;
   // shared memory: K and V levels of some steps (this CTA's half of them: rows of K, coordinates of V), the tile's queries as they came, the
   // second term of Q (D = 256), the rest
@@ -455,8 +465,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
 #pragma unroll 1
           for (int k = 0; k < NB / 64; k++)  // 64 rows: two parts of weights
 #pragma unroll
-            for (int i = 0; i < 4; i++)
-              chunk_mma(tmem + L::O_COL, tmem + L::S_COL + o * NB + (2 * k + (i >> 1)) * NC + (i & 1) * 8, b + ((k * (D / 2 * 128) + i * 32) >> 4), L::IDESC_PV, !(first && k + i == 0));
+            for (int i = 0; i < 8; i++)  // 16 rows, their weights' second terms and then their first
+              chunk_mma(tmem + L::O_COL, tmem + L::S_COL + o * NB + (2 * k + (i >> 2)) * NC + (i & 1 ? 0 : NC / 2) + (i >> 1 & 1) * 8, b + ((k * (D / 2 * 128) + (i >> 1) * 32) >> 4), L::IDESC_PV,
+                        !(first && k + i == 0));
           chunk_commit(&s.o_done[o]);
           chunk_commit(&s.v_empty[st]);
         }
@@ -809,7 +820,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         // ---- weights, over the scores, and their sums
 #pragma unroll
         for (int x = 0; x < PARTS; x++) {
-          uint32_t pk[2 * NI];
+          uint32_t pk[2 * NI], rest[2 * NI];
 #pragma unroll
           for (int i = 0; i < NI; i++) {
             const float2 a = *reinterpret_cast<const float2*>(wt + NC * x + 8 * i);
@@ -818,9 +829,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
               const F32x2 e = f32x2(ex2f(t[x][k][i].lo()), ex2f(t[x][k][i].hi()));
               l[k] = fma2(e, f32x2(a.x, a.y), l[k]);
               pk[2 * i + k] = pack_half2(e.lo(), e.hi());
+              rest[2 * i + k] = chunk_rest(pk[2 * i + k], e.lo(), e.hi());
             }
           }
           chunk_st_pairs(s_col + NC * x, pk);
+          chunk_st_pairs(s_col + NC * x + NC / 2, rest);
         }
         tc_wait_st();
         tc_fence_before();

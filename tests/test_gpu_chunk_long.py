@@ -37,7 +37,8 @@ def shrunk(c, out, at, causal):
 
 @pytest.mark.parametrize("d,cross", [(128, False), (256, False), (128, True)])
 def test_values_of_one_sign(iq, d, cross):
-    """A product adds 16 rows and cuts the sum so far towards zero, by 2^-23 of it at most: 512 products in a segment. All else rounds to nearest,
+    """A product adds 16 rows and cuts the sum so far towards zero, by 2^-23 of it at most: 512 products in a segment (those of the
+    weights' second terms come before the first of the same rows and are given no share of their own). All else rounds to nearest,
     independently from row to row, and averages out over the 64 heads: 2^-16 is allowed for it (an output's own rounding is 2^-11 / sqrt(3) of
     an element, some 2^-18.4 of the mean over a token's 64 d). Over the whole context it would be 8192 products, a cut of 2^-11.4 or so."""
     c = step(iq, d, 131072 - 320, cross)
