@@ -180,7 +180,8 @@ struct ChunkLayout {
 template <int D>
 struct ChunkShared {
   using L = ChunkLayout<D>;
-  // In the first CTA, arrived at by both: k_full, v_full, p_full, q_ready. In each: the others.
+  // In the first CTA, arrived at by both: k_full, v_full, p_full, q_ready. In the second: column_full. In each: the others.
+  uint64_t column_full[L::COLUMNS];          // the factors of a step's columns
   uint64_t k_full[L::STAGES], k_empty[L::STAGES], v_full[L::STAGES], v_empty[L::STAGES];
   uint64_t s_full[2], p_full[2], o_done[2];  // of even and odd steps
   uint64_t q_ready, raw_full, raw_empty, drain;
@@ -213,7 +214,8 @@ __device__ __forceinline__ uint32_t chunk_at(const void* p, uint32_t rank) {
   return a;
 }
 // (No generic write of one CTA is read by the other: levels and second terms are read by products, behind a proxy fence, the rest lies in tensor
-// memory. A release at the pair's scope would wait for every load and store of the thread.)
+// memory. The factors of a step's columns are passed on within each CTA: arrivals and waits at the pair's scope took 15 % more time, as a release
+// there waits for every load and store of the thread.)
 __device__ __forceinline__ void chunk_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void chunk_pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -319,6 +321,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       mbar_init(&s.k_empty[i], 1);
       mbar_init(&s.v_empty[i], 1);
     }
+    for (int i = 0; i < L::COLUMNS; i++) mbar_init(&s.column_full[i], NB / 32);
     for (int i = 0; i < 2; i++) {
       mbar_init(&s.s_full[i], 2);
       mbar_init(&s.o_done[i], 1);
@@ -434,7 +437,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       // (an operand further on in shared memory: its descriptor plus the distance in units of 16 bytes, which stays within the address's bits)
       const uint64_t k_desc = smem_desc_k128(smem_u32(smem + L::OFF_K)), v_desc = smem_desc_k128(smem_u32(smem + L::OFF_V));
       const uint64_t q_desc = smem_desc_k128(smem_u32(smem + L::OFF_Q));
-      const uint32_t s_full_1[2] = {chunk_at(&s.s_full[0], 1), chunk_at(&s.s_full[1], 1)};
       constexpr int ROLL = D == 256 ? 8 : 1;  // (a product of 64 columns takes half as long as the loop around four of them allows for)
       auto scores = [&](uint32_t i) {  // S = Q K^T of step i, whose levels are there; the second terms first
         const uint32_t o = i & 1, st = i % ST;
@@ -453,8 +455,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
           }
           chunk_commit(&s.s_full[o]);
           chunk_commit(&s.k_empty[st]);
-          mbar_arrive(&s.s_full[o]);  // (these pass on the factors of the step's columns, which came with the levels)
-          chunk_arrive(s_full_1[o]);
+          mbar_arrive(&s.s_full[o]);  // (passes on the factors of the step's columns, which came with this CTA's levels)
         }
         __syncwarp();
       };
@@ -496,6 +497,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
           if (j + 2 < steps) scores(n + 2);
         }
       }
+    } else {
+      // ================================================================ in the second CTA: the factors of a step's columns passed on beside its scores
+      while (walk.next(p, c))
+        for (int j = (c.hi - c.lo) * SUB; j > 0; j--, n++) {
+          chunk_wait(&s.column_full[n % L::COLUMNS], (n / L::COLUMNS) & 1, p.wait_polls, &s.failed);
+          if (n >= 2) chunk_wait(&s.s_full[n & 1], ((n >> 1) - 1) & 1, p.wait_polls, &s.failed);  // (one arrival to a phase)
+          if (lane == 0) mbar_arrive(&s.s_full[n & 1]);
+          __syncwarp();
+        }
     }
   } else if (warp >= L::K_WARP) {
     // ================================================================ levels: of K, a thread 64 coordinates of a row, and the factors of the
@@ -550,7 +560,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
       if (have) load();
       fence_proxy_async();
       __syncwarp();
-      if (lane == 0) chunk_arrive(full + 8 * st);
+      if (lane == 0) {
+        chunk_arrive(full + 8 * st);
+        if (factors && rank == 1) mbar_arrive(&s.column_full[n % L::COLUMNS]);
+      }
       n++;
     }
   } else {
