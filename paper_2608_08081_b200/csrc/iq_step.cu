@@ -99,7 +99,7 @@ constexpr int ROTARY_TOKENS = 16;  // most tokens of a CTA
 // Bound by memory: 8192 tokens, 64/8 heads of 128: 55.6 us = 5.4 TB/s read and written (one token 2.9). Two tasks of a thread in flight: slower;
 // as many threads as fill all rounds: 57.4 us (1000 tokens, 32/8 heads: 6.05 for 6.75); the first elements asked for before the angles are worked out: 60.5 us (2107 tokens, 16/8 heads of 256, a quarter turned: 10.6 for 11.7).
 __global__ void __launch_bounds__(ROTARY_THREADS) rotary_kernel(const __grid_constant__ RotaryParams p, int tokens) {
-  __shared__ float2 turn[ROTARY_TOKENS * IQ_ROTARY_MAX_PAIRS];  // cosines and sines times the magnitude, [token][pair]
+  __shared__ alignas(16) float2 turn[ROTARY_TOKENS * IQ_ROTARY_MAX_PAIRS];  // cosines and sines times the magnitude, [token][pair]; read two at a time
   __shared__ int position[ROTARY_TOKENS];
   const int tid = threadIdx.x, pairs = p.rotary.rotary_dim / 2;
   const int first = blockIdx.x * tokens, n = min(tokens, p.n_tokens - first);
