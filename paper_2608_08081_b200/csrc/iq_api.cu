@@ -1178,6 +1178,7 @@ int iq_apply_rotary(const iq_shape* shape, const iq_rotary* rotary, const void* 
   if (!rotary) return IQ_ERR_NULL;
   if (rotary->rotary_dim <= 0 || (rotary->rotary_dim & 15) || rotary->rotary_dim > shape->head_dim) return IQ_ERR_SHAPE;
   if (n_tokens < 0) return IQ_ERR_SHAPE;
+  if (n_tokens == 0) return IQ_OK;  // (before the pointers are looked at: an empty array's may be NULL)
   if (!q && !k) return IQ_ERR_NULL;
   if ((q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr)) return IQ_ERR_NULL;
   const int64_t strides[8] = {q_stride_t, q_stride_h, q_out_stride_t, q_out_stride_h, k_stride_t, k_stride_h, k_out_stride_t, k_out_stride_h};
@@ -1189,7 +1190,6 @@ int iq_apply_rotary(const iq_shape* shape, const iq_rotary* rotary, const void* 
   if ((q && q == q_out && (q_stride_t != q_out_stride_t || q_stride_h != q_out_stride_h)) ||
       (k && k == k_out && (k_stride_t != k_out_stride_t || k_stride_h != k_out_stride_h)))
     return IQ_ERR_SHAPE;  // in place, with other strides
-  if (n_tokens == 0) return IQ_OK;
   if (!positions_dev) return IQ_ERR_NULL;
   iq::RotaryParams p = {};
   p.side[0] = {static_cast<const __half*>(q), static_cast<__half*>(q_out), q_stride_t, q_stride_h, q_out_stride_t, q_out_stride_h, q ? shape->n_q_heads : 0};
