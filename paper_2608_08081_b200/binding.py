@@ -663,10 +663,12 @@ def _token_rows(x, heads, head_dim):
     else:
         B, T, h, d = size
         s_b, s_t, s_h, s_d = st
-        assert B <= 1 or s_b == T * s_t  # the tokens of all sequences as one run
         n = B * T
+        if T == 1:
+            s_t = s_b                                # (a token's own stride is then nobody's)
+        assert B <= 1 or T <= 1 or s_b == T * s_t    # the tokens of all sequences as one run
     assert x.dtype is torch.float16 and h == heads and d == head_dim and s_d == 1
-    return n, s_t, s_h
+    return n, 0 if n <= 1 else s_t, 0 if h <= 1 else s_h  # (what is not stepped over may be anything in a tensor)
 
 
 def iq_apply_rotary(shape: Shape, rotary: Rotary, q, k, positions, q_out=None, k_out=None, stream=None) -> None:
