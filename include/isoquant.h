@@ -93,7 +93,7 @@ enum {
 };
 
 enum {
-  IQ_STATUS_ROW_OUT_OF_RANGE = 1u, /* quantize-append: append_pos + i >= t_cap, row skipped */
+  IQ_STATUS_ROW_OUT_OF_RANGE = 1u, /* quantize-append: append_pos + i >= t_cap, row skipped; packed: also more rows than n_new_max */
   IQ_STATUS_WAIT_TIMEOUT = 2u,     /* decode, tree, chunk and cross attention, bulk append: a bounded wait on an asynchronous copy or tensor-core result ran out; results invalid */
   IQ_STATUS_SCALE_OVERFLOW = 8u,   /* binary16 scales: a row norm above 65504 was stored as 65504 */
   IQ_STATUS_BAD_PAGE = 4u,         /* paged cache: a block-table entry outside [0, num_pages) was met: read as page 0 by
@@ -626,7 +626,8 @@ int iq_apply_rotary(const iq_shape* shape, const iq_rotary* rotary, const void* 
 
 /*
  * iq_quantize_append for a packed step: new row i of sequence b is k_new, v_new row token_start[b] + i (element (t, h, c) at t*stride_t +
- * h*stride_h + c, t < n_tokens_max), for i < token_start[b + 1] - token_start[b], at most n_new_max of them. Everything else as there.
+ * h*stride_h + c, t < n_tokens_max), for i < token_start[b + 1] - token_start[b], at most n_new_max of them: the rows behind those are left out, flagged
+ * (IQ_STATUS_ROW_OUT_OF_RANGE) and counted like rows outside the cache. Everything else as there.
  */
 int iq_quantize_append_packed(const iq_shape* shape, const float* rot_dev, const iq_codebook* codebook, const void* k_new,
                               const void* v_new, int64_t stride_t, int64_t stride_h, const int32_t* append_pos_dev,

@@ -504,6 +504,7 @@ __global__ void __launch_bounds__(BulkLayout<D>::THREADS, 1) append_bulk_kernel(
       int pos0, n;
       long long blk0;
       sum += seq_blocks(b, pos0, n, blk0);
+      if (blockIdx.x == 0) append_left_out(p, b, 2 * p.n_kv_heads);
     }
     long long inc = sum;
 #pragma unroll

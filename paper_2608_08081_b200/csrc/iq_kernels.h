@@ -60,6 +60,15 @@ __device__ __forceinline__ int append_rows(const QuantizeParams& p, int b) {
   const int n = p.token_start ? packed_tokens(p.token_start, b, p.n_rows) : p.n_new ? p.n_new[b] : p.n_new_max;
   return min(n, p.n_new_max);
 }
+// Rows of packed sequence b that n_new_max leaves out: flagged, and counted `times` each. By one thread per sequence, or with times = 1 by one per
+// (sequence, KV head, side).
+__device__ __forceinline__ void append_left_out(const QuantizeParams& p, int b, int times) {
+  if (p.token_start == nullptr || p.status == nullptr) return;
+  const int left = packed_tokens(p.token_start, b, p.n_rows) - p.n_new_max;
+  if (left <= 0) return;
+  atomicOr(&p.status[0], IQ_STATUS_ROW_OUT_OF_RANGE);
+  atomicAdd(&p.status[2], (uint32_t)left * (uint32_t)times);
+}
 __device__ __forceinline__ size_t append_source(const QuantizeParams& p, int b) {
   return p.token_start ? (size_t)packed_start(p.token_start, b, p.n_rows) * p.stride_t : (size_t)b * p.stride_b;
 }

@@ -125,6 +125,7 @@ __global__ void __launch_bounds__(32) quantize_append_few_kernel(const __grid_co
   const int h = blockIdx.y, b = blockIdx.z;
   const int n_new = append_rows(p, b);
   if (n_new <= 0) return;
+  if (chunk == 0 && lane == 0) append_left_out(p, b, 1);
   const long long pos0 = p.append_pos[b];
   // rows i with floor((pos0 + i) / 128) == floor(pos0 / 128) + chunk (rows at negative positions: chunk 0, they are refused below)
   const long long blk0 = pos0 >= 0 ? pos0 / 128 : 0;
