@@ -652,7 +652,8 @@ int iq_quantize_append_packed(const iq_shape* shape, const float* rot_dev, const
  *   lse_out        device fp32, the same without the last dimension, or NULL.
  *   status_dev     optional (see top). Pages whose rows no token sees need not be in the block table.
  * Codebooks as for iq_decode_attention; scales must not be negative. A token that sees no row yields out = 0, lse = -inf.
- * Arithmetic: q~ as two binary16 terms (22 bits of the largest element of 128 (token, head) pairs), levels exact; a row's weight times its V
+ * Arithmetic: q~ as two binary16 terms (an element is off by 2^-22 of itself, or by 2^-33 of the largest finite element of the queries of the 128 (token,
+ * head) pairs it is worked with), levels exact; a row's weight times its V
  * scale, relative to the largest such of its token, as two binary16 terms (off by 2^-22 of itself, or 2^-25 of the largest); tensor-core
  * sums over 8192 rows at most, each with a largest of its own and cut towards zero (5e-5 of values of one sign), joined in fp32: neither grows with the rows. V scales below 2^-60 count as 2^-60. Sequences of few tokens (64 / heads per KV head where
  * n_tokens_max says that there are no longer ones, else 16 / heads per KV head in batches of two or more, of up to 2^13 and 2^15 sequences times KV

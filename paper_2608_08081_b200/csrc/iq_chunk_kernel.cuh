@@ -8,8 +8,8 @@
 // goes to the tensor cores as two binary16 terms (22 bits, or 2^-25 of the reference), also where a row with most of the weight has next to no
 // value. One term would add as much error as the binary16 output's own rounding (outputs 2.6e-4 - 2.8e-4 off in norm instead of 2.07e-4, which the rounding alone
 // makes), and a token's precision would hang on whether enough others come with it to take this kernel; it took 5.0 ms for 5.9 with 4096 tokens behind 28 000 rows, 159
-// us for 180 with 1000 behind 6000, half of the difference instructions, half products. The queries have two terms as well (22 bits), as their
-// error would grow with the scores.
+// us for 180 with 1000 behind 6000, half of the difference instructions, half products. The queries have two terms as well, as their
+// error would grow with the scores: 2^-22 of an element, or 2^-25 where one power of two scales the CTA's 128 pairs to a largest element of 2^8 to 2^9.
 // References are raised only when a weight passes 2^15: then sums and O are scaled, which waits for the values of the step before (a raised
 // reference is the step's maximum; with it 5 log2 units lower, raises took 6 % of the time).
 //
