@@ -42,11 +42,7 @@ __device__ __forceinline__ long long chunk_units_before(const ChunkParams& p, co
 __device__ __forceinline__ long long chunk_seq_units(const ChunkParams& p, const ChunkSeq& s) {
   return (long long)p.n_kv_heads * chunk_units_before(p, s, s.tiles);
 }
-// (The products of most launches fit 32 bits, whose division takes a fraction of the time.)
-__device__ __forceinline__ long long chunk_div(long long a, long long b) {
-  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
-__device__ __forceinline__ long long chunk_cut(long long total, int pair, int pairs) { return chunk_div(total * pair, pairs); }
+__device__ __forceinline__ long long chunk_cut(long long total, int pair, int pairs) { return unit_div(total * pair, pairs); }
 
 // The blocks of 128 rows that a tile's tokens see: the first `sink_blocks`, then those from the first window on.
 struct ChunkTile {
@@ -69,7 +65,7 @@ __device__ __forceinline__ ChunkTile chunk_tile(const ChunkParams& p, const Chun
 // Blocks of an item before its unit o. (units * blocks < 2^62: the host's limit.)
 __device__ __forceinline__ int chunk_blocks_before(const ChunkParams& p, long long o, long long units, int blocks) {
   if (o >= units) return blocks;
-  return o <= p.seg_units ? 0 : (int)chunk_div((o - p.seg_units) * blocks, units - p.seg_units);
+  return o <= p.seg_units ? 0 : (int)unit_div((o - p.seg_units) * blocks, units - p.seg_units);
 }
 
 // The launch's items (sequence, KV head, tile), laid end to end and cut into one range of equal length per pair of CTAs.
@@ -92,7 +88,7 @@ __device__ __forceinline__ ChunkRange chunk_range(const ChunkParams& p, int pair
 #pragma unroll 1
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(FULL, total, o);
   r.total = total;
-  r.pairs = (int)max(1ll, min((long long)p.pairs, chunk_div(total, p.least_units)));
+  r.pairs = (int)max(1ll, min((long long)p.pairs, unit_div(total, p.least_units)));
   r.at = r.end = total;
   r.b = 0;
   r.seq_at = 0;
@@ -158,7 +154,7 @@ struct ChunkWalk {
     sq = r.sq;
     const long long head = chunk_units_before(p, sq, sq.tiles);
     long long rest = unit - r.seq_at;
-    g = (int)chunk_div(rest, head);
+    g = (int)unit_div(rest, head);
     rest -= g * head;
     int lo = 0, hi = sq.tiles;  // the last tile that starts at or before it
     while (hi - lo > 1) {

@@ -429,7 +429,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ChunkLayout<D>::THRE
         pieces++;
       }
       if (t == 0 && rank == 0) {  // (also where a wait gave up, whose pieces have not all been walked: the outputs are invalid, the places are not)
-        if (walk.cut.last == 0) walk.cut.last = (int)min((long long)s.range.pairs - 1, chunk_div(walk.cut_end * s.range.pairs - 1, s.range.total));
+        if (walk.cut.last == 0) walk.cut.last = (int)min((long long)s.range.pairs - 1, unit_div(walk.cut_end * s.range.pairs - 1, s.range.total));
         p.cuts[pair] = walk.cut;
       }
     } else if (rank == 0) {

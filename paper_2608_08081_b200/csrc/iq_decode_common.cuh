@@ -194,6 +194,11 @@ __device__ __forceinline__ void dequant32_f16(const uint32_t* w, const uint32_t 
   }
 }
 
+// a / b of numbers that are not negative. (Units of work: the products of most launches fit 32 bits, whose division takes a fraction of the time.)
+__device__ __forceinline__ long long unit_div(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 // Pairs of fp32 values, one instruction for the two (each rounded like the scalar operation).
 struct F32x2 {
   uint64_t v;

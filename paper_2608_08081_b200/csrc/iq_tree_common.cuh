@@ -94,13 +94,9 @@ struct TreeRange {
   int b;                     // the sequence in which the range starts
   long long seq_at;          // where that sequence starts
 };
-// (total * ctas < 2^63: an item takes 8 KB of the workspace, so a launch has some 2^25 of them at most, each of at most 2^24 blocks. The
-// products of most launches fit 32 bits, whose division takes a fraction of the time.)
-__device__ __forceinline__ long long tree_div(long long a, long long b) {
-  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
-__device__ __forceinline__ long long tree_cut(long long total, int cta, int ctas) { return tree_div(total * cta, ctas); }
-__device__ __forceinline__ int tree_cta_of(long long unit, long long total, int ctas) { return (int)tree_div((unit + 1) * ctas - 1, total); }
+// (total * ctas < 2^63: an item takes 8 KB of the workspace, so a launch has some 2^25 of them at most, each of at most 2^24 blocks.)
+__device__ __forceinline__ long long tree_cut(long long total, int cta, int ctas) { return unit_div(total * cta, ctas); }
+__device__ __forceinline__ int tree_cta_of(long long unit, long long total, int ctas) { return (int)unit_div((unit + 1) * ctas - 1, total); }
 
 // By one converged warp, 32 sequences at a time: first the launch's units, then the sequence that this CTA's range starts in. (The other
 // warps need neither; with all of them at it, each fetching the code, a launch over one short sequence took 2 us longer.)

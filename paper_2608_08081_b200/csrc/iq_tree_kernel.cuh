@@ -416,7 +416,7 @@ __global__ void __launch_bounds__((TreeLayout<D, BITS, N>::THREADS), (TreeLayout
         while (count < TREE_BATCH && at < range.end) {
           if (at >= seq_at + sq.weight) { seq_at += sq.weight; sq = tree_seq<N>(p, ++b); continue; }
           const int len = sq.blocks + TREE_SEG_COST;
-          const int m = (int)tree_div(at - seq_at, len);  // item of the sequence
+          const int m = (int)unit_div(at - seq_at, len);  // item of the sequence
           const long long item_at = seq_at + (long long)m * len;
           const int off = (int)(at - item_at), take = (int)min((long long)(len - off), range.end - at);
           const int lo = max(off - TREE_SEG_COST, 0), hi = max(off + take - TREE_SEG_COST, 0), g = m / sq.tiles, tile = m - g * sq.tiles;
