@@ -7,8 +7,8 @@
 // A row's V scale is part of its exponent, so p is the row's weight in the OUTPUT, and the reference follows the largest of those: p
 // goes to the tensor cores as two binary16 terms (22 bits, or 2^-25 of the reference), also where a row with most of the weight has next to no
 // value. One term would add as much error as the binary16 output's own rounding (outputs 2.6e-4 - 2.8e-4 off in norm instead of 2.07e-4, which the rounding alone
-// makes), and a token's precision would hang on whether enough others come with it to take this kernel; it took 5.0 ms for 5.9 with 4096 tokens behind 28 000 rows, 159
-// us for 180 with 1000 behind 6000, half of the difference instructions, half products. The queries have two terms as well, as their
+// makes), and a token's precision would hang on whether enough others come with it to take this kernel; it took 5.0 ms for 6.0 with 4096 tokens behind 28 000 rows, 159
+// us for 179 with 1000 behind 6000, half of the difference instructions, half products. The queries have two terms as well, as their
 // error would grow with the scores: 2^-22 of an element, or 2^-25 where one power of two scales the CTA's 128 pairs to a largest element of 2^8 to 2^9.
 // References are raised only when a weight passes 2^15: then sums and O are scaled, which waits for the values of the step before (a raised
 // reference is the step's maximum; with it 5 log2 units lower, raises took 6 % of the time).
@@ -24,7 +24,7 @@
 // tile's queries. Softmax warps meet nobody in the loop over the steps. Items (sequence, KV head, tile) are laid end to end and cut into
 // equal ranges, one per pair of CTAs; tiles that two or more pairs share are merged by a second launch.
 //
-// What bounds it. 4096 tokens behind 28 000 rows, 64/8 heads, 3 bits: 5.9 ms = 0.67 PFLOP/s of the 4 d a (pair, row) needs; the two terms of Q and of the
+// What bounds it. 4096 tokens behind 28 000 rows, 64/8 heads, 3 bits: 6.0 ms = 0.67 PFLOP/s of the 4 d a (pair, row) needs; the two terms of Q and of the
 // weights make it 8 d, 1.35 PFLOP/s on the tensor pipe. A step of 128 rows takes the pipe 2048 cycles and a softmax warp some 3000, one instruction after the
 // other (with one term to a weight 2600 - 2700: barrier 210, scores 250, exponents 850, exponentials and sums 1150, weights handed over 110, loop 150). Two buffers of
 // scores and the trip from weights to the scores that take their place (2100 cycles with one term) keep the steps from overlapping further. The schedulers issue
@@ -47,8 +47,8 @@ namespace iq {
 
 constexpr float CHUNK_LIMIT = 15.f;                   // log2 of the largest p ...
 constexpr float CHUNK_START = 0.f;                    // ... and of the step's largest behind a raise
-// Blocks of a segment (a power of two). 16, 32 and 64 blocks and no segments: 5.19, 5.18, 5.07 and 5.05 ms for 4096 tokens behind 28 000 rows; 175, 166, 159 and
-// 161 us for 1000 behind 6000.
+// Blocks of a segment (a power of two). 16, 32 and 64 blocks and no segments, with one term to a weight: 5.19, 5.18, 5.07 and 5.05 ms for 4096 tokens behind 28 000
+// rows; 175, 166, 159 and 161 us for 1000 behind 6000.
 constexpr int CHUNK_SEGMENT = 64;
 constexpr float CHUNK_LEAST_SCALE = 8.67361738e-19f;  // 2^-60: V scales below it count as this
 

@@ -294,13 +294,13 @@ struct ChunkParams {
   uint32_t wait_polls;
 };
 // What an item costs beside its blocks (queries, outputs or a partial), and the least that a pair of CTAs is given, in blocks. With 3, 4, 6, 8 in
-// place of 6: 2047 tokens of a prompt 124, 119, 113, 115 us; 1000 tokens of a window of 4096 rows, head_dim 256, 277, 273, 265, 264; 64
-// tokens behind 1000 rows 37.6, 38.0, 38.2, 39.6; 4 for the least 39.7.
+// place of 6: 2047 tokens of a prompt 111, 107, 101, 106 us; 1000 tokens of a window of 4096 rows, head_dim 256, 140, 139, 145, 145; 64
+// tokens behind 1000 rows 28.3, 28.5, 28.6, 29.3; 4 for the least 30.6.
 constexpr int CHUNK_SEG_COST = 6, CHUNK_LEAST = 2;
 // (token, head) pairs of a KV head up to which a sequence of a step is the tree attention kernel's, whose tiles are that small: where the call
-// says that no sequence has more (64 pairs of 16 sequences of 16 K rows 181 us, here 352; of one of 1000 rows 20 and 26); and where
-// one may (a launch of its own for them, with the limit's tile; most such sequences have one token. 28 sequences of one token beside four of 500: 0.59
-// ms, all of them here 0.96).
+// says that no sequence has more (64 pairs of 16 sequences of 16 K rows 180 us, here 367; of one of 1000 rows 20 and 25); and where
+// one may (a launch of its own for them, with the limit's tile; most such sequences have one token. 28 sequences of one token beside four of 500: 0.56
+// ms, all of them here 0.99).
 constexpr int CHUNK_SHORT = 64, CHUNK_SHORT_MIXED = 16;
 // Places of a CTA's segments: references and sums, then O, a softmax thread's (256 of them) next to another's.
 constexpr size_t chunk_kept(int head_dim) { return 256 * (size_t)(1 + head_dim / 8); }
