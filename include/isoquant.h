@@ -655,7 +655,7 @@ int iq_quantize_append_packed(const iq_shape* shape, const float* rot_dev, const
  * Arithmetic: q~ as two binary16 terms (an element is off by 2^-22 of itself, or by 2^-33 of the largest finite element of the queries of the 128 (token,
  * head) pairs it is worked with), levels exact; a row's weight times its V
  * scale, relative to the largest such of its token, as two binary16 terms (off by 2^-22 of itself, or 2^-25 of the largest); tensor-core
- * sums over 8192 rows at most, each with a largest of its own and cut towards zero (5e-5 of values of one sign), joined in fp32: neither grows with the rows. V scales below 2^-60 count as 2^-60. Sequences of few tokens (64 / heads per KV head where
+ * sums over 8192 rows at most, each with a largest of its own and cut towards zero (some 5e-5 of values of one sign), joined in fp32: neither grows with the rows. V scales below 2^-60 count as 2^-60. Sequences of few tokens (64 / heads per KV head where
  * n_tokens_max says that there are no longer ones, else 16 / heads per KV head in batches of two or more, of up to 2^13 and 2^15 sequences times KV
  * heads) go through iq_tree_attention's kernel, with its arithmetic. The same call with the same inputs gives the same bits every time on the same kind of
  * device; a sequence's bits can depend on which others are in the call, within these roundings.

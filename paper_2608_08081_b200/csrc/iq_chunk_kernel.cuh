@@ -16,7 +16,7 @@
 // Segments. The tensor core cuts its running sum towards zero with each product of 16 rows (measured: 1e-7 of the final sum, all in one direction), and
 // weights below 2^-25 of the reference are left out of O though not of l: both would grow with the rows, to 8e-4 and up to 2^-8 of an output behind 128 K of them.
 // So a piece is worked in segments of at most 8192 rows with references and sums of their own, joined in fp32 through each thread's own
-// places of the workspace: at most 5e-5 and 2^-12, however many rows there are.
+// places of the workspace: some 5e-5 and at most 2^-12, however many rows there are.
 //
 // Work split. The two CTAs of a pair have 128 rows of Q, S and O each in their tensor memory, and half of the levels of a step each in shared memory: one
 // product of both (cta_group::2, M = 256) reads the operand once from either, and each block is dequantised once for 256 pairs. Warps of a
